@@ -437,6 +437,85 @@ int dualgcn_weight_grad_noalloc(const void *X, const void *G, float *dW, int32_t
 int dualgcn_backward_data(const void *G, const float *W, const void *M, float *dX, int32_t n,
                           int32_t F_in, int32_t F_out, uint32_t flags, void *stream);
 
+/* ------------------------------------------------------------------ deep GCNs */
+
+/* Flags of the norms around a block. */
+#define DUALGCN_STREAM_BF16 16u   /* the residual stream (R, Rn) and its gradients hold bfloat16 */
+#define DUALGCN_NORM_LAYER 32u    /* layer norms (the mean is taken off); else RMS norms */
+#define DUALGCN_NORM_POST 64u     /* the block's output is normed before its gate */
+#define DUALGCN_GATE_FEATURE 128u /* gate: float32[F], one for each feature */
+#define DUALGCN_GATE_NODE 256u    /* gate: float32[n], one for each node */
+#define DUALGCN_GATE_FULL 512u    /* gate: n x F, float32 or (DUALGCN_IN_BF16) bfloat16 */
+#define DUALGCN_GATE_SIGMOID 1024u /* the gate holds logits: their sigmoid multiplies */
+
+/*
+ * The norms of a residual block.  The vectors are float32[F] (device); a NULL weight is all
+ * ones, a NULL bias all zeros.  gate goes by the flags (at most one of the three kinds; NULL
+ * without any).  eps is at least 2^-126.
+ */
+typedef struct dualgcn_norm {
+    const float *post_weight, *post_bias;   /* the norm after the block (DUALGCN_NORM_POST) */
+    const float *pre_weight, *pre_bias;     /* the norm before the next block */
+    const void *gate;
+    float eps;
+    float scale;                            /* of the block in the residual stream */
+    uint32_t flags;
+} dualgcn_norm;
+
+/*
+ * dualgcn_norm_residual -- what stands between two blocks of a deep GCN (Sec. 2.1: layers are
+ * stacked; a block is a layer's update and aggregation), in one pass:
+ *   Rn = R + scale * gate * post(B)      the block's output B enters the residual stream
+ *   Z  = pre(Rn)                         the input of the next block's update
+ * where post is the identity without DUALGCN_NORM_POST, and a norm of a row x is
+ *   weight * (x - m) / sqrt(mean((x - m)^2) + eps) + bias,  m = mean(x) for layer norms, else 0.
+ *
+ * R, Rn: n x F row-major, float32, or bfloat16 with DUALGCN_STREAM_BF16; B: n x F, float32, or
+ * bfloat16 with DUALGCN_IN_BF16; Z: n x F, float32, or bfloat16 with DUALGCN_OUT_BF16 (what
+ * dualgcn_update reads with DUALGCN_IN_BF16).  The second norm takes Rn as it is stored.
+ *   B NULL   the norm before the first block: Z = pre(R); Rn must be NULL and no flag of the
+ *            post norm or a gate set.
+ *   Z NULL   the last block, or a block whose next one takes the stream as it is.
+ * Rn may be R (the stream is updated in place); no other output may overlap an operand or
+ * another output (DUALGCN_ERR_INVALID_ARG).  float32 arithmetic; every output element is written
+ * by one thread, and the order of every sum is fixed.  n >= 1, 1 <= F <= 8192 (larger F:
+ * DUALGCN_ERR_UNSUPPORTED); rows may start at any element.  No workspace.  Asynchronous.
+ */
+int dualgcn_norm_residual(const dualgcn_norm *norm, const void *R, const void *B, void *Rn, void *Z,
+                          int32_t n, int32_t F, void *stream);
+
+/* Where the parameters' gradients go; NULL = not wanted.  float32[F], and gate in the gate's
+ * shape: float32[F], float32[n], or n x F in the gradients' type (DUALGCN_GRAD_BF16). */
+typedef struct dualgcn_norm_grads {
+    float *post_weight, *post_bias, *pre_weight, *pre_bias;
+    void *gate;
+} dualgcn_norm_grads;
+
+/* Bytes of the workspace dualgcn_norm_residual_backward needs (host only). */
+int dualgcn_norm_residual_backward_workspace(int32_t n, int32_t F, size_t *bytes);
+
+/*
+ * dualgcn_norm_residual_backward -- the gradients of dualgcn_norm_residual.
+ *
+ * norm as in the forward call; Rn the stream it left (for B NULL: its R), B its block output.
+ *   dZ    gradient of Z, n x F, float32 or (DUALGCN_GRAD_BF16) bfloat16; NULL when Z was not
+ *         made or has no gradient (Rn is then not read and may be NULL)
+ *   dRn   gradient of Rn from elsewhere, in the stream's type; NULL = zeros.  Not both NULL.
+ *   dR    gradient of R, in the stream's type; may be dRn (in place); NULL = not wanted
+ *   dB    gradient of B, float32 or (DUALGCN_GRAD_BF16) bfloat16; NULL = not wanted
+ *   grads the parameters' gradients; NULL = none.  post_* needs DUALGCN_NORM_POST, pre_* needs
+ *         dZ, gate a gate.
+ * The rows' statistics are computed again from Rn and B.  Sums over the rows are formed in
+ * float32 by each workgroup and joined in float64 in a fixed order (in `workspace`, device,
+ * 256-byte aligned, at least dualgcn_norm_residual_backward_workspace bytes), so results do not
+ * depend on timing.  Outputs overlap nothing but as said for dR.  Limits as for
+ * dualgcn_norm_residual.  DUALGCN_OUT_BF16 has no meaning here and is ignored.  Asynchronous.
+ */
+int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, const void *B, const void *dZ,
+                                   const void *dRn, void *dR, void *dB, const dualgcn_norm_grads *grads,
+                                   int32_t n, int32_t F, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+
 /* ------------------------------------------------------------------ measurement */
 
 enum { DUALGCN_PROBE_COPY = 0, DUALGCN_PROBE_READ = 1 };

@@ -10,6 +10,7 @@ is missing, importing this package raises ImportError: there is no fallback.
     T = update(X, W)                            # T = X W, bf16 matrix cores
     H = gcn_layer(plan, X, W, relu=True)        # H = relu(A (X W)), X W in bf16 MFMA
 """
+import collections
 import ctypes
 import os
 
@@ -22,6 +23,8 @@ OK, ERR_INVALID_ARG, ERR_BAD_CSR, ERR_UNSUPPORTED, ERR_OOM, ERR_HIP, ERR_NO_DEVI
     0, -1, -2, -3, -4, -5, -6
 FORCE_AUTO, FORCE_SPARSE, FORCE_DENSE = 0, 1, 2
 RELU, OUT_BF16, IN_BF16, GRAD_BF16 = 1, 2, 4, 8
+STREAM_BF16, NORM_LAYER, NORM_POST = 16, 32, 64
+GATE_FEATURE, GATE_NODE, GATE_FULL, GATE_SIGMOID = 128, 256, 512, 1024
 LOSS_SLOTS = 1025                # float64 entries of the loss buffer of softmax_xent
 ALPHA_ADAPTIVE = 0xFFFFFFFF      # alpha = (ALPHA_ADAPTIVE, q): adaptive weight in steps of 1/q
 ALPHA_BALANCED = 0xFFFFFFFE      # alpha = (ALPHA_BALANCED, q): weight balancing the spreads of N and D
@@ -63,6 +66,19 @@ class PlanInfo(ctypes.Structure):
                 ("cold_marked", ctypes.c_int32)]
 
 
+class Norm(ctypes.Structure):
+    _fields_ = [("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
+                ("flags", ctypes.c_uint32)]
+
+
+class NormGradPointers(ctypes.Structure):
+    _fields_ = [("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python paper_2609_01983_amd/build.py`")
@@ -95,6 +111,11 @@ def _load():
         "dualgcn_weight_grad_noalloc": ([P, P, P, I32, I32, I32, U32, ctypes.c_float, P, P],
                                         ctypes.c_int),
         "dualgcn_backward_data": ([P, P, P, P, I32, I32, I32, U32, P], ctypes.c_int),
+        "dualgcn_norm_residual": ([ctypes.POINTER(Norm), P, P, P, P, I32, I32, P], ctypes.c_int),
+        "dualgcn_norm_residual_backward_workspace": ([I32, I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "dualgcn_norm_residual_backward": ([ctypes.POINTER(Norm), P, P, P, P, P, P,
+                                            ctypes.POINTER(NormGradPointers), I32, I32, P, SZ, P],
+                                           ctypes.c_int),
         "dualgcn_bandwidth_probe": ([I32, P, P, SZ, P], ctypes.c_int),
         "dualgcn_bandwidth_probe_out_floats": ([], I32),
     }
@@ -485,6 +506,169 @@ def backward_data(G, W, M=None, dX=None, stream=None):
     return dX
 
 
+# ------------------------------------------------------------------ deep GCNs
+
+def _on_device(stream, *tensors):
+    """The torch stream the call is queued on.  Every tensor is on the current device, and so
+    is the stream: the library launches on the current device."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
+    if stream is None:
+        return torch.cuda.current_stream()
+    if stream.device.index != device:
+        raise ValueError(f"stream on {stream.device}, the current device is cuda:{device}")
+    return stream
+
+
+def _empty(shape, dtype, like, stream):
+    """Device memory for work queued on `stream`: taken from that stream's pool, so that it is
+    neither still in use by an earlier owner nor handed on while the work runs."""
+    if stream == torch.cuda.current_stream():
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _shaped(t, dtype, shape, name):
+    _dev(t, dtype, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def _norm(R, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pre_weight, pre_bias, kind, eps):
+    """The checked parameters of a block's norms, as the library takes them."""
+    if kind not in ("rms", "layer"):
+        raise ValueError('kind must be "rms" or "layer"')
+    n, F = R.shape
+    flags = (NORM_LAYER if kind == "layer" else 0) | (NORM_POST if post_norm else 0)
+    flags |= STREAM_BF16 if R.dtype == torch.bfloat16 else 0
+    for t, name in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
+                    (pre_bias, "pre_bias")):
+        if t is not None:
+            _shaped(t, torch.float32, (F,), name)
+    if B is not None:
+        _float_or_bf16(B, "B")
+        _shaped(B, B.dtype, (n, F), "B")
+        flags |= IN_BF16 if B.dtype == torch.bfloat16 else 0
+    if gate is not None:
+        if B is None:
+            raise ValueError("a gate needs a block B")
+        if gate.dim() == 1:
+            _shaped(gate, torch.float32, (F,), "gate")
+            flags |= GATE_FEATURE
+        elif gate.dim() == 2 and gate.shape[1] == 1 and F != 1:
+            _shaped(gate, torch.float32, (n, 1), "gate")
+            flags |= GATE_NODE
+        else:
+            _shaped(gate, B.dtype, (n, F), "gate")
+            flags |= GATE_FULL
+    if gate_sigmoid:
+        flags |= GATE_SIGMOID
+    return Norm(_ptr(post_weight), _ptr(post_bias), _ptr(pre_weight), _ptr(pre_bias), _ptr(gate), float(eps),
+                float(scale), flags)
+
+
+def norm_residual(R, B=None, *, post_norm=True, post_weight=None, post_bias=None, gate=None,
+                  gate_sigmoid=False, scale=1.0, pre_norm=True, pre_weight=None, pre_bias=None,
+                  kind="rms", eps=1e-5, norm_bf16=False, Rn=None, Z=None, stream=None):
+    """What stands between two residual blocks: Rn = R + scale * gate * post(B), Z = pre(Rn).
+
+    R: [n, F] float32 or bfloat16 (the residual stream); B: [n, F] float32 or bfloat16 (the
+    block's output), or None before the first block (Rn is then R itself, and Z = pre(R)).
+    post and pre are RMS norms (kind "rms") or layer norms ("layer") with float32 [F] weights and
+    biases (None: ones and zeros); post_norm=False leaves the block as it is, pre_norm=False
+    makes no Z.  gate: None, float32 [F] (one for each feature), float32 [n, 1] (one for each
+    node), or [n, F] in B's type; with gate_sigmoid it holds logits.  Z is float32, or bfloat16
+    with norm_bf16 (what `update` takes).  Rn may be R (in place).  Returns (Rn, Z)."""
+    _float_or_bf16(R, "R")
+    n, F = R.shape
+    if B is None:
+        if not pre_norm:
+            raise ValueError("nothing to do: no block and no norm")
+        if Rn is not None and Rn is not R:
+            raise ValueError("Rn is R where there is no block")
+        post_norm = False
+    p = _norm(R, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pre_weight, pre_bias, kind, eps)
+    s = _on_device(stream, R, B, post_weight, post_bias, gate, pre_weight, pre_bias, Rn, Z)
+    if B is not None:
+        Rn = _shaped(_empty((n, F), R.dtype, R, s) if Rn is None else Rn, R.dtype, (n, F), "Rn")
+    if pre_norm:
+        zdt = torch.bfloat16 if norm_bf16 else torch.float32
+        Z = _shaped(_empty((n, F), zdt, R, s) if Z is None else Z, zdt, (n, F), "Z")
+        p.flags |= OUT_BF16 if norm_bf16 else 0
+    elif Z is not None:
+        raise ValueError("Z without pre_norm")
+    _check(_lib.dualgcn_norm_residual(ctypes.byref(p), R.data_ptr(), _ptr(B), _ptr(Rn) if B is not None else None,
+                                      _ptr(Z), n, F, _stream(s)), "dualgcn_norm_residual")
+    return (Rn if B is not None else R), Z
+
+
+class NormGrads(collections.namedtuple("NormGrads", "R B gate post_weight post_bias pre_weight pre_bias")):
+    """Gradients of norm_residual's operands; None where there is no such operand."""
+    __slots__ = ()
+
+
+def norm_residual_backward_workspace_bytes(n, F):
+    nbytes = ctypes.c_size_t()
+    _check(_lib.dualgcn_norm_residual_backward_workspace(n, F, ctypes.byref(nbytes)),
+           "dualgcn_norm_residual_backward_workspace")
+    return nbytes.value
+
+
+def norm_residual_backward(Rn, B=None, dZ=None, dRn=None, *, post_norm=True, post_weight=None, post_bias=None,
+                           gate=None, gate_sigmoid=False, scale=1.0, pre_norm=True, pre_weight=None,
+                           pre_bias=None, kind="rms", eps=1e-5, grad_bf16=False, dR=None, dB=None,
+                           workspace=None, stream=None):
+    """Gradients of norm_residual: Rn is the stream it returned, B and the parameters are its own.
+
+    dZ: gradient of Z (None: none), float32, or bfloat16 with grad_bf16; dRn: gradient of Rn from
+    elsewhere, in Rn's type (None: zeros); not both None.  Returns NormGrads: R in Rn's type (dR
+    may be dRn), B and a full gate in dZ's type, the vectors in float32 ([F], or [n, 1] for a
+    gate per node).  A weight or bias that is None has no gradient."""
+    _float_or_bf16(Rn, "Rn")
+    n, F = Rn.shape
+    if B is None:
+        post_norm = False
+    if not pre_norm and dZ is not None:
+        raise ValueError("dZ without pre_norm")
+    p = _norm(Rn, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pre_weight, pre_bias, kind, eps)
+    gdt = torch.bfloat16 if grad_bf16 else torch.float32
+    p.flags |= GRAD_BF16 if grad_bf16 else 0
+    s = _on_device(stream, Rn, B, dZ, dRn, post_weight, post_bias, gate, pre_weight, pre_bias, dR, dB, workspace)
+    if dZ is not None:
+        _shaped(dZ, gdt, (n, F), "dZ")
+    if dRn is not None:
+        _shaped(dRn, Rn.dtype, (n, F), "dRn")
+    dR = _shaped(_empty((n, F), Rn.dtype, Rn, s) if dR is None else dR, Rn.dtype, (n, F), "dR")
+    if B is not None:
+        dB = _shaped(_empty((n, F), gdt, Rn, s) if dB is None else dB, gdt, (n, F), "dB")
+    elif dB is not None:
+        raise ValueError("dB without B")
+    vec = lambda t: None if t is None else _empty((F,), torch.float32, Rn, s)  # noqa: E731
+    dgate = None
+    if gate is not None:
+        dgate = _empty(tuple(gate.shape), gdt if p.flags & GATE_FULL else torch.float32, Rn, s)
+    out = NormGrads(dR, dB, dgate, vec(post_weight), vec(post_bias), vec(pre_weight) if dZ is not None else None,
+                    vec(pre_bias) if dZ is not None else None)
+    if workspace is None:
+        workspace = _empty((norm_residual_backward_workspace_bytes(n, F),), torch.uint8, Rn, s)
+    _dev(workspace, torch.uint8, "workspace")
+    g = NormGradPointers(_ptr(out.post_weight), _ptr(out.post_bias), _ptr(out.pre_weight), _ptr(out.pre_bias),
+                         _ptr(out.gate))
+    _check(_lib.dualgcn_norm_residual_backward(ctypes.byref(p), Rn.data_ptr(), _ptr(B), _ptr(dZ), _ptr(dRn),
+                                               dR.data_ptr(), _ptr(dB), ctypes.byref(g), n, F,
+                                               workspace.data_ptr(), workspace.numel(), _stream(s)),
+           "dualgcn_norm_residual_backward")
+    return out
+
+
 PROBE_COPY, PROBE_READ = 0, 1
 
 
@@ -520,4 +704,6 @@ __all__ = ["Plan", "spmm", "spmm_update", "update", "gcn_layer", "gcn_layer_work
            "ALPHA_ADAPTIVE", "ALPHA_BALANCED", "GRAD_BF16", "LOSS_SLOTS", "softmax_xent", "weight_grad", "weight_grad_noalloc",
            "weight_grad_workspace_bytes", "backward_data", "aggregator_values", "AGG_GCN",
            "AGG_MEAN", "AGG_SUM", "bandwidth_probe", "bandwidth_probe_out_floats",
-           "PROBE_COPY", "PROBE_READ"]
+           "PROBE_COPY", "PROBE_READ", "norm_residual", "norm_residual_backward", "NormGrads",
+           "norm_residual_backward_workspace_bytes", "Norm", "NormGradPointers", "STREAM_BF16", "NORM_LAYER",
+           "NORM_POST", "GATE_FEATURE", "GATE_NODE", "GATE_FULL", "GATE_SIGMOID"]

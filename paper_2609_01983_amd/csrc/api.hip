@@ -250,6 +250,62 @@ int check_update(const void *X, const float *W, const void *T, int32_t F_in, int
     return DUALGCN_OK;
 }
 
+// A range of device memory; `same` is the one operand that an output may be in place of.
+struct Span {
+    const void *p;
+    size_t bytes;
+    const void *same = nullptr;
+};
+
+// No output shares a byte with an operand (but for the one it may replace whole) or with
+// another output.  NULL ranges share nothing.
+template <size_t I, size_t O>
+bool apart(const Span (&in)[I], const Span (&out)[O]) {
+    for (size_t o = 0; o < O; ++o) {
+        if (!out[o].p) continue;
+        for (size_t i = 0; i < I; ++i)
+            if (in[i].p && !(out[o].same && in[i].p == out[o].same && out[o].p == out[o].same) &&
+                overlaps(out[o].p, out[o].bytes, in[i].p, in[i].bytes))
+                return false;
+        for (size_t k = 0; k < o; ++k)
+            if (out[k].p && overlaps(out[o].p, out[o].bytes, out[k].p, out[k].bytes)) return false;
+    }
+    return true;
+}
+
+size_t vector_bytes(int32_t F) { return sizeof(float) * static_cast<size_t>(F); }
+
+bool norm_aligned(const void *p, bool bf16) { return reinterpret_cast<uintptr_t>(p) % (bf16 ? 2 : 4) == 0; }
+
+size_t gate_bytes(const dualgcn_norm &p, int32_t n, int32_t F) {
+    if (p.flags & DUALGCN_GATE_FEATURE) return vector_bytes(F);
+    if (p.flags & DUALGCN_GATE_NODE) return sizeof(float) * static_cast<size_t>(n);
+    if (p.flags & DUALGCN_GATE_FULL) return static_cast<size_t>(n) * F * (p.flags & DUALGCN_IN_BF16 ? 2 : 4);
+    return 0;
+}
+
+// Parameters of the norms around a block; `more` are the flags a call takes beside its own.
+int check_norm(const dualgcn_norm *p, const void *B, int32_t n, int32_t F, uint32_t more) {
+    if (!p || n < 1 || F < 1) return DUALGCN_ERR_INVALID_ARG;
+    constexpr uint32_t kGates = DUALGCN_GATE_FEATURE | DUALGCN_GATE_NODE | DUALGCN_GATE_FULL;
+    const uint32_t known = DUALGCN_IN_BF16 | DUALGCN_STREAM_BF16 | DUALGCN_NORM_LAYER | DUALGCN_NORM_POST | kGates |
+                           DUALGCN_GATE_SIGMOID;
+    if (p->flags & ~(known | more)) return DUALGCN_ERR_INVALID_ARG;
+    const uint32_t gate = p->flags & kGates;
+    if (gate & (gate - 1)) return DUALGCN_ERR_INVALID_ARG;                       // two kinds
+    if (!gate != !p->gate || (!gate && (p->flags & DUALGCN_GATE_SIGMOID))) return DUALGCN_ERR_INVALID_ARG;
+    if (!B && (gate || (p->flags & DUALGCN_NORM_POST))) return DUALGCN_ERR_INVALID_ARG;
+    if (!(p->flags & DUALGCN_NORM_POST) && (p->post_weight || p->post_bias)) return DUALGCN_ERR_INVALID_ARG;
+    if (!norm_aligned(p->post_weight, false) || !norm_aligned(p->post_bias, false) ||
+        !norm_aligned(p->pre_weight, false) || !norm_aligned(p->pre_bias, false) ||
+        !norm_aligned(p->gate, (p->flags & DUALGCN_GATE_FULL) && (p->flags & DUALGCN_IN_BF16)))
+        return DUALGCN_ERR_INVALID_ARG;
+    // eps is a normal number (the reciprocal root is the hardware's), and neither is a NaN
+    if (!(p->eps >= 0x1p-126f) || !(p->eps < 0x1p127f) || !(p->scale == p->scale)) return DUALGCN_ERR_INVALID_ARG;
+    if (F > dgc::kMaxNormWidth) return DUALGCN_ERR_UNSUPPORTED;
+    return DUALGCN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -503,6 +559,68 @@ int dualgcn_backward_data(const void *G, const float *W, const void *M, float *d
         return DUALGCN_ERR_INVALID_ARG;
     if ((st = dgc::device_status())) return st;
     return dgc::launch_backward_data(G, gbf, W, M, mbf, dX, n, F_in, F_out,
+                                     static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_norm_residual(const dualgcn_norm *norm, const void *R, const void *B, void *Rn, void *Z,
+                          int32_t n, int32_t F, void *stream) {
+    dgc::TraceRange trace("dualgcn_norm_residual");
+    int st = check_norm(norm, B, n, F, DUALGCN_OUT_BF16);
+    if (st) return st;
+    if (!R || (!B && (Rn || !Z)) || (B && !Rn)) return DUALGCN_ERR_INVALID_ARG;
+    if (!norm_aligned(R, norm->flags & DUALGCN_STREAM_BF16) || !norm_aligned(B, norm->flags & DUALGCN_IN_BF16) ||
+        !norm_aligned(Rn, norm->flags & DUALGCN_STREAM_BF16) || !norm_aligned(Z, norm->flags & DUALGCN_OUT_BF16))
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t elems = static_cast<size_t>(n) * F;
+    const size_t rb = elems * (norm->flags & DUALGCN_STREAM_BF16 ? 2 : 4);
+    const Span in[] = {{R, rb}, {B, elems * (norm->flags & DUALGCN_IN_BF16 ? 2 : 4)}, {norm->gate, gate_bytes(*norm, n, F)},
+                       {norm->post_weight, vector_bytes(F)}, {norm->post_bias, vector_bytes(F)},
+                       {norm->pre_weight, vector_bytes(F)}, {norm->pre_bias, vector_bytes(F)}};
+    const Span out[] = {{Rn, rb, R}, {Z, elems * (norm->flags & DUALGCN_OUT_BF16 ? 2 : 4)}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    if ((st = dgc::device_status())) return st;
+    return dgc::launch_norm_residual(*norm, R, B, Rn, Z, n, F, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_norm_residual_backward_workspace(int32_t n, int32_t F, size_t *bytes) {
+    if (!bytes || n < 1 || F < 1) return DUALGCN_ERR_INVALID_ARG;
+    if (F > dgc::kMaxNormWidth) return DUALGCN_ERR_UNSUPPORTED;
+    *bytes = dgc::norm_backward_workspace_bytes(n, F);
+    return DUALGCN_OK;
+}
+
+int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, const void *B, const void *dZ,
+                                   const void *dRn, void *dR, void *dB, const dualgcn_norm_grads *grads,
+                                   int32_t n, int32_t F, void *workspace, size_t workspace_bytes,
+                                   void *stream) {
+    dgc::TraceRange trace("dualgcn_norm_residual_backward");
+    int st = check_norm(norm, B, n, F, DUALGCN_OUT_BF16 | DUALGCN_GRAD_BF16);
+    if (st) return st;
+    const dualgcn_norm_grads g = grads ? *grads : dualgcn_norm_grads{};
+    const uint32_t f = norm->flags;
+    const uint32_t gated = f & (DUALGCN_GATE_FEATURE | DUALGCN_GATE_NODE | DUALGCN_GATE_FULL);
+    if ((!dZ && !dRn) || (dZ && !Rn) || (!B && dB)) return DUALGCN_ERR_INVALID_ARG;
+    if ((!(f & DUALGCN_NORM_POST) && (g.post_weight || g.post_bias)) || (!dZ && (g.pre_weight || g.pre_bias)) ||
+        (!gated && g.gate))
+        return DUALGCN_ERR_INVALID_ARG;
+    const bool sbf = f & DUALGCN_STREAM_BF16, abf = f & DUALGCN_IN_BF16, gbf = f & DUALGCN_GRAD_BF16;
+    if (!norm_aligned(Rn, sbf) || !norm_aligned(B, abf) || !norm_aligned(dZ, gbf) || !norm_aligned(dRn, sbf) ||
+        !norm_aligned(dR, sbf) || !norm_aligned(dB, gbf) ||
+        !norm_aligned(g.gate, (f & DUALGCN_GATE_FULL) && gbf) || !norm_aligned(g.post_weight, false) ||
+        !norm_aligned(g.post_bias, false) || !norm_aligned(g.pre_weight, false) || !norm_aligned(g.pre_bias, false))
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t ws = dgc::norm_backward_workspace_bytes(n, F);
+    if (!workspace || workspace_bytes < ws || reinterpret_cast<uintptr_t>(workspace) % 256)
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t elems = static_cast<size_t>(n) * F, vb = vector_bytes(F);
+    const size_t rb = elems * (sbf ? 2 : 4), gb = elems * (gbf ? 2 : 4);
+    const Span in[] = {{Rn, rb}, {B, elems * (abf ? 2 : 4)}, {dZ, gb}, {dRn, rb}, {norm->gate, gate_bytes(*norm, n, F)},
+                       {norm->post_weight, vb}, {norm->post_bias, vb}, {norm->pre_weight, vb}, {norm->pre_bias, vb}};
+    const Span out[] = {{dR, rb, dRn}, {dB, gb}, {g.post_weight, vb}, {g.post_bias, vb}, {g.pre_weight, vb},
+                        {g.pre_bias, vb}, {g.gate, f & DUALGCN_GATE_FULL ? gb : gate_bytes(*norm, n, F)}, {workspace, ws}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    if ((st = dgc::device_status())) return st;
+    return dgc::launch_norm_backward(*norm, Rn, B, dZ, dRn, dR, dB, g, n, F, workspace,
                                      static_cast<hipStream_t>(stream));
 }
 

@@ -317,6 +317,16 @@ int launch_weight_grad_noalloc(const void *X, bool x_bf16, const void *G, bool g
                                int32_t n, int32_t F_in, int32_t F_out, float lr, float *W,
                                hipStream_t stream);
 
+// ---- norms around a block (norm.hip): arguments as dualgcn_norm_residual and its backward pass
+// take them, checked
+constexpr int kMaxNormWidth = 8192;
+int launch_norm_residual(const dualgcn_norm &p, const void *R, const void *B, void *Rn, void *Z, int32_t n,
+                         int32_t F, hipStream_t stream);
+size_t norm_backward_workspace_bytes(int32_t n, int32_t F);
+int launch_norm_backward(const dualgcn_norm &p, const void *Rn, const void *B, const void *dZ, const void *dRn,
+                         void *dR, void *dB, const dualgcn_norm_grads &g, int32_t n, int32_t F, void *workspace,
+                         hipStream_t stream);
+
 // ---- attainable bandwidth (probe.hip): kind DUALGCN_PROBE_COPY or DUALGCN_PROBE_READ; the
 // read probe writes one float per workgroup (probe_grid() <= kMaxProbeGrid) to dst.
 constexpr int kMaxProbeGrid = 16384;
