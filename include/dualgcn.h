@@ -451,7 +451,7 @@ int dualgcn_backward_data(const void *G, const float *W, const void *M, float *d
 /*
  * The norms of a residual block.  The vectors are float32[F] (device); a NULL weight is all
  * ones, a NULL bias all zeros.  gate goes by the flags (at most one of the three kinds; NULL
- * without any).  eps is at least 2^-126.
+ * without any).  eps is at least 2^-126 and scale finite.
  */
 typedef struct dualgcn_norm {
     const float *post_weight, *post_bias;   /* the norm after the block (DUALGCN_NORM_POST) */
@@ -515,6 +515,43 @@ int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, con
                                    const void *dRn, void *dR, void *dB, const dualgcn_norm_grads *grads,
                                    int32_t n, int32_t F, void *workspace, size_t workspace_bytes,
                                    void *stream);
+
+#define DUALGCN_TEACHER_BF16 2048u /* the teacher's logits are bfloat16 */
+
+/* Bytes of the workspace dualgcn_distill_xent needs (host only). */
+int dualgcn_distill_workspace(int32_t n, int32_t C, int32_t K, size_t *bytes);
+
+/*
+ * dualgcn_distill_xent -- the loss of a student against its teacher's top logits, with the
+ * labels' cross-entropy beside it, and the gradient (dualgcn_softmax_xent's companion for
+ * training a GCN from a larger one).
+ *
+ * Y (device, n x C row-major, float32, or bfloat16 with DUALGCN_IN_BF16) holds the student's
+ * logits.  Row v of ids (device, int32[n][K]) and teacher (device, [n][K], float32, or bfloat16
+ * with DUALGCN_TEACHER_BF16) are the classes and logits kept of its teacher, in any order.  An
+ * entry whose id is outside [0, C) or whose logit is -infinity is none; an id given twice counts
+ * twice.  With p = softmax(entries / temperature) over the row's entries,
+ * Q = softmax(Y_v / temperature) over all classes, and labels (device, int32[n], or NULL for
+ * none; a row whose label is outside [0, C) is unlabeled):
+ *   soft = soft_scale temperature^2 sum over rows with an entry of sum_k p_k (log p_k - log Q[id_k])
+ *   hard = hard_scale sum over labeled rows of -log softmax(Y_v)[label_v]
+ *   loss = {soft + hard, soft, hard}          (device, float32[3])
+ *   G    = d loss[0] / dY                     (device, n x C, float32, or bfloat16 with
+ *                                              DUALGCN_GRAD_BF16)
+ *        = soft_scale temperature (Q - P) on rows with an entry, P the p at their classes,
+ *        + hard_scale (softmax(Y_v) - e_label) on labeled rows, and 0 on the others.
+ * A student logit of -infinity is a class the row cannot take (its Q and gradient are 0; the loss
+ * is infinite if the teacher or the label takes it).  A row with a NaN, a +infinity or nothing
+ * above -infinity among the logits it needs gives NaN, in its own row of G and in the loss.
+ * float32 arithmetic, the loss joined in float64 in a fixed order; G does not depend on timing.
+ * n >= 1, 1 <= C < 2^20, 1 <= K <= 4096 (larger: DUALGCN_ERR_UNSUPPORTED), temperature in
+ * [2^-14, 2^14], finite scales; outputs overlap nothing.  `workspace` (device, 256-byte aligned)
+ * holds at least dualgcn_distill_workspace bytes.  Asynchronous.
+ */
+int dualgcn_distill_xent(const void *Y, const int32_t *ids, const void *teacher, const int32_t *labels,
+                         int32_t n, int32_t C, int32_t K, float temperature, float soft_scale,
+                         float hard_scale, uint32_t flags, void *G, float *loss, void *workspace,
+                         size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------ measurement */
 

@@ -25,6 +25,7 @@ FORCE_AUTO, FORCE_SPARSE, FORCE_DENSE = 0, 1, 2
 RELU, OUT_BF16, IN_BF16, GRAD_BF16 = 1, 2, 4, 8
 STREAM_BF16, NORM_LAYER, NORM_POST = 16, 32, 64
 GATE_FEATURE, GATE_NODE, GATE_FULL, GATE_SIGMOID = 128, 256, 512, 1024
+TEACHER_BF16 = 2048
 LOSS_SLOTS = 1025                # float64 entries of the loss buffer of softmax_xent
 ALPHA_ADAPTIVE = 0xFFFFFFFF      # alpha = (ALPHA_ADAPTIVE, q): adaptive weight in steps of 1/q
 ALPHA_BALANCED = 0xFFFFFFFE      # alpha = (ALPHA_BALANCED, q): weight balancing the spreads of N and D
@@ -116,6 +117,9 @@ def _load():
         "dualgcn_norm_residual_backward": ([ctypes.POINTER(Norm), P, P, P, P, P, P,
                                             ctypes.POINTER(NormGradPointers), I32, I32, P, SZ, P],
                                            ctypes.c_int),
+        "dualgcn_distill_workspace": ([I32, I32, I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "dualgcn_distill_xent": ([P, P, P, P, I32, I32, I32, ctypes.c_float, ctypes.c_float, ctypes.c_float,
+                                  U32, P, P, P, SZ, P], ctypes.c_int),
         "dualgcn_bandwidth_probe": ([I32, P, P, SZ, P], ctypes.c_int),
         "dualgcn_bandwidth_probe_out_floats": ([], I32),
     }
@@ -669,6 +673,55 @@ def norm_residual_backward(Rn, B=None, dZ=None, dRn=None, *, post_norm=True, pos
     return out
 
 
+def distill_workspace_bytes(n, C, K):
+    nbytes = ctypes.c_size_t()
+    _check(_lib.dualgcn_distill_workspace(n, C, K, ctypes.byref(nbytes)), "dualgcn_distill_workspace")
+    return nbytes.value
+
+
+def distill_xent(Y, ids, teacher, labels=None, temperature=1.0, soft_scale=None, hard_scale=None,
+                 grad_bf16=False, G=None, loss=None, workspace=None, stream=None):
+    """The loss of a student's logits Y against its teacher's top logits, and its gradient.
+
+    Y: [n, C] float32 or bfloat16; ids: int32 [n, K] classes kept of each row's teacher, teacher:
+    [n, K] float32 or bfloat16 their logits (an id outside [0, C) or a logit of -inf: no entry);
+    labels: int32 [n] or None.  Returns (G, loss): G = dloss[0]/dY ([n, C] float32, or bfloat16
+    with grad_bf16) and the float32 device tensor loss = [soft + hard, soft, hard], soft =
+    soft_scale T^2 sum KL(teacher || softmax(Y / T)), hard = hard_scale sum of the labels'
+    cross-entropy.  The scales default to 1 / (rows with an entry) and 1 / (labeled rows),
+    counted on the host only when not given."""
+    _float_or_bf16(Y, "Y")
+    n, C = Y.shape
+    _dev(ids, torch.int32, "ids")
+    if ids.dim() != 2 or ids.shape[0] != n:
+        raise ValueError("ids must be [n, K]")
+    K = ids.shape[1]
+    _float_or_bf16(teacher, "teacher")
+    _shaped(teacher, teacher.dtype, (n, K), "teacher")
+    if labels is not None:
+        _shaped(labels, torch.int32, (n,), "labels")
+    s = _on_device(stream, Y, ids, teacher, labels, G, loss, workspace)
+    if soft_scale is None:
+        kept = (ids >= 0) & (ids < C) & (teacher != float("-inf"))
+        soft_scale = 1.0 / max(1, int(kept.any(1).sum().item()))
+    if hard_scale is None:
+        hard_scale = 0.0 if labels is None else \
+            1.0 / max(1, int(((labels >= 0) & (labels < C)).sum().item()))
+    gdt = torch.bfloat16 if grad_bf16 else torch.float32
+    G = _shaped(_empty((n, C), gdt, Y, s) if G is None else G, gdt, (n, C), "G")
+    loss = _shaped(_empty((3,), torch.float32, Y, s) if loss is None else loss, torch.float32, (3,), "loss")
+    if workspace is None:
+        workspace = _empty((distill_workspace_bytes(n, C, K),), torch.uint8, Y, s)
+    _dev(workspace, torch.uint8, "workspace")
+    flags = (IN_BF16 if Y.dtype == torch.bfloat16 else 0) | (GRAD_BF16 if grad_bf16 else 0) | \
+        (TEACHER_BF16 if teacher.dtype == torch.bfloat16 else 0)
+    _check(_lib.dualgcn_distill_xent(Y.data_ptr(), ids.data_ptr(), teacher.data_ptr(), _ptr(labels), n, C, K,
+                                     float(temperature), float(soft_scale), float(hard_scale), flags,
+                                     G.data_ptr(), loss.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                     _stream(s)), "dualgcn_distill_xent")
+    return G, loss
+
+
 PROBE_COPY, PROBE_READ = 0, 1
 
 
@@ -706,4 +759,5 @@ __all__ = ["Plan", "spmm", "spmm_update", "update", "gcn_layer", "gcn_layer_work
            "AGG_MEAN", "AGG_SUM", "bandwidth_probe", "bandwidth_probe_out_floats",
            "PROBE_COPY", "PROBE_READ", "norm_residual", "norm_residual_backward", "NormGrads",
            "norm_residual_backward_workspace_bytes", "Norm", "NormGradPointers", "STREAM_BF16", "NORM_LAYER",
-           "NORM_POST", "GATE_FEATURE", "GATE_NODE", "GATE_FULL", "GATE_SIGMOID"]
+           "NORM_POST", "GATE_FEATURE", "GATE_NODE", "GATE_FULL", "GATE_SIGMOID",
+           "distill_xent", "distill_workspace_bytes", "TEACHER_BF16"]

@@ -273,9 +273,11 @@ bool apart(const Span (&in)[I], const Span (&out)[O]) {
     return true;
 }
 
+bool finite(float x) { return x - x == 0.f; }
+
 size_t vector_bytes(int32_t F) { return sizeof(float) * static_cast<size_t>(F); }
 
-bool norm_aligned(const void *p, bool bf16) { return reinterpret_cast<uintptr_t>(p) % (bf16 ? 2 : 4) == 0; }
+bool elem_aligned(const void *p, bool bf16) { return reinterpret_cast<uintptr_t>(p) % (bf16 ? 2 : 4) == 0; }
 
 size_t gate_bytes(const dualgcn_norm &p, int32_t n, int32_t F) {
     if (p.flags & DUALGCN_GATE_FEATURE) return vector_bytes(F);
@@ -296,12 +298,12 @@ int check_norm(const dualgcn_norm *p, const void *B, int32_t n, int32_t F, uint3
     if (!gate != !p->gate || (!gate && (p->flags & DUALGCN_GATE_SIGMOID))) return DUALGCN_ERR_INVALID_ARG;
     if (!B && (gate || (p->flags & DUALGCN_NORM_POST))) return DUALGCN_ERR_INVALID_ARG;
     if (!(p->flags & DUALGCN_NORM_POST) && (p->post_weight || p->post_bias)) return DUALGCN_ERR_INVALID_ARG;
-    if (!norm_aligned(p->post_weight, false) || !norm_aligned(p->post_bias, false) ||
-        !norm_aligned(p->pre_weight, false) || !norm_aligned(p->pre_bias, false) ||
-        !norm_aligned(p->gate, (p->flags & DUALGCN_GATE_FULL) && (p->flags & DUALGCN_IN_BF16)))
+    if (!elem_aligned(p->post_weight, false) || !elem_aligned(p->post_bias, false) ||
+        !elem_aligned(p->pre_weight, false) || !elem_aligned(p->pre_bias, false) ||
+        !elem_aligned(p->gate, (p->flags & DUALGCN_GATE_FULL) && (p->flags & DUALGCN_IN_BF16)))
         return DUALGCN_ERR_INVALID_ARG;
-    // eps is a normal number (the reciprocal root is the hardware's), and neither is a NaN
-    if (!(p->eps >= 0x1p-126f) || !(p->eps < 0x1p127f) || !(p->scale == p->scale)) return DUALGCN_ERR_INVALID_ARG;
+    // eps is a normal number: the reciprocal root is the hardware's
+    if (!(p->eps >= 0x1p-126f) || !(p->eps < 0x1p127f) || !finite(p->scale)) return DUALGCN_ERR_INVALID_ARG;
     if (F > dgc::kMaxNormWidth) return DUALGCN_ERR_UNSUPPORTED;
     return DUALGCN_OK;
 }
@@ -568,8 +570,8 @@ int dualgcn_norm_residual(const dualgcn_norm *norm, const void *R, const void *B
     int st = check_norm(norm, B, n, F, DUALGCN_OUT_BF16);
     if (st) return st;
     if (!R || (!B && (Rn || !Z)) || (B && !Rn)) return DUALGCN_ERR_INVALID_ARG;
-    if (!norm_aligned(R, norm->flags & DUALGCN_STREAM_BF16) || !norm_aligned(B, norm->flags & DUALGCN_IN_BF16) ||
-        !norm_aligned(Rn, norm->flags & DUALGCN_STREAM_BF16) || !norm_aligned(Z, norm->flags & DUALGCN_OUT_BF16))
+    if (!elem_aligned(R, norm->flags & DUALGCN_STREAM_BF16) || !elem_aligned(B, norm->flags & DUALGCN_IN_BF16) ||
+        !elem_aligned(Rn, norm->flags & DUALGCN_STREAM_BF16) || !elem_aligned(Z, norm->flags & DUALGCN_OUT_BF16))
         return DUALGCN_ERR_INVALID_ARG;
     const size_t elems = static_cast<size_t>(n) * F;
     const size_t rb = elems * (norm->flags & DUALGCN_STREAM_BF16 ? 2 : 4);
@@ -604,10 +606,10 @@ int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, con
         (!gated && g.gate))
         return DUALGCN_ERR_INVALID_ARG;
     const bool sbf = f & DUALGCN_STREAM_BF16, abf = f & DUALGCN_IN_BF16, gbf = f & DUALGCN_GRAD_BF16;
-    if (!norm_aligned(Rn, sbf) || !norm_aligned(B, abf) || !norm_aligned(dZ, gbf) || !norm_aligned(dRn, sbf) ||
-        !norm_aligned(dR, sbf) || !norm_aligned(dB, gbf) ||
-        !norm_aligned(g.gate, (f & DUALGCN_GATE_FULL) && gbf) || !norm_aligned(g.post_weight, false) ||
-        !norm_aligned(g.post_bias, false) || !norm_aligned(g.pre_weight, false) || !norm_aligned(g.pre_bias, false))
+    if (!elem_aligned(Rn, sbf) || !elem_aligned(B, abf) || !elem_aligned(dZ, gbf) || !elem_aligned(dRn, sbf) ||
+        !elem_aligned(dR, sbf) || !elem_aligned(dB, gbf) ||
+        !elem_aligned(g.gate, (f & DUALGCN_GATE_FULL) && gbf) || !elem_aligned(g.post_weight, false) ||
+        !elem_aligned(g.post_bias, false) || !elem_aligned(g.pre_weight, false) || !elem_aligned(g.pre_bias, false))
         return DUALGCN_ERR_INVALID_ARG;
     const size_t ws = dgc::norm_backward_workspace_bytes(n, F);
     if (!workspace || workspace_bytes < ws || reinterpret_cast<uintptr_t>(workspace) % 256)
@@ -622,6 +624,40 @@ int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, con
     if ((st = dgc::device_status())) return st;
     return dgc::launch_norm_backward(*norm, Rn, B, dZ, dRn, dR, dB, g, n, F, workspace,
                                      static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_distill_workspace(int32_t n, int32_t C, int32_t K, size_t *bytes) {
+    if (!bytes || n < 1 || C < 1 || K < 1) return DUALGCN_ERR_INVALID_ARG;
+    if (C >= (1 << 20) || K > 4096) return DUALGCN_ERR_UNSUPPORTED;
+    *bytes = dgc::distill_workspace_bytes(n, C);
+    return DUALGCN_OK;
+}
+
+int dualgcn_distill_xent(const void *Y, const int32_t *ids, const void *teacher, const int32_t *labels,
+                         int32_t n, int32_t C, int32_t K, float temperature, float soft_scale,
+                         float hard_scale, uint32_t flags, void *G, float *loss, void *workspace,
+                         size_t workspace_bytes, void *stream) {
+    dgc::TraceRange trace("dualgcn_distill_xent");
+    if (!Y || !ids || !teacher || !G || !loss || !workspace || n < 1 || C < 1 || K < 1) return DUALGCN_ERR_INVALID_ARG;
+    if (flags & ~(DUALGCN_IN_BF16 | DUALGCN_GRAD_BF16 | DUALGCN_TEACHER_BF16)) return DUALGCN_ERR_INVALID_ARG;
+    if (!(temperature >= 0x1p-14f && temperature <= 0x1p14f) || !finite(soft_scale) || !finite(hard_scale))
+        return DUALGCN_ERR_INVALID_ARG;
+    if (C >= (1 << 20) || K > 4096) return DUALGCN_ERR_UNSUPPORTED;
+    const bool ybf = flags & DUALGCN_IN_BF16, gbf = flags & DUALGCN_GRAD_BF16, tbf = flags & DUALGCN_TEACHER_BF16;
+    if (!elem_aligned(Y, ybf) || !elem_aligned(G, gbf) || !elem_aligned(teacher, tbf) || !elem_aligned(ids, false) ||
+        !elem_aligned(labels, false) || !elem_aligned(loss, false) || reinterpret_cast<uintptr_t>(workspace) % 256)
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t ws = dgc::distill_workspace_bytes(n, C);
+    if (workspace_bytes < ws) return DUALGCN_ERR_INVALID_ARG;
+    const size_t un = static_cast<size_t>(n), elems = un * C, entries = un * K;
+    const Span in[] = {{Y, elems * (ybf ? 2 : 4)}, {ids, entries * sizeof(int32_t)}, {teacher, entries * (tbf ? 2 : 4)},
+                       {labels, un * sizeof(int32_t)}};
+    const Span out[] = {{G, elems * (gbf ? 2 : 4)}, {loss, 3 * sizeof(float)}, {workspace, ws}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    return dgc::launch_distill(Y, ybf, ids, teacher, tbf, labels, n, C, K, temperature, soft_scale, hard_scale, G, gbf,
+                               loss, workspace, static_cast<hipStream_t>(stream));
 }
 
 int dualgcn_plan_query(const dualgcn_plan *plan, dualgcn_plan_info *out) {

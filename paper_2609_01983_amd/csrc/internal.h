@@ -327,6 +327,12 @@ int launch_norm_backward(const dualgcn_norm &p, const void *Rn, const void *B, c
                          void *dR, void *dB, const dualgcn_norm_grads &g, int32_t n, int32_t F, void *workspace,
                          hipStream_t stream);
 
+// ---- distillation (distill.hip): arguments as dualgcn_distill_xent takes them, checked
+size_t distill_workspace_bytes(int32_t n, int32_t C);
+int launch_distill(const void *Y, bool y_bf16, const int32_t *ids, const void *teacher, bool t_bf16,
+                   const int32_t *labels, int32_t n, int32_t C, int32_t K, float T, float soft, float hard, void *G,
+                   bool g_bf16, float *loss, void *workspace, hipStream_t stream);
+
 // ---- attainable bandwidth (probe.hip): kind DUALGCN_PROBE_COPY or DUALGCN_PROBE_READ; the
 // read probe writes one float per workgroup (probe_grid() <= kMaxProbeGrid) to dst.
 constexpr int kMaxProbeGrid = 16384;
