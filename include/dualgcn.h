@@ -553,6 +553,52 @@ int dualgcn_distill_xent(const void *Y, const int32_t *ids, const void *teacher,
                          float hard_scale, uint32_t flags, void *G, float *loss, void *workspace,
                          size_t workspace_bytes, void *stream);
 
+/* Elements that share a scale in the 8-bit operands. */
+#define DUALGCN_FP8_BLOCK 128
+
+/*
+ * The update phase from 8-bit operands: features kept, or activations quantised, in e4m3 (one
+ * byte: sign, 4 exponent bits of bias 7, 3 fraction bits; largest 448, NaN 0x7F, no infinity)
+ * with a float32 scale for each block of 128 elements; the value of an element is its e4m3
+ * number times its block's scale.
+ *
+ * dualgcn_quantize_fp8 -- X (device, n x F row-major, float32, or bfloat16 with DUALGCN_IN_BF16)
+ * into Q (device, n x F bytes) and scales (device, float32[n][ceil(F / 128)]), a scale for each
+ * 128 consecutive features of a row (the last block of a row may be shorter).  A scale is the
+ * least power of two, 2^-126 or more, that brings the block's largest finite magnitude to 448 or
+ * below (1 for a block without one), so that the division is exact; elements are rounded once, to nearest
+ * even.  Infinities and NaN become NaN.  n >= 1, F >= 1.  Asynchronous.
+ *
+ * dualgcn_quantize_weight_fp8 -- W (device, float32 F_in x F_out row-major) with a scale for each
+ * 128 x 128 block, in the layout dualgcn_update_fp8 reads: with `transpose` not 0, Q is
+ * F_out x F_in (for X W) and scales float32[ceil(F_out / 128)][ceil(F_in / 128)]; with 0, Q is
+ * F_in x F_out (for G W^T, the gradient's product) and scales [ceil(F_in / 128)][ceil(F_out / 128)].
+ * Both hold the same numbers.  1 <= F_in, F_out <= 65536 (larger: DUALGCN_ERR_UNSUPPORTED).
+ * Asynchronous.
+ */
+int dualgcn_quantize_fp8(const void *X, int32_t n, int32_t F, uint32_t flags, void *Q, float *scales,
+                         void *stream);
+int dualgcn_quantize_weight_fp8(const float *W, int32_t F_in, int32_t F_out, int32_t transpose, void *Q,
+                                float *scales, void *stream);
+
+/*
+ * dualgcn_update_fp8 -- T = X W from 8-bit operands on the matrix cores (dualgcn_update's
+ * companion for serving: a quarter of float32 features' bytes).
+ *
+ * X (device, e4m3 n x F_in row-major) with sx (float32[n][ceil(F_in / 128)]); W (device, e4m3
+ * F_out x F_in row-major: W transposed) with sw (float32[ceil(F_out / 128)][ceil(F_in / 128)], one
+ * for each 128 x 128 block); T (device, n x F_out row-major, float32, or bfloat16 with
+ * DUALGCN_OUT_BF16).  The scales may be any float32 numbers.  Products of a block (of the e4m3
+ * numbers widened to bfloat16, which is exact) are summed by the matrix cores in float32, multiplied by the two scales and added in float32, block after
+ * block, in an order that depends on the shape only.  The gradient G W^T is the same call on a
+ * quantised G and W not transposed.
+ * n >= 1; F_in a multiple of 16, at most 1024; 1 <= F_out <= 65536 (else
+ * DUALGCN_ERR_UNSUPPORTED); X and W 16-byte aligned; T overlaps no operand.  No workspace.
+ * Asynchronous.
+ */
+int dualgcn_update_fp8(const void *X, const float *sx, const void *W, const float *sw, void *T, int32_t n,
+                       int32_t F_in, int32_t F_out, uint32_t flags, void *stream);
+
 /* ------------------------------------------------------------------ measurement */
 
 enum { DUALGCN_PROBE_COPY = 0, DUALGCN_PROBE_READ = 1 };

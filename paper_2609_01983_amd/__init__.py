@@ -26,6 +26,7 @@ RELU, OUT_BF16, IN_BF16, GRAD_BF16 = 1, 2, 4, 8
 STREAM_BF16, NORM_LAYER, NORM_POST = 16, 32, 64
 GATE_FEATURE, GATE_NODE, GATE_FULL, GATE_SIGMOID = 128, 256, 512, 1024
 TEACHER_BF16 = 2048
+FP8_BLOCK = 128                  # elements that share a scale in the 8-bit operands
 LOSS_SLOTS = 1025                # float64 entries of the loss buffer of softmax_xent
 ALPHA_ADAPTIVE = 0xFFFFFFFF      # alpha = (ALPHA_ADAPTIVE, q): adaptive weight in steps of 1/q
 ALPHA_BALANCED = 0xFFFFFFFE      # alpha = (ALPHA_BALANCED, q): weight balancing the spreads of N and D
@@ -120,6 +121,9 @@ def _load():
         "dualgcn_distill_workspace": ([I32, I32, I32, ctypes.POINTER(SZ)], ctypes.c_int),
         "dualgcn_distill_xent": ([P, P, P, P, I32, I32, I32, ctypes.c_float, ctypes.c_float, ctypes.c_float,
                                   U32, P, P, P, SZ, P], ctypes.c_int),
+        "dualgcn_quantize_fp8": ([P, I32, I32, U32, P, P, P], ctypes.c_int),
+        "dualgcn_quantize_weight_fp8": ([P, I32, I32, I32, P, P, P], ctypes.c_int),
+        "dualgcn_update_fp8": ([P, P, P, P, P, I32, I32, I32, U32, P], ctypes.c_int),
         "dualgcn_bandwidth_probe": ([I32, P, P, SZ, P], ctypes.c_int),
         "dualgcn_bandwidth_probe_out_floats": ([], I32),
     }
@@ -722,6 +726,62 @@ def distill_xent(Y, ids, teacher, labels=None, temperature=1.0, soft_scale=None,
     return G, loss
 
 
+def _fp8_blocks(F):
+    return (F + FP8_BLOCK - 1) // FP8_BLOCK
+
+
+def quantize_fp8(X, Q=None, scales=None, stream=None):
+    """(Q, scales): X ([n, F] float32 or bfloat16) as float8_e4m3fn [n, F] with a float32 scale, a
+    power of two, for each 128 consecutive features of a row ([n, ceil(F / 128)])."""
+    _float_or_bf16(X, "X")
+    n, F = X.shape
+    s = _on_device(stream, X, Q, scales)
+    Q = _shaped(_empty((n, F), torch.float8_e4m3fn, X, s) if Q is None else Q, torch.float8_e4m3fn, (n, F), "Q")
+    shape = (n, _fp8_blocks(F))
+    scales = _shaped(_empty(shape, torch.float32, X, s) if scales is None else scales, torch.float32, shape, "scales")
+    _check(_lib.dualgcn_quantize_fp8(X.data_ptr(), n, F, IN_BF16 if X.dtype == torch.bfloat16 else 0, Q.data_ptr(),
+                                     scales.data_ptr(), _stream(s)), "dualgcn_quantize_fp8")
+    return Q, scales
+
+
+def quantize_weight_fp8(W, transpose=True, Q=None, scales=None, stream=None):
+    """(Q, scales): W ([F_in, F_out] float32) as float8_e4m3fn with a float32 scale for each 128 x 128
+    block, as update_fp8 reads it: [F_out, F_in] for X W, or with transpose=False [F_in, F_out]
+    for the gradient's product G W^T."""
+    _dev(W, torch.float32, "W")
+    if W.dim() != 2:
+        raise ValueError("W must be [F_in, F_out]")
+    F_in, F_out = W.shape
+    s = _on_device(stream, W, Q, scales)
+    shape = (F_out, F_in) if transpose else (F_in, F_out)
+    Q = _shaped(_empty(shape, torch.float8_e4m3fn, W, s) if Q is None else Q, torch.float8_e4m3fn, shape, "Q")
+    shape = (_fp8_blocks(shape[0]), _fp8_blocks(shape[1]))
+    scales = _shaped(_empty(shape, torch.float32, W, s) if scales is None else scales, torch.float32, shape, "scales")
+    _check(_lib.dualgcn_quantize_weight_fp8(W.data_ptr(), F_in, F_out, 1 if transpose else 0, Q.data_ptr(),
+                                            scales.data_ptr(), _stream(s)), "dualgcn_quantize_weight_fp8")
+    return Q, scales
+
+
+def update_fp8(X, sx, W, sw, T=None, out_bf16=False, stream=None):
+    """T = X W from 8-bit operands on the matrix cores: X float8_e4m3fn [n, F_in] with its float32
+    scales sx [n, ceil(F_in / 128)], W float8_e4m3fn [F_out, F_in] (transposed) with sw
+    [ceil(F_out / 128), ceil(F_in / 128)].  T is float32 [n, F_out], or bfloat16 with out_bf16."""
+    _dev(X, torch.float8_e4m3fn, "X")
+    _dev(W, torch.float8_e4m3fn, "W")
+    if X.dim() != 2 or W.dim() != 2 or W.shape[1] != X.shape[1]:
+        raise ValueError("X must be [n, F_in] and W [F_out, F_in]")
+    n, F_in = X.shape
+    F_out = W.shape[0]
+    _shaped(sx, torch.float32, (n, _fp8_blocks(F_in)), "sx")
+    _shaped(sw, torch.float32, (_fp8_blocks(F_out), _fp8_blocks(F_in)), "sw")
+    s = _on_device(stream, X, sx, W, sw, T)
+    tdt = torch.bfloat16 if out_bf16 else torch.float32
+    T = _shaped(_empty((n, F_out), tdt, X, s) if T is None else T, tdt, (n, F_out), "T")
+    _check(_lib.dualgcn_update_fp8(X.data_ptr(), sx.data_ptr(), W.data_ptr(), sw.data_ptr(), T.data_ptr(), n, F_in,
+                                   F_out, OUT_BF16 if out_bf16 else 0, _stream(s)), "dualgcn_update_fp8")
+    return T
+
+
 PROBE_COPY, PROBE_READ = 0, 1
 
 
@@ -760,4 +820,5 @@ __all__ = ["Plan", "spmm", "spmm_update", "update", "gcn_layer", "gcn_layer_work
            "PROBE_COPY", "PROBE_READ", "norm_residual", "norm_residual_backward", "NormGrads",
            "norm_residual_backward_workspace_bytes", "Norm", "NormGradPointers", "STREAM_BF16", "NORM_LAYER",
            "NORM_POST", "GATE_FEATURE", "GATE_NODE", "GATE_FULL", "GATE_SIGMOID",
-           "distill_xent", "distill_workspace_bytes", "TEACHER_BF16"]
+           "distill_xent", "distill_workspace_bytes", "TEACHER_BF16",
+           "quantize_fp8", "quantize_weight_fp8", "update_fp8", "FP8_BLOCK"]

@@ -273,6 +273,8 @@ bool apart(const Span (&in)[I], const Span (&out)[O]) {
     return true;
 }
 
+size_t fp8_blocks(int32_t F) { return (static_cast<size_t>(F) + DUALGCN_FP8_BLOCK - 1) / DUALGCN_FP8_BLOCK; }
+
 bool finite(float x) { return x - x == 0.f; }
 
 size_t vector_bytes(int32_t F) { return sizeof(float) * static_cast<size_t>(F); }
@@ -658,6 +660,56 @@ int dualgcn_distill_xent(const void *Y, const int32_t *ids, const void *teacher,
     if (st) return st;
     return dgc::launch_distill(Y, ybf, ids, teacher, tbf, labels, n, C, K, temperature, soft_scale, hard_scale, G, gbf,
                                loss, workspace, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_quantize_fp8(const void *X, int32_t n, int32_t F, uint32_t flags, void *Q, float *scales,
+                         void *stream) {
+    dgc::TraceRange trace("dualgcn_quantize_fp8");
+    if (!X || !Q || !scales || n < 1 || F < 1 || (flags & ~DUALGCN_IN_BF16)) return DUALGCN_ERR_INVALID_ARG;
+    const bool bf = flags & DUALGCN_IN_BF16;
+    if (!elem_aligned(X, bf) || !elem_aligned(scales, false)) return DUALGCN_ERR_INVALID_ARG;
+    const size_t un = static_cast<size_t>(n), elems = un * F;
+    const Span in[] = {{X, elems * (bf ? 2 : 4)}};
+    const Span out[] = {{Q, elems}, {scales, un * fp8_blocks(F) * sizeof(float)}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    return dgc::launch_quantize(X, bf, n, F, Q, scales, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_quantize_weight_fp8(const float *W, int32_t F_in, int32_t F_out, int32_t transpose, void *Q,
+                                float *scales, void *stream) {
+    dgc::TraceRange trace("dualgcn_quantize_weight_fp8");
+    if (!W || !Q || !scales || F_in < 1 || F_out < 1) return DUALGCN_ERR_INVALID_ARG;
+    if (F_in > (1 << 16) || F_out > (1 << 16)) return DUALGCN_ERR_UNSUPPORTED;
+    if (!elem_aligned(W, false) || !elem_aligned(scales, false)) return DUALGCN_ERR_INVALID_ARG;
+    const size_t elems = static_cast<size_t>(F_in) * F_out;
+    const Span in[] = {{W, elems * sizeof(float)}};
+    const Span out[] = {{Q, elems}, {scales, fp8_blocks(F_in) * fp8_blocks(F_out) * sizeof(float)}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    return dgc::launch_quantize_weight(W, F_in, F_out, transpose != 0, Q, scales, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_update_fp8(const void *X, const float *sx, const void *W, const float *sw, void *T, int32_t n,
+                       int32_t F_in, int32_t F_out, uint32_t flags, void *stream) {
+    dgc::TraceRange trace("dualgcn_update_fp8");
+    if (!X || !sx || !W || !sw || !T || n < 1 || F_in < 1 || F_out < 1 || (flags & ~DUALGCN_OUT_BF16))
+        return DUALGCN_ERR_INVALID_ARG;
+    if (F_in % 16 || F_in > 1024 || F_out > (1 << 16)) return DUALGCN_ERR_UNSUPPORTED;
+    const bool bf = flags & DUALGCN_OUT_BF16;
+    if (reinterpret_cast<uintptr_t>(X) % 16 || reinterpret_cast<uintptr_t>(W) % 16 || !elem_aligned(sx, false) ||
+        !elem_aligned(sw, false) || !elem_aligned(T, bf))
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t un = static_cast<size_t>(n), kb = fp8_blocks(F_in);
+    const Span in[] = {{X, un * F_in}, {sx, un * kb * sizeof(float)}, {W, static_cast<size_t>(F_in) * F_out},
+                       {sw, fp8_blocks(F_out) * kb * sizeof(float)}};
+    const Span out[] = {{T, un * F_out * (bf ? 2 : 4)}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    return dgc::launch_update_fp8(X, sx, W, sw, T, bf, n, F_in, F_out, static_cast<hipStream_t>(stream));
 }
 
 int dualgcn_plan_query(const dualgcn_plan *plan, dualgcn_plan_info *out) {

@@ -333,6 +333,14 @@ int launch_distill(const void *Y, bool y_bf16, const int32_t *ids, const void *t
                    const int32_t *labels, int32_t n, int32_t C, int32_t K, float T, float soft, float hard, void *G,
                    bool g_bf16, float *loss, void *workspace, hipStream_t stream);
 
+// ---- the update phase in 8 bits (fp8.hip): arguments as the entry points take them, checked
+constexpr int kFp8Block = DUALGCN_FP8_BLOCK;
+int launch_quantize(const void *X, bool bf16, int32_t n, int32_t F, void *Q, float *scales, hipStream_t stream);
+int launch_quantize_weight(const float *W, int32_t rows, int32_t cols, bool transpose, void *Q, float *scales,
+                           hipStream_t stream);
+int launch_update_fp8(const void *X, const float *sx, const void *W, const float *sw, void *T, bool out_bf16,
+                      int32_t n, int32_t F_in, int32_t F_out, hipStream_t stream);
+
 // ---- attainable bandwidth (probe.hip): kind DUALGCN_PROBE_COPY or DUALGCN_PROBE_READ; the
 // read probe writes one float per workgroup (probe_grid() <= kMaxProbeGrid) to dst.
 constexpr int kMaxProbeGrid = 16384;

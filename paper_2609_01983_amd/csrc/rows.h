@@ -72,6 +72,30 @@ struct RawRowQuad {
     }
 };
 
+// Elements [at, at + count) of an array as float32, zeros from `count` on (count <= 0: nothing is
+// read); for places with no row of at least four elements around them.
+template <bool BF>
+__device__ __forceinline__ row_f32x4 load_quad(const void *base, int64_t at, int count) {
+    row_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (count >= 4) {
+        if constexpr (BF) {
+            const row_u16x4 u = *reinterpret_cast<const row_u16x4_any *>(static_cast<const unsigned short *>(base) + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = bf16_to_float(u[i]);
+        } else {
+            v = *reinterpret_cast<const row_f32x4_any *>(static_cast<const float *>(base) + at);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < count) {
+                if constexpr (BF) v[i] = bf16_to_float(static_cast<const unsigned short *>(base)[at + i]);
+                else v[i] = static_cast<const float *>(base)[at + i];
+            }
+    }
+    return v;
+}
+
 // The first `count` of four values to [at, at + count), bfloat16 rounded to nearest even.
 template <bool BF>
 __device__ __forceinline__ void store_quad(void *base, int64_t at, int count, row_f32x4 v) {
