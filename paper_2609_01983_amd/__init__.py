@@ -516,27 +516,33 @@ def backward_data(G, W, M=None, dX=None, stream=None):
 
 # ------------------------------------------------------------------ deep GCNs
 
-def _on_device(stream, *tensors):
-    """The torch stream the call is queued on.  Every tensor is on the current device, and so
-    is the stream: the library launches on the current device."""
+# A call's host time counts where the work is small, so its checks take the plain attribute tests
+# first (several microseconds less than building stream and device objects).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _queue(stream, *tensors):
+    """The HIP stream a call goes to.  Every tensor, and the stream, is on the current device: the
+    library launches there."""
     device = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != device:
+        if t is not None and t.get_device() != device:
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
     if stream is None:
-        return torch.cuda.current_stream()
+        return _raw_stream(device)
     if stream.device.index != device:
         raise ValueError(f"stream on {stream.device}, the current device is cuda:{device}")
-    return stream
+    return stream.cuda_stream
 
 
 def _empty(shape, dtype, like, stream):
     """Device memory for work queued on `stream`: taken from that stream's pool, so that it is
     neither still in use by an earlier owner nor handed on while the work runs."""
-    if stream == torch.cuda.current_stream():
-        return torch.empty(shape, dtype=dtype, device=like.device)
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _ptr(t):
@@ -544,32 +550,49 @@ def _ptr(t):
 
 
 def _shaped(t, dtype, shape, name):
-    _dev(t, dtype, name)
-    if tuple(t.shape) != tuple(shape):
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous()):
+        _dev(t, dtype, name)
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     return t
 
 
+def _rows(t, name):
+    """A float32 or bfloat16 matrix: is it bfloat16?"""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.is_contiguous() and
+            (t.dtype is torch.float32 or t.dtype is torch.bfloat16)):
+        _float_or_bf16(t, name)
+    return t.dtype is torch.bfloat16
+
+
 def _norm(R, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pre_weight, pre_bias, kind, eps):
     """The checked parameters of a block's norms, as the library takes them."""
-    if kind not in ("rms", "layer"):
+    if kind != "rms" and kind != "layer":
         raise ValueError('kind must be "rms" or "layer"')
     n, F = R.shape
-    flags = (NORM_LAYER if kind == "layer" else 0) | (NORM_POST if post_norm else 0)
-    flags |= STREAM_BF16 if R.dtype == torch.bfloat16 else 0
-    for t, name in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
-                    (pre_bias, "pre_bias")):
-        if t is not None:
-            _shaped(t, torch.float32, (F,), name)
+    flags = NORM_LAYER if kind == "layer" else 0
+    if post_norm:
+        flags |= NORM_POST
+    if _rows(R, "R"):
+        flags |= STREAM_BF16
+    width = (F,)
+    if post_weight is not None:
+        _shaped(post_weight, torch.float32, width, "post_weight")
+    if post_bias is not None:
+        _shaped(post_bias, torch.float32, width, "post_bias")
+    if pre_weight is not None:
+        _shaped(pre_weight, torch.float32, width, "pre_weight")
+    if pre_bias is not None:
+        _shaped(pre_bias, torch.float32, width, "pre_bias")
     if B is not None:
-        _float_or_bf16(B, "B")
+        if _rows(B, "B"):
+            flags |= IN_BF16
         _shaped(B, B.dtype, (n, F), "B")
-        flags |= IN_BF16 if B.dtype == torch.bfloat16 else 0
     if gate is not None:
         if B is None:
             raise ValueError("a gate needs a block B")
         if gate.dim() == 1:
-            _shaped(gate, torch.float32, (F,), "gate")
+            _shaped(gate, torch.float32, width, "gate")
             flags |= GATE_FEATURE
         elif gate.dim() == 2 and gate.shape[1] == 1 and F != 1:
             _shaped(gate, torch.float32, (n, 1), "gate")
@@ -579,8 +602,7 @@ def _norm(R, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pr
             flags |= GATE_FULL
     if gate_sigmoid:
         flags |= GATE_SIGMOID
-    return Norm(_ptr(post_weight), _ptr(post_bias), _ptr(pre_weight), _ptr(pre_bias), _ptr(gate), float(eps),
-                float(scale), flags)
+    return Norm(_ptr(post_weight), _ptr(post_bias), _ptr(pre_weight), _ptr(pre_bias), _ptr(gate), eps, scale, flags)
 
 
 def norm_residual(R, B=None, *, post_norm=True, post_weight=None, post_bias=None, gate=None,
@@ -595,8 +617,8 @@ def norm_residual(R, B=None, *, post_norm=True, post_weight=None, post_bias=None
     makes no Z.  gate: None, float32 [F] (one for each feature), float32 [n, 1] (one for each
     node), or [n, F] in B's type; with gate_sigmoid it holds logits.  Z is float32, or bfloat16
     with norm_bf16 (what `update` takes).  Rn may be R (in place).  Returns (Rn, Z)."""
-    _float_or_bf16(R, "R")
-    n, F = R.shape
+    _rows(R, "R")
+    n, F = shape = R.shape
     if B is None:
         if not pre_norm:
             raise ValueError("nothing to do: no block and no norm")
@@ -604,18 +626,19 @@ def norm_residual(R, B=None, *, post_norm=True, post_weight=None, post_bias=None
             raise ValueError("Rn is R where there is no block")
         post_norm = False
     p = _norm(R, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pre_weight, pre_bias, kind, eps)
-    s = _on_device(stream, R, B, post_weight, post_bias, gate, pre_weight, pre_bias, Rn, Z)
+    s = _queue(stream, R, B, post_weight, post_bias, gate, pre_weight, pre_bias, Rn, Z)
     if B is not None:
-        Rn = _shaped(_empty((n, F), R.dtype, R, s) if Rn is None else Rn, R.dtype, (n, F), "Rn")
+        Rn = _empty(shape, R.dtype, R, stream) if Rn is None else _shaped(Rn, R.dtype, shape, "Rn")
     if pre_norm:
         zdt = torch.bfloat16 if norm_bf16 else torch.float32
-        Z = _shaped(_empty((n, F), zdt, R, s) if Z is None else Z, zdt, (n, F), "Z")
-        p.flags |= OUT_BF16 if norm_bf16 else 0
+        Z = _empty(shape, zdt, R, stream) if Z is None else _shaped(Z, zdt, shape, "Z")
+        if norm_bf16:
+            p.flags |= OUT_BF16
     elif Z is not None:
         raise ValueError("Z without pre_norm")
-    _check(_lib.dualgcn_norm_residual(ctypes.byref(p), R.data_ptr(), _ptr(B), _ptr(Rn) if B is not None else None,
-                                      _ptr(Z), n, F, _stream(s)), "dualgcn_norm_residual")
-    return (Rn if B is not None else R), Z
+    _check(_lib.dualgcn_norm_residual(p, R.data_ptr(), _ptr(B), None if B is None else Rn.data_ptr(), _ptr(Z), n, F, s),
+           "dualgcn_norm_residual")
+    return (R if B is None else Rn), Z
 
 
 class NormGrads(collections.namedtuple("NormGrads", "R B gate post_weight post_bias pre_weight pre_bias")):
@@ -640,39 +663,43 @@ def norm_residual_backward(Rn, B=None, dZ=None, dRn=None, *, post_norm=True, pos
     elsewhere, in Rn's type (None: zeros); not both None.  Returns NormGrads: R in Rn's type (dR
     may be dRn), B and a full gate in dZ's type, the vectors in float32 ([F], or [n, 1] for a
     gate per node).  A weight or bias that is None has no gradient."""
-    _float_or_bf16(Rn, "Rn")
-    n, F = Rn.shape
+    _rows(Rn, "Rn")
+    n, F = shape = Rn.shape
     if B is None:
         post_norm = False
+        if dB is not None:
+            raise ValueError("dB without B")
     if not pre_norm and dZ is not None:
         raise ValueError("dZ without pre_norm")
     p = _norm(Rn, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pre_weight, pre_bias, kind, eps)
-    gdt = torch.bfloat16 if grad_bf16 else torch.float32
-    p.flags |= GRAD_BF16 if grad_bf16 else 0
-    s = _on_device(stream, Rn, B, dZ, dRn, post_weight, post_bias, gate, pre_weight, pre_bias, dR, dB, workspace)
+    gdt = torch.float32
+    if grad_bf16:
+        gdt = torch.bfloat16
+        p.flags |= GRAD_BF16
+    s = _queue(stream, Rn, B, dZ, dRn, post_weight, post_bias, gate, pre_weight, pre_bias, dR, dB, workspace)
     if dZ is not None:
-        _shaped(dZ, gdt, (n, F), "dZ")
+        _shaped(dZ, gdt, shape, "dZ")
     if dRn is not None:
-        _shaped(dRn, Rn.dtype, (n, F), "dRn")
-    dR = _shaped(_empty((n, F), Rn.dtype, Rn, s) if dR is None else dR, Rn.dtype, (n, F), "dR")
+        _shaped(dRn, Rn.dtype, shape, "dRn")
+    dR = _empty(shape, Rn.dtype, Rn, stream) if dR is None else _shaped(dR, Rn.dtype, shape, "dR")
     if B is not None:
-        dB = _shaped(_empty((n, F), gdt, Rn, s) if dB is None else dB, gdt, (n, F), "dB")
-    elif dB is not None:
-        raise ValueError("dB without B")
-    vec = lambda t: None if t is None else _empty((F,), torch.float32, Rn, s)  # noqa: E731
+        dB = _empty(shape, gdt, Rn, stream) if dB is None else _shaped(dB, gdt, shape, "dB")
     dgate = None
     if gate is not None:
-        dgate = _empty(tuple(gate.shape), gdt if p.flags & GATE_FULL else torch.float32, Rn, s)
-    out = NormGrads(dR, dB, dgate, vec(post_weight), vec(post_bias), vec(pre_weight) if dZ is not None else None,
-                    vec(pre_bias) if dZ is not None else None)
+        dgate = _empty(gate.shape, gdt if p.flags & GATE_FULL else torch.float32, Rn, stream)
+    # the vectors' gradients: one piece of memory, a row each
+    want = [post_weight is not None, post_bias is not None, pre_weight is not None and dZ is not None,
+            pre_bias is not None and dZ is not None]
+    rows = iter(_empty((sum(want), F), torch.float32, Rn, stream).unbind(0) if any(want) else ())
+    vec = [next(rows) if w else None for w in want]
+    out = NormGrads(dR, dB, dgate, *vec)
     if workspace is None:
-        workspace = _empty((norm_residual_backward_workspace_bytes(n, F),), torch.uint8, Rn, s)
-    _dev(workspace, torch.uint8, "workspace")
-    g = NormGradPointers(_ptr(out.post_weight), _ptr(out.post_bias), _ptr(out.pre_weight), _ptr(out.pre_bias),
-                         _ptr(out.gate))
-    _check(_lib.dualgcn_norm_residual_backward(ctypes.byref(p), Rn.data_ptr(), _ptr(B), _ptr(dZ), _ptr(dRn),
-                                               dR.data_ptr(), _ptr(dB), ctypes.byref(g), n, F,
-                                               workspace.data_ptr(), workspace.numel(), _stream(s)),
+        workspace = _empty((norm_residual_backward_workspace_bytes(n, F),), torch.uint8, Rn, stream)
+    else:
+        _dev(workspace, torch.uint8, "workspace")
+    g = NormGradPointers(_ptr(vec[0]), _ptr(vec[1]), _ptr(vec[2]), _ptr(vec[3]), _ptr(dgate))
+    _check(_lib.dualgcn_norm_residual_backward(p, Rn.data_ptr(), _ptr(B), _ptr(dZ), _ptr(dRn), dR.data_ptr(), _ptr(dB),
+                                               g, n, F, workspace.data_ptr(), workspace.numel(), s),
            "dualgcn_norm_residual_backward")
     return out
 
@@ -694,35 +721,37 @@ def distill_xent(Y, ids, teacher, labels=None, temperature=1.0, soft_scale=None,
     soft_scale T^2 sum KL(teacher || softmax(Y / T)), hard = hard_scale sum of the labels'
     cross-entropy.  The scales default to 1 / (rows with an entry) and 1 / (labeled rows),
     counted on the host only when not given."""
-    _float_or_bf16(Y, "Y")
-    n, C = Y.shape
-    _dev(ids, torch.int32, "ids")
-    if ids.dim() != 2 or ids.shape[0] != n:
-        raise ValueError("ids must be [n, K]")
+    flags = IN_BF16 if _rows(Y, "Y") else 0
+    n, C = shape = Y.shape
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("ids must be an [n, K] tensor")
     K = ids.shape[1]
-    _float_or_bf16(teacher, "teacher")
+    _shaped(ids, torch.int32, (n, K), "ids")
+    if _rows(teacher, "teacher"):
+        flags |= TEACHER_BF16
     _shaped(teacher, teacher.dtype, (n, K), "teacher")
     if labels is not None:
         _shaped(labels, torch.int32, (n,), "labels")
-    s = _on_device(stream, Y, ids, teacher, labels, G, loss, workspace)
+    s = _queue(stream, Y, ids, teacher, labels, G, loss, workspace)
     if soft_scale is None:
         kept = (ids >= 0) & (ids < C) & (teacher != float("-inf"))
         soft_scale = 1.0 / max(1, int(kept.any(1).sum().item()))
     if hard_scale is None:
         hard_scale = 0.0 if labels is None else \
             1.0 / max(1, int(((labels >= 0) & (labels < C)).sum().item()))
-    gdt = torch.bfloat16 if grad_bf16 else torch.float32
-    G = _shaped(_empty((n, C), gdt, Y, s) if G is None else G, gdt, (n, C), "G")
-    loss = _shaped(_empty((3,), torch.float32, Y, s) if loss is None else loss, torch.float32, (3,), "loss")
+    gdt = torch.float32
+    if grad_bf16:
+        gdt = torch.bfloat16
+        flags |= GRAD_BF16
+    G = _empty(shape, gdt, Y, stream) if G is None else _shaped(G, gdt, shape, "G")
+    loss = _empty((3,), torch.float32, Y, stream) if loss is None else _shaped(loss, torch.float32, (3,), "loss")
     if workspace is None:
-        workspace = _empty((distill_workspace_bytes(n, C, K),), torch.uint8, Y, s)
-    _dev(workspace, torch.uint8, "workspace")
-    flags = (IN_BF16 if Y.dtype == torch.bfloat16 else 0) | (GRAD_BF16 if grad_bf16 else 0) | \
-        (TEACHER_BF16 if teacher.dtype == torch.bfloat16 else 0)
+        workspace = _empty((distill_workspace_bytes(n, C, K),), torch.uint8, Y, stream)
+    else:
+        _dev(workspace, torch.uint8, "workspace")
     _check(_lib.dualgcn_distill_xent(Y.data_ptr(), ids.data_ptr(), teacher.data_ptr(), _ptr(labels), n, C, K,
-                                     float(temperature), float(soft_scale), float(hard_scale), flags,
-                                     G.data_ptr(), loss.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                     _stream(s)), "dualgcn_distill_xent")
+                                     temperature, soft_scale, hard_scale, flags, G.data_ptr(), loss.data_ptr(),
+                                     workspace.data_ptr(), workspace.numel(), s), "dualgcn_distill_xent")
     return G, loss
 
 
@@ -730,17 +759,23 @@ def _fp8_blocks(F):
     return (F + FP8_BLOCK - 1) // FP8_BLOCK
 
 
+def _fp8_out(like, shape, blocks, Q, scales, stream):
+    e4m3 = torch.float8_e4m3fn
+    Q = _empty(shape, e4m3, like, stream) if Q is None else _shaped(Q, e4m3, shape, "Q")
+    if scales is None:
+        return Q, _empty(blocks, torch.float32, like, stream)
+    return Q, _shaped(scales, torch.float32, blocks, "scales")
+
+
 def quantize_fp8(X, Q=None, scales=None, stream=None):
     """(Q, scales): X ([n, F] float32 or bfloat16) as float8_e4m3fn [n, F] with a float32 scale, a
     power of two, for each 128 consecutive features of a row ([n, ceil(F / 128)])."""
-    _float_or_bf16(X, "X")
+    flags = IN_BF16 if _rows(X, "X") else 0
     n, F = X.shape
-    s = _on_device(stream, X, Q, scales)
-    Q = _shaped(_empty((n, F), torch.float8_e4m3fn, X, s) if Q is None else Q, torch.float8_e4m3fn, (n, F), "Q")
-    shape = (n, _fp8_blocks(F))
-    scales = _shaped(_empty(shape, torch.float32, X, s) if scales is None else scales, torch.float32, shape, "scales")
-    _check(_lib.dualgcn_quantize_fp8(X.data_ptr(), n, F, IN_BF16 if X.dtype == torch.bfloat16 else 0, Q.data_ptr(),
-                                     scales.data_ptr(), _stream(s)), "dualgcn_quantize_fp8")
+    s = _queue(stream, X, Q, scales)
+    Q, scales = _fp8_out(X, (n, F), (n, _fp8_blocks(F)), Q, scales, stream)
+    _check(_lib.dualgcn_quantize_fp8(X.data_ptr(), n, F, flags, Q.data_ptr(), scales.data_ptr(), s),
+           "dualgcn_quantize_fp8")
     return Q, scales
 
 
@@ -752,13 +787,11 @@ def quantize_weight_fp8(W, transpose=True, Q=None, scales=None, stream=None):
     if W.dim() != 2:
         raise ValueError("W must be [F_in, F_out]")
     F_in, F_out = W.shape
-    s = _on_device(stream, W, Q, scales)
+    s = _queue(stream, W, Q, scales)
     shape = (F_out, F_in) if transpose else (F_in, F_out)
-    Q = _shaped(_empty(shape, torch.float8_e4m3fn, W, s) if Q is None else Q, torch.float8_e4m3fn, shape, "Q")
-    shape = (_fp8_blocks(shape[0]), _fp8_blocks(shape[1]))
-    scales = _shaped(_empty(shape, torch.float32, W, s) if scales is None else scales, torch.float32, shape, "scales")
+    Q, scales = _fp8_out(W, shape, (_fp8_blocks(shape[0]), _fp8_blocks(shape[1])), Q, scales, stream)
     _check(_lib.dualgcn_quantize_weight_fp8(W.data_ptr(), F_in, F_out, 1 if transpose else 0, Q.data_ptr(),
-                                            scales.data_ptr(), _stream(s)), "dualgcn_quantize_weight_fp8")
+                                            scales.data_ptr(), s), "dualgcn_quantize_weight_fp8")
     return Q, scales
 
 
@@ -766,19 +799,19 @@ def update_fp8(X, sx, W, sw, T=None, out_bf16=False, stream=None):
     """T = X W from 8-bit operands on the matrix cores: X float8_e4m3fn [n, F_in] with its float32
     scales sx [n, ceil(F_in / 128)], W float8_e4m3fn [F_out, F_in] (transposed) with sw
     [ceil(F_out / 128), ceil(F_in / 128)].  T is float32 [n, F_out], or bfloat16 with out_bf16."""
-    _dev(X, torch.float8_e4m3fn, "X")
-    _dev(W, torch.float8_e4m3fn, "W")
-    if X.dim() != 2 or W.dim() != 2 or W.shape[1] != X.shape[1]:
-        raise ValueError("X must be [n, F_in] and W [F_out, F_in]")
+    if not (isinstance(X, torch.Tensor) and isinstance(W, torch.Tensor)) or X.dim() != 2 or W.dim() != 2:
+        raise ValueError("X must be an [n, F_in] tensor and W an [F_out, F_in] tensor")
     n, F_in = X.shape
     F_out = W.shape[0]
+    _shaped(X, torch.float8_e4m3fn, (n, F_in), "X")
+    _shaped(W, torch.float8_e4m3fn, (F_out, F_in), "W")
     _shaped(sx, torch.float32, (n, _fp8_blocks(F_in)), "sx")
     _shaped(sw, torch.float32, (_fp8_blocks(F_out), _fp8_blocks(F_in)), "sw")
-    s = _on_device(stream, X, sx, W, sw, T)
+    s = _queue(stream, X, sx, W, sw, T)
     tdt = torch.bfloat16 if out_bf16 else torch.float32
-    T = _shaped(_empty((n, F_out), tdt, X, s) if T is None else T, tdt, (n, F_out), "T")
+    T = _empty((n, F_out), tdt, X, stream) if T is None else _shaped(T, tdt, (n, F_out), "T")
     _check(_lib.dualgcn_update_fp8(X.data_ptr(), sx.data_ptr(), W.data_ptr(), sw.data_ptr(), T.data_ptr(), n, F_in,
-                                   F_out, OUT_BF16 if out_bf16 else 0, _stream(s)), "dualgcn_update_fp8")
+                                   F_out, OUT_BF16 if out_bf16 else 0, s), "dualgcn_update_fp8")
     return T
 
 
