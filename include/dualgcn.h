@@ -450,7 +450,7 @@ int dualgcn_backward_data(const void *G, const float *W, const void *M, float *d
 
 /*
  * The norms of a residual block.  The vectors are float32[F] (device); a NULL weight is all
- * ones, a NULL bias all zeros.  gate goes by the flags (at most one of the three kinds; NULL
+ * ones, a NULL bias all zeros; only layer norms take biases.  gate goes by the flags (at most one of the three kinds; NULL
  * without any).  eps is at least 2^-126 and scale finite.
  */
 typedef struct dualgcn_norm {

@@ -300,6 +300,7 @@ int check_norm(const dualgcn_norm *p, const void *B, int32_t n, int32_t F, uint3
     if (!gate != !p->gate || (!gate && (p->flags & DUALGCN_GATE_SIGMOID))) return DUALGCN_ERR_INVALID_ARG;
     if (!B && (gate || (p->flags & DUALGCN_NORM_POST))) return DUALGCN_ERR_INVALID_ARG;
     if (!(p->flags & DUALGCN_NORM_POST) && (p->post_weight || p->post_bias)) return DUALGCN_ERR_INVALID_ARG;
+    if (!(p->flags & DUALGCN_NORM_LAYER) && (p->post_bias || p->pre_bias)) return DUALGCN_ERR_INVALID_ARG;
     if (!elem_aligned(p->post_weight, false) || !elem_aligned(p->post_bias, false) ||
         !elem_aligned(p->pre_weight, false) || !elem_aligned(p->pre_bias, false) ||
         !elem_aligned(p->gate, (p->flags & DUALGCN_GATE_FULL) && (p->flags & DUALGCN_IN_BF16)))
@@ -604,6 +605,7 @@ int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, con
     const uint32_t f = norm->flags;
     const uint32_t gated = f & (DUALGCN_GATE_FEATURE | DUALGCN_GATE_NODE | DUALGCN_GATE_FULL);
     if ((!dZ && !dRn) || (dZ && !Rn) || (!B && dB)) return DUALGCN_ERR_INVALID_ARG;
+    if (!(f & DUALGCN_NORM_LAYER) && (g.post_bias || g.pre_bias)) return DUALGCN_ERR_INVALID_ARG;
     if ((!(f & DUALGCN_NORM_POST) && (g.post_weight || g.post_bias)) || (!dZ && (g.pre_weight || g.pre_bias)) ||
         (!gated && g.gate))
         return DUALGCN_ERR_INVALID_ARG;

@@ -37,6 +37,7 @@ struct Args {
     int32_t n, C, K;
     float temp_a;                    // log2(e) / T
     float soft, hard;                // coefficients of the gradient: soft T, hard
+    bool g_bf16, streaming;          // G is bfloat16; G is past the L2s
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -82,7 +83,7 @@ struct Entries {
         ids = a.ids;
         teacher = a.teacher;
         at = row * a.K;
-        K = a.K;
+        K = row < a.n ? a.K : 0;                         // a row behind the last has no entries
         C = a.C;
         l = lane;
 #pragma unroll
@@ -198,21 +199,21 @@ __device__ __forceinline__ void write_partial(double soft, double hard, double *
 // Rows whose logits stay in the registers of their TPR threads, Q quads each.  YBF, TBF: the
 // logits, the teacher's are bfloat16.
 template <int TPR, int Q, bool YBF, bool TBF>
-__global__ __launch_bounds__((TPR > kThreads ? TPR : kThreads)) void distill_rows_kernel(Args a, bool g_bf16) {
+__global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_rows_kernel(Args a) {
     constexpr bool TINY = TPR == 1;
-    constexpr int kBlock = TPR > kThreads ? TPR : kThreads, kGroups = kBlock / TPR;
+    constexpr int kBlock = TPR > 64 ? TPR : kThreads, kGroups = kBlock / TPR;
     __shared__ float sh[row_reduce_floats<TPR>()];
     __shared__ row_f32x4 tiles[kGroups][TPR * Q];
     __shared__ int flag;
     int turn = 0;
     const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
     const int C = a.C;
-    const bool ragged = C != 4 * TPR * Q;
+    const bool odd = C & 3, ragged = C != 4 * TPR * Q;
     float *tile = reinterpret_cast<float *>(tiles[g]);
     QuadPlace at[Q];
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-        at[q].set(4 * (l + q * TPR), C);
+        at[q].set(static_cast<uint32_t>(g) * C, 4 * (l + q * TPR), C);
         tiles[g][l + q * TPR] = row_f32x4{0.f, 0.f, 0.f, 0.f};
     }
     if (threadIdx.x == 0) flag = 0;
@@ -220,104 +221,111 @@ __global__ __launch_bounds__((TPR > kThreads ? TPR : kThreads)) void distill_row
     const bool same = a.temp_a == kLog2e;                // T = 1: one softmax serves both
     double soft = 0.0, hard = 0.0;
 
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + g; row < a.n;
-         row += static_cast<int64_t>(gridDim.x) * kGroups) {
-        const int64_t r0 = row * C;
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kGroups; row0 < a.n;
+         row0 += static_cast<int64_t>(gridDim.x) * kGroups) {
+        const int64_t row = row0 + g;
+        const int64_t elems = min(static_cast<int64_t>(kGroups), a.n - row0) * C;
+        const __amdgpu_buffer_rsrc_t wy = row_window<YBF>(a.Y, row0 * C, elems);
         RawRowQuad<YBF, TINY> raw[Q];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) raw[q].load(a.Y, r0, at[q]);
+        for (int q = 0; q < Q; ++q) raw[q].load(wy, at[q].at, at[q].count);
         Entries<TPR, TBF> en;
         en.load(a, row, l);
-        const int lab = a.labels ? a.labels[row] : -1;
+        const int lab = a.labels && row < a.n ? a.labels[row] : -1;
         const bool labeled = lab >= 0 && lab < C;
         float entropy;
         en.prepare(a.temp_a, sh, turn, entropy);
+        row_f32x4 o[Q];
         if (!en.taught && !labeled) {                    // zeros, whatever the logits
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const row_f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                if (g_bf16) store_quad<true>(a.G, r0 + 4 * (l + q * TPR), at[q].count, z);
-                else store_quad<false>(a.G, r0 + 4 * (l + q * TPR), at[q].count, z);
-            }
-            continue;
-        }
-        row_f32x4 y[Q];
-        float m[1] = {-FLT_MAX};                         // all of the row -inf: the sums are 0, G NaN
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            y[q] = raw[q].get(at[q], ragged);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (ragged && i >= at[q].count) y[q][i] = -INFINITY;
-                m[0] = fmaxf(m[0], y[q][i]);
-            }
-        }
-        row_reduce<TPR>(m, MaxOp(), sh, turn);
-        row_f32x4 et[Q], e1[Q];
-        float s[3] = {0.f, 0.f, 0.f};                    // at T, at 1, the label's y - m
-#pragma unroll
-        for (int q = 0; q < Q; ++q)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                y[q][i] -= m[0];
-                et[q][i] = exp2_fast(y[q][i] * a.temp_a);
-                s[0] += et[q][i];
-            }
-        if (labeled && !same) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    e1[q][i] = exp2_fast(y[q][i] * kLog2e);
-                    s[1] += e1[q][i];
-                }
+            for (int q = 0; q < Q; ++q) o[q] = row_f32x4{0.f, 0.f, 0.f, 0.f};
         } else {
+            row_f32x4 y[Q];
+            float m[1] = {-FLT_MAX};                     // all of the row -inf: the sums are 0, G NaN
 #pragma unroll
-            for (int q = 0; q < Q; ++q) e1[q] = et[q];
-            s[1] = s[0];
-        }
-        if (labeled) {
+            for (int q = 0; q < Q; ++q) {
+                y[q] = raw[q].get(at[q], odd);
+                if (ragged)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i >= at[q].count) y[q][i] = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m[0] = fmaxf(m[0], y[q][i]);
+            }
+            row_reduce<TPR>(m, MaxOp(), sh, turn);
+            row_f32x4 e1[Q];
+            float s[3] = {0.f, 0.f, 0.f};                // at T, at 1, the label's y - m
 #pragma unroll
             for (int q = 0; q < Q; ++q)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (4 * (l + q * TPR) + i == lab) s[2] = y[q][i];
-        }
-        row_reduce<TPR>(s, AddOp(), sh, turn);
-        if (en.taught) en.scatter(tile, 0, C, a.temp_a, &flag);
-        const float ct = en.taught ? a.soft : 0.f, c1 = labeled ? a.hard : 0.f;
-        const float it = ct / s[0], i1 = c1 / s[1];
-        float cross[1] = {0.f};
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            row_f32x4 o = et[q] * it;
-            if (labeled) o += e1[q] * i1;
-            if (en.taught) {
-                const row_f32x4 P = tiles[g][l + q * TPR];
-#pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (!(P[i] == 0.f)) {
-                        cross[0] = fmaf(P[i], y[q][i], cross[0]);
-                        o[i] = fmaf(-ct, P[i], o[i]);
+                    y[q][i] -= m[0];
+                    o[q][i] = exp2_fast(y[q][i] * a.temp_a);
+                    s[0] += o[q][i];
+                }
+            if (labeled) {
+                if (!same)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            e1[q][i] = exp2_fast(y[q][i] * kLog2e);
+                            s[1] += e1[q][i];
+                        }
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (4 * (l + q * TPR) + i == lab) s[2] = y[q][i];
+            }
+            row_reduce<TPR>(s, AddOp(), sh, turn);
+            if (en.taught) en.scatter(tile, 0, C, a.temp_a, &flag);
+            if (same) s[1] = s[0];
+            const float ct = en.taught ? a.soft : 0.f;
+            // at T = 1 the label's share of the softmax joins the teacher's
+            const float it = ct / s[0] + (same && labeled ? a.hard / s[0] : 0.f);
+            float cross[1] = {0.f};
+#pragma unroll
+            for (int q = 0; q < Q; ++q) o[q] *= it;
+            if (labeled) {
+                const float i1 = a.hard / s[1];
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    if (!same) o[q] += e1[q] * i1;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (4 * (l + q * TPR) + i == lab) o[q][i] -= a.hard;
+                }
+            }
+            if (en.taught) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    const row_f32x4 P = tiles[g][l + q * TPR];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        // no 0 * infinity where the class has no P
+                        cross[0] = fmaf(P[i], P[i] == 0.f ? 0.f : y[q][i], cross[0]);
+                        o[q][i] = fmaf(-ct, P[i], o[q][i]);
                     }
                 }
+                row_reduce<TPR>(cross, AddOp(), sh, turn);
+                if constexpr (TPR <= 64) row_sync<TPR>();    // P is read before it is cleared
+                en.clear(tile, 0, C);
+                row_sync<TPR>();
             }
-            if (labeled)
+            if (l == 0) {
+                if (en.taught) soft += entropy - static_cast<double>(a.temp_a) * cross[0] + __builtin_amdgcn_logf(s[0]);
+                if (labeled) hard += __builtin_amdgcn_logf(s[1]) - static_cast<double>(kLog2e) * s[2];
+            }
+        }
+        if (a.g_bf16) {
+            const __amdgpu_buffer_rsrc_t w = row_window<true>(a.G, row0 * C, elems);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (4 * (l + q * TPR) + i == lab) o[i] -= c1;
-            if (g_bf16) store_quad<true>(a.G, r0 + 4 * (l + q * TPR), at[q].count, o);
-            else store_quad<false>(a.G, r0 + 4 * (l + q * TPR), at[q].count, o);
-        }
-        if (en.taught) {
-            row_reduce<TPR>(cross, AddOp(), sh, turn);
-            if constexpr (TPR <= 64) row_sync<TPR>();    // P is read before it is cleared
-            en.clear(tile, 0, C);
-            row_sync<TPR>();
-        }
-        if (l == 0) {
-            if (en.taught) soft += entropy - static_cast<double>(a.temp_a) * cross[0] + __builtin_amdgcn_logf(s[0]);
-            if (labeled) hard += __builtin_amdgcn_logf(s[1]) - static_cast<double>(kLog2e) * s[2];
+            for (int q = 0; q < Q; ++q) store_row_quad<true, TINY>(w, at[q], o[q], odd, a.streaming);
+        } else {
+            const __amdgpu_buffer_rsrc_t w = row_window<false>(a.G, row0 * C, elems);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) store_row_quad<false, TINY>(w, at[q], o[q], odd, a.streaming);
         }
     }
     write_partial<kBlock>(soft, hard, a.partial + 2 * static_cast<int64_t>(blockIdx.x));
@@ -337,30 +345,38 @@ struct RowStats {
     float m, st, s1;
 };
 
+// Quad q of this thread in the piece at class c, none from class c1 on (a whole number of quads, or
+// the row's end).
+__device__ __forceinline__ void place(QuadPlace &at, int c, int q, int c1, int C) {
+    const int first = c + 4 * (static_cast<int>(threadIdx.x) + q * kLong);
+    at.set(0, first < c1 ? first : C, C);
+}
+
 // Classes [c0, c1) of a row: maximum and sums at T and at 1, over the workgroup.
 template <bool YBF>
 __device__ __forceinline__ RowStats sweep_stats(const Args &a, int64_t row, int c0, int c1, bool one, float *sh,
                                                 int &turn) {
     float m = -FLT_MAX, st = 0.f, s1 = 0.f;
-    const int64_t r0 = row * a.C;
+    const __amdgpu_buffer_rsrc_t w = row_window<YBF>(a.Y, row * a.C, a.C);
     for (int c = c0; c < c1; c += kPiece) {
         RawRowQuad<YBF, false> raw[kLongQ];
         QuadPlace at[kLongQ];
 #pragma unroll
         for (int q = 0; q < kLongQ; ++q) {
-            at[q].set(c + 4 * (static_cast<int>(threadIdx.x) + q * kLong), c1);
-            raw[q].load(a.Y, r0, at[q]);
+            place(at[q], c, q, c1, a.C);
+            raw[q].load(w, at[q].at, at[q].count);
         }
         row_f32x4 y[kLongQ];
         float top = m;
 #pragma unroll
         for (int q = 0; q < kLongQ; ++q) {
-            y[q] = raw[q].get(at[q], c + kPiece > c1);
+            y[q] = raw[q].get(at[q], a.C & 3);
+            if (c + kPiece > c1)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (c + kPiece > c1 && i >= at[q].count) y[q][i] = -INFINITY;
-                top = fmaxf(top, y[q][i]);
-            }
+                for (int i = 0; i < 4; ++i)
+                    if (i >= at[q].count) y[q][i] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, y[q][i]);
         }
         st *= exp2_fast((m - top) * a.temp_a);
         s1 *= exp2_fast((m - top) * kLog2e);
@@ -382,32 +398,36 @@ __device__ __forceinline__ RowStats sweep_stats(const Args &a, int64_t row, int 
     return RowStats{all[0], s[0], s[1]};
 }
 
+__device__ __forceinline__ void put(const Args &a, int64_t row, const QuadPlace &at, row_f32x4 o) {
+    const bool odd = a.C & 3;
+    if (a.g_bf16) store_row_quad<true, false>(row_window<true>(a.G, row * a.C, a.C), at, o, odd, a.streaming);
+    else store_row_quad<false, false>(row_window<false>(a.G, row * a.C, a.C), at, o, odd, a.streaming);
+}
+
 // The gradient of classes [c0, c1) and their part of the loss: sum of P (y - m), the
 // label's y - m (both on every thread).
 template <bool YBF, bool TBF>
 __device__ __forceinline__ float2 sweep_grad(const Args &a, int64_t row, int c0, int c1, const RowStats &s,
-                                             const Entries<kLong, TBF> &en, int lab, bool g_bf16,
-                                             row_f32x4 *tile, int *flag, float *sh, int &turn) {
-    const int64_t r0 = row * a.C;
-    const bool labeled = lab >= 0 && lab < a.C, same = a.temp_a == kLog2e;
+                                             const Entries<kLong, TBF> &en, int lab, row_f32x4 *tile, int *flag, float *sh, int &turn) {
+    const __amdgpu_buffer_rsrc_t wy = row_window<YBF>(a.Y, row * a.C, a.C);
+    const bool odd = a.C & 3, labeled = lab >= 0 && lab < a.C, same = a.temp_a == kLog2e;
     const float ct = en.taught ? a.soft : 0.f, ch = labeled ? a.hard : 0.f;
     const float it = ct / s.st, i1 = ch / (same ? s.st : s.s1);
     float part[2] = {0.f, 0.f};
     for (int c = c0; c < c1; c += kPiece) {
         const int end = min(c1, c + kPiece);
-        const bool ragged = c + kPiece > c1;
         RawRowQuad<YBF, false> raw[kLongQ];
         QuadPlace at[kLongQ];
 #pragma unroll
         for (int q = 0; q < kLongQ; ++q) {
-            at[q].set(c + 4 * (static_cast<int>(threadIdx.x) + q * kLong), c1);
-            raw[q].load(a.Y, r0, at[q]);
+            place(at[q], c, q, c1, a.C);
+            raw[q].load(wy, at[q].at, at[q].count);
         }
         if (en.taught) en.scatter(reinterpret_cast<float *>(tile), c, end, a.temp_a, flag);
 #pragma unroll
         for (int q = 0; q < kLongQ; ++q) {
             const int col = c + 4 * (static_cast<int>(threadIdx.x) + q * kLong);
-            const row_f32x4 y = raw[q].get(at[q], ragged);
+            const row_f32x4 y = raw[q].get(at[q], odd);
             row_f32x4 o;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -424,14 +444,12 @@ __device__ __forceinline__ float2 sweep_grad(const Args &a, int64_t row, int c0,
             if (en.taught) {
                 const row_f32x4 P = tile[threadIdx.x + q * kLong];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!(P[i] == 0.f)) {
-                        part[0] = fmaf(P[i], y[i] - s.m, part[0]);
-                        o[i] = fmaf(-ct, P[i], o[i]);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    part[0] = fmaf(P[i], P[i] == 0.f ? 0.f : y[i] - s.m, part[0]);
+                    o[i] = fmaf(-ct, P[i], o[i]);
+                }
             }
-            if (g_bf16) store_quad<true>(a.G, r0 + col, at[q].count, o);
-            else store_quad<false>(a.G, r0 + col, at[q].count, o);
+            put(a, row, at[q], o);
         }
         if (en.taught) {
             __syncthreads();
@@ -467,7 +485,7 @@ __global__ __launch_bounds__(kLong) void distill_stats_kernel(Args a) {
 // The gradient of rows of any length.  With one split the workgroup sweeps its rows' statistics
 // itself; else they come from `stats`.
 template <bool YBF, bool TBF>
-__global__ __launch_bounds__(kLong) void distill_long_kernel(Args a, bool g_bf16) {
+__global__ __launch_bounds__(kLong) void distill_long_kernel(Args a) {
     __shared__ float sh[row_reduce_floats<kLong>()];
     __shared__ row_f32x4 tile[kLong * kLongQ];
     __shared__ int flag;
@@ -487,10 +505,10 @@ __global__ __launch_bounds__(kLong) void distill_long_kernel(Args a, bool g_bf16
         float entropy;
         en.prepare(a.temp_a, sh, turn, entropy);
         if (!en.taught && !labeled) {
-            for (int c = c0 + 4 * static_cast<int>(threadIdx.x); c < c1; c += 4 * kLong) {
-                const row_f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                if (g_bf16) store_quad<true>(a.G, row * a.C + c, c1 - c, z);
-                else store_quad<false>(a.G, row * a.C + c, c1 - c, z);
+            for (int c = c0; c < c1; c += 4 * kLong) {
+                QuadPlace at;
+                place(at, c, 0, c1, a.C);
+                put(a, row, at, row_f32x4{0.f, 0.f, 0.f, 0.f});
             }
             continue;
         }
@@ -506,7 +524,7 @@ __global__ __launch_bounds__(kLong) void distill_long_kernel(Args a, bool g_bf16
                 s.s1 = fmaf(in[3 * k + 2], exp2_fast((in[3 * k] - s.m) * kLog2e), s.s1);
             }
         }
-        const float2 part = sweep_grad<YBF, TBF>(a, row, c0, c1, s, en, lab, g_bf16, tile, &flag, sh, turn);
+        const float2 part = sweep_grad<YBF, TBF>(a, row, c0, c1, s, en, lab, tile, &flag, sh, turn);
         if (threadIdx.x == 0) {
             if (en.taught) {
                 soft -= static_cast<double>(a.temp_a) * part.x;
@@ -554,7 +572,7 @@ __global__ __launch_bounds__(kThreads) void distill_loss_kernel(const double *__
 // ------------------------------------------------------------------ dispatch
 
 constexpr int kRegisterClasses = 8192;               // widest row in registers
-constexpr int kMaxBlocks = 2048;
+constexpr int kMaxBlocks = 8192;
 constexpr int kSplitBlocks = 512;                    // workgroups that fill the chip (two a CU)
 constexpr int kMinSplit = 4096;                      // classes a split has at least
 
@@ -569,32 +587,32 @@ int row_blocks(int32_t n, int groups) {
 }
 
 template <int TPR, int Q, bool YBF>
-int launch_rows(const Args &a, bool tbf, bool gbf, hipStream_t s) {
-    constexpr int kBlock = TPR > kThreads ? TPR : kThreads;
+int launch_rows(const Args &a, bool tbf, hipStream_t s) {
+    constexpr int kBlock = TPR > 64 ? TPR : kThreads;
     const int blocks = row_blocks(a.n, kBlock / TPR);
-    if (tbf) hipLaunchKernelGGL((distill_rows_kernel<TPR, Q, YBF, true>), dim3(blocks), dim3(kBlock), 0, s, a, gbf);
-    else hipLaunchKernelGGL((distill_rows_kernel<TPR, Q, YBF, false>), dim3(blocks), dim3(kBlock), 0, s, a, gbf);
+    if (tbf) hipLaunchKernelGGL((distill_rows_kernel<TPR, Q, YBF, true>), dim3(blocks), dim3(kBlock), 0, s, a);
+    else hipLaunchKernelGGL((distill_rows_kernel<TPR, Q, YBF, false>), dim3(blocks), dim3(kBlock), 0, s, a);
     return blocks;
 }
 
 template <bool YBF>
-int launch_any(const Args &a, bool tbf, bool gbf, hipStream_t s) {
+int launch_any(const Args &a, bool tbf, hipStream_t s) {
     const int C = a.C;
-    if (C < 4) return launch_rows<1, 1, YBF>(a, tbf, gbf, s);
-    if (C <= 32) return launch_rows<8, 1, YBF>(a, tbf, gbf, s);
-    if (C <= 64) return launch_rows<16, 1, YBF>(a, tbf, gbf, s);
-    if (C <= 128) return launch_rows<32, 1, YBF>(a, tbf, gbf, s);
-    if (C <= 256) return launch_rows<64, 1, YBF>(a, tbf, gbf, s);
-    if (C <= 512) return launch_rows<64, 2, YBF>(a, tbf, gbf, s);
-    if (C <= 1024) return launch_rows<64, 4, YBF>(a, tbf, gbf, s);
-    if (C <= 2048) return launch_rows<256, 2, YBF>(a, tbf, gbf, s);
-    if (C <= 4096) return launch_rows<256, 4, YBF>(a, tbf, gbf, s);
-    if (C <= kRegisterClasses) return launch_rows<512, 4, YBF>(a, tbf, gbf, s);
+    if (C < 4) return launch_rows<1, 1, YBF>(a, tbf, s);
+    if (C <= 32) return launch_rows<8, 1, YBF>(a, tbf, s);
+    if (C <= 64) return launch_rows<16, 1, YBF>(a, tbf, s);
+    if (C <= 128) return launch_rows<32, 1, YBF>(a, tbf, s);
+    if (C <= 256) return launch_rows<64, 1, YBF>(a, tbf, s);
+    if (C <= 512) return launch_rows<64, 2, YBF>(a, tbf, s);
+    if (C <= 1024) return launch_rows<64, 4, YBF>(a, tbf, s);
+    if (C <= 2048) return launch_rows<256, 2, YBF>(a, tbf, s);
+    if (C <= 4096) return launch_rows<256, 4, YBF>(a, tbf, s);
+    if (C <= kRegisterClasses) return launch_rows<512, 4, YBF>(a, tbf, s);
     const int splits = splits_of(a.n, C);
     const dim3 grid(splits, row_blocks(a.n, 1));
     if (splits > 1) hipLaunchKernelGGL(distill_stats_kernel<YBF>, grid, dim3(kLong), 0, s, a);
-    if (tbf) hipLaunchKernelGGL((distill_long_kernel<YBF, true>), grid, dim3(kLong), 0, s, a, gbf);
-    else hipLaunchKernelGGL((distill_long_kernel<YBF, false>), grid, dim3(kLong), 0, s, a, gbf);
+    if (tbf) hipLaunchKernelGGL((distill_long_kernel<YBF, true>), grid, dim3(kLong), 0, s, a);
+    else hipLaunchKernelGGL((distill_long_kernel<YBF, false>), grid, dim3(kLong), 0, s, a);
     return static_cast<int>(grid.x * grid.y);
 }
 
@@ -611,9 +629,10 @@ int launch_distill(const void *Y, bool y_bf16, const int32_t *ids, const void *t
                    const int32_t *labels, int32_t n, int32_t C, int32_t K, float T, float soft, float hard, void *G,
                    bool g_bf16, float *loss, void *workspace, hipStream_t s) {
     double *partial = static_cast<double *>(workspace);
+    const int64_t elems = static_cast<int64_t>(n) * C;
     const Args a{Y, teacher, ids, labels, G, partial, reinterpret_cast<float *>(partial + 2 * kMaxBlocks), n, C, K,
-                 T == 1.f ? kLog2e : kLog2e / T, soft * T, hard};
-    const int blocks = y_bf16 ? launch_any<true>(a, t_bf16, g_bf16, s) : launch_any<false>(a, t_bf16, g_bf16, s);
+                 T == 1.f ? kLog2e : kLog2e / T, soft * T, hard, g_bf16, elems * (g_bf16 ? 2 : 4) > (int64_t{32} << 20)};
+    const int blocks = y_bf16 ? launch_any<true>(a, t_bf16, s) : launch_any<false>(a, t_bf16, s);
     const int st = hip_status(hipGetLastError());
     if (st) return st;
     hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kThreads), 0, s, partial, blocks,

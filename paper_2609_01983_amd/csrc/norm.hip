@@ -17,7 +17,7 @@
 // Both passes are bound by memory (about one flop a byte): a row stays in the registers of
 // its threads from the load to the store, so every operand is read and every output written
 // once.  The threads of a row are as many as hold it in few quads: 8 to 64 lanes of a
-// wavefront up to 1,024 features, 256 or 512 threads up to 8,192.
+// wavefront up to 768 features, a workgroup of 128 to 1,024 threads up to 8,192.
 #include "rows.h"
 
 #include <algorithm>
@@ -27,46 +27,54 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxBlocks = 1024;                     // workgroups, hence partial column sums, of a backward pass
+constexpr int64_t kMaxForwardBlocks = int64_t{1} << 21;
 
 // ------------------------------------------------------------------ shared by both directions
 
 template <int TPR, int Q>
 struct Shape {
-    static constexpr int kBlock = TPR > kThreads ? TPR : kThreads;   // threads of a workgroup
+    static constexpr int kBlock = TPR > 64 ? TPR : kThreads;         // threads of a workgroup
     static constexpr int kGroups = kBlock / TPR;                     // rows it works on at a time
 };
 
-// rows whose threads hold more than they have: the row's columns past F are zeros
-template <int TPR, int Q>
-__device__ __forceinline__ bool is_ragged(int F) {
-    return F != 4 * TPR * Q;
-}
-
-template <int Q, bool TINY>
-__device__ __forceinline__ void load_vector(const float *w, float missing, const QuadPlace (&at)[Q],
-                                            bool ragged, row_f32x4 (&out)[Q]) {
+// Where a vector of F features may be: a window of it, or what stands for a missing one.
+struct Vector {
+    __amdgpu_buffer_rsrc_t w;
+    bool there;
+    float missing;
+    __device__ __forceinline__ Vector(const void *p, int F, float missing_)
+        : w(row_window<false>(p, 0, p ? F : 0)), there(p != nullptr), missing(missing_) {}
+    template <int Q, bool TINY>
+    __device__ __forceinline__ void load(const QuadPlace (&at)[Q], bool odd, row_f32x4 (&out)[Q]) const {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        if (w) {
-            RawRowQuad<false, TINY> raw;
-            raw.load(w, 0, at[q]);
-            out[q] = raw.get(at[q], ragged);
-        } else {
-            out[q] = row_f32x4{missing, missing, missing, missing};
+        for (int q = 0; q < Q; ++q) {
+            if (there) {
+                RawRowQuad<false, TINY> raw;
+                raw.load(w, at[q].col, at[q].count);
+                out[q] = raw.get(at[q], odd);
+            } else {
+                out[q] = row_f32x4{missing, missing, missing, missing};
+            }
         }
     }
+};
+
+// zeros behind the row's end; ragged: the row has fewer columns than its threads have places
+template <int Q>
+__device__ __forceinline__ void cut(row_f32x4 (&x)[Q], const QuadPlace (&at)[Q], bool ragged) {
+    if (ragged)
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i >= at[q].count) x[q][i] = 0.f;
 }
 
-// x - mean on the row's columns, zeros behind them
 template <int Q>
 __device__ __forceinline__ void centre(row_f32x4 (&x)[Q], float mean, const QuadPlace (&at)[Q], bool ragged) {
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float c = x[q][i] - mean;
-            x[q][i] = ragged && i >= at[q].count ? 0.f : c;
-        }
+    for (int q = 0; q < Q; ++q) x[q] -= mean;
+    cut(x, at, ragged);
 }
 
 template <int Q>
@@ -90,10 +98,10 @@ __device__ __forceinline__ float dot_of(const row_f32x4 (&x)[Q], const row_f32x4
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
 // x on entry, (x - mean) r on return; the row's threads share the statistics
-template <int TPR, int Q>
-__device__ __forceinline__ void normalise(row_f32x4 (&x)[Q], const QuadPlace (&at)[Q], bool ragged, bool layer,
-                                          float inv_f, float eps, float *sh, int &turn) {
-    if (layer) {
+template <int TPR, int Q, bool LAYER>
+__device__ __forceinline__ void normalise(row_f32x4 (&x)[Q], const QuadPlace (&at)[Q], bool ragged, float inv_f,
+                                          float eps, float *sh, int &turn) {
+    if constexpr (LAYER) {
         float m[1] = {sum_of(x)};
         row_reduce<TPR>(m, AddOp(), sh, turn);
         centre(x, m[0] * inv_f, at, ragged);
@@ -114,91 +122,79 @@ struct ForwardArgs {
     int32_t n, F;
     float eps, scale;
     uint32_t flags;
+    bool streaming;                  // outputs past the L2s: stored with a non-temporal hint
 };
 
-// A: B and a full gate are bfloat16; S: the stream is.
-template <int TPR, int Q, bool A, bool S>
+// LAYER: layer norms; A: B and a full gate are bfloat16; S: the stream is.  Behind a row's end every
+// operand and weight is zero, so RMS norms need no masks; a mean taken off is cut there.
+template <int TPR, int Q, bool LAYER, bool A, bool S>
 __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(ForwardArgs a) {
     constexpr bool TINY = TPR == 1;
-    constexpr bool kHold = Q <= 2;                   // the weights stay in registers over the rows
     constexpr int kGroups = Shape<TPR, Q>::kGroups;
     __shared__ float sh[row_reduce_floats<TPR>()];
     int turn = 0;
     const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
     const int F = a.F;
-    const bool ragged = is_ragged<TPR, Q>(F);
+    const bool odd = F & 3, ragged = F != 4 * TPR * Q;
     const float inv_f = 1.f / static_cast<float>(F);
-    const bool layer = a.flags & DUALGCN_NORM_LAYER, post = a.flags & DUALGCN_NORM_POST;
-    const bool sig = a.flags & DUALGCN_GATE_SIGMOID;
+    const bool post = a.flags & DUALGCN_NORM_POST, sig = a.flags & DUALGCN_GATE_SIGMOID;
     QuadPlace at[Q];
 #pragma unroll
-    for (int q = 0; q < Q; ++q) at[q].set(4 * (l + q * TPR), F);
+    for (int q = 0; q < Q; ++q) at[q].set(static_cast<uint32_t>(g) * F, 4 * (l + q * TPR), F);
 
-    row_f32x4 w1[Q], b1[Q], w2[Q], b2[Q], gc[Q];
-    auto vectors = [&]() {
-        if (post) {
-            load_vector<Q, TINY>(a.w1, 1.f, at, ragged, w1);
-            load_vector<Q, TINY>(a.b1, 0.f, at, ragged, b1);
-        }
-        if (a.Z) {
-            load_vector<Q, TINY>(a.w2, 1.f, at, ragged, w2);
-            load_vector<Q, TINY>(a.b2, 0.f, at, ragged, b2);
-        }
-        if (a.flags & DUALGCN_GATE_FEATURE) {
-            load_vector<Q, TINY>(static_cast<const float *>(a.gate), 1.f, at, ragged, gc);
-            if (sig)
-#pragma unroll
-                for (int q = 0; q < Q; ++q)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) gc[q][i] = sigmoid(gc[q][i]);
-        }
-    };
-    if constexpr (kHold) vectors();
-
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + g; row < a.n;
-         row += static_cast<int64_t>(gridDim.x) * kGroups) {
-        const int64_t r0 = row * F;
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kGroups; row0 < a.n;
+         row0 += static_cast<int64_t>(gridDim.x) * kGroups) {
+        const int64_t first = row0 * F;
+        const int rows = static_cast<int>(min(static_cast<int64_t>(kGroups), a.n - row0));
+        const int64_t elems = static_cast<int64_t>(rows) * F;
         RawRowQuad<S, TINY> rr[Q];
         RawRowQuad<A, TINY> rb[Q], rg[Q];
         float gn = 1.f;
+        const __amdgpu_buffer_rsrc_t wr = row_window<S>(a.R, first, elems);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) rr[q].load(a.R, r0, at[q]);
+        for (int q = 0; q < Q; ++q) rr[q].load(wr, at[q].at, at[q].count);
         if (a.B) {
+            const __amdgpu_buffer_rsrc_t wb = row_window<A>(a.B, first, elems);
 #pragma unroll
-            for (int q = 0; q < Q; ++q) rb[q].load(a.B, r0, at[q]);
-            if (a.flags & DUALGCN_GATE_FULL)
+            for (int q = 0; q < Q; ++q) rb[q].load(wb, at[q].at, at[q].count);
+            if (a.flags & DUALGCN_GATE_FULL) {
+                const __amdgpu_buffer_rsrc_t wg = row_window<A>(a.gate, first, elems);
 #pragma unroll
-                for (int q = 0; q < Q; ++q) rg[q].load(a.gate, r0, at[q]);
-            if (a.flags & DUALGCN_GATE_NODE) gn = static_cast<const float *>(a.gate)[row];
+                for (int q = 0; q < Q; ++q) rg[q].load(wg, at[q].at, at[q].count);
+            }
+            if (a.flags & DUALGCN_GATE_NODE) gn = static_cast<const float *>(a.gate)[row0 + (g < rows ? g : 0)];
         }
-        if constexpr (!kHold) vectors();
         row_f32x4 x[Q];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) x[q] = rr[q].get(at[q], ragged);
+        for (int q = 0; q < Q; ++q) x[q] = rr[q].get(at[q], odd);
         if (a.B) {
-            row_f32x4 v[Q];
+            row_f32x4 v[Q], w[Q], c[Q];
 #pragma unroll
-            for (int q = 0; q < Q; ++q) v[q] = rb[q].get(at[q], ragged);
+            for (int q = 0; q < Q; ++q) v[q] = rb[q].get(at[q], odd);
             if (post) {
-                normalise<TPR, Q>(v, at, ragged, layer, inv_f, a.eps, sh, turn);
+                Vector(a.w1, F, 1.f).load<Q, TINY>(at, odd, w);
+                if constexpr (LAYER) Vector(a.b1, F, 0.f).load<Q, TINY>(at, odd, c);
+                normalise<TPR, Q, LAYER>(v, at, ragged, inv_f, a.eps, sh, turn);
 #pragma unroll
-                for (int q = 0; q < Q; ++q) v[q] = v[q] * w1[q] + b1[q];
+                for (int q = 0; q < Q; ++q) v[q] = LAYER ? v[q] * w[q] + c[q] : v[q] * w[q];
             }
-            if (a.flags & DUALGCN_GATE_FEATURE) {
+            if (a.flags & (DUALGCN_GATE_FEATURE | DUALGCN_GATE_FULL)) {
+                if (a.flags & DUALGCN_GATE_FEATURE) {
+                    Vector(a.gate, F, 1.f).load<Q, TINY>(at, odd, w);
+                } else {
 #pragma unroll
-                for (int q = 0; q < Q; ++q) v[q] *= gc[q];
-            }
-            if (a.flags & DUALGCN_GATE_FULL) {
-#pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    row_f32x4 gate = rg[q].get(at[q], ragged);
-                    if (sig)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) gate[i] = sigmoid(gate[i]);
-                    v[q] *= gate;
+                    for (int q = 0; q < Q; ++q) w[q] = rg[q].get(at[q], odd);
                 }
+                if (sig)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[q][i] = sigmoid(w[q][i]);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) v[q] *= w[q];
             }
             const float scale = a.scale * (sig && (a.flags & DUALGCN_GATE_NODE) ? sigmoid(gn) : gn);
+            const __amdgpu_buffer_rsrc_t wn = row_window<S>(a.Rn, first, elems);
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
 #pragma unroll
@@ -206,18 +202,25 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(
                     x[q][i] = fmaf(scale, v[q][i], x[q][i]);
                     // the next norm (and the backward pass) take the stream as it is stored
                     if constexpr (S) x[q][i] = through_bf16(x[q][i]);
-                    if (ragged && i >= at[q].count) x[q][i] = 0.f;     // b1 may have left the row's end
                 }
-                store_quad<S>(a.Rn, r0 + 4 * (l + q * TPR), at[q].count, x[q]);
+                store_row_quad<S, TINY>(wn, at[q], x[q], odd, a.streaming);
             }
         }
         if (a.Z) {
-            normalise<TPR, Q>(x, at, ragged, layer, inv_f, a.eps, sh, turn);
+            row_f32x4 w[Q], c[Q];
+            Vector(a.w2, F, 1.f).load<Q, TINY>(at, odd, w);
+            if constexpr (LAYER) Vector(a.b2, F, 0.f).load<Q, TINY>(at, odd, c);
+            normalise<TPR, Q, LAYER>(x, at, ragged, inv_f, a.eps, sh, turn);
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const row_f32x4 z = x[q] * w2[q] + b2[q];
-                if (a.flags & DUALGCN_OUT_BF16) store_quad<true>(a.Z, r0 + 4 * (l + q * TPR), at[q].count, z);
-                else store_quad<false>(a.Z, r0 + 4 * (l + q * TPR), at[q].count, z);
+            for (int q = 0; q < Q; ++q) x[q] = LAYER ? x[q] * w[q] + c[q] : x[q] * w[q];
+            if (a.flags & DUALGCN_OUT_BF16) {
+                const __amdgpu_buffer_rsrc_t wz = row_window<true>(a.Z, first, elems);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) store_row_quad<true, TINY>(wz, at[q], x[q], odd, a.streaming);
+            } else {
+                const __amdgpu_buffer_rsrc_t wz = row_window<false>(a.Z, first, elems);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) store_row_quad<false, TINY>(wz, at[q], x[q], odd, a.streaming);
             }
         }
     }
@@ -238,38 +241,77 @@ struct BackwardArgs {
     float eps, scale;
     uint32_t flags;
     uint32_t want;                   // bit s: slot s is wanted
+    bool streaming;
 };
 
-// A: B and a full gate are bfloat16; S: the stream and its gradients are; G: dZ, dB and a full
-// gate's gradient are.
-template <int TPR, int Q, bool A, bool S, bool G>
+// What a backward pass reads of its rows, from `row0` on.
+template <int Q, bool TINY, bool A, bool S, bool G>
+struct RowIn {
+    RawRowQuad<S, TINY> r[Q], d[Q];
+    RawRowQuad<G, TINY> z[Q];
+    RawRowQuad<A, TINY> b[Q], g[Q];
+    float gn;
+
+    template <class T>
+    __device__ __forceinline__ static void take(T (&to)[Q], __amdgpu_buffer_rsrc_t w, const QuadPlace (&at)[Q]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) to[q].load(w, at[q].at, at[q].count);
+    }
+    // no rows (row0 >= n): zeros
+    __device__ __forceinline__ void load(const BackwardArgs &a, int64_t row0, int groups, int group, const QuadPlace (&at)[Q]) {
+        const int64_t rows = max(int64_t{0}, min(static_cast<int64_t>(groups), a.n - row0));
+        const int64_t first = row0 * a.F, elems = rows * a.F;
+        if (a.dZ) {
+            take(r, row_window<S>(a.Rn, first, elems), at);
+            take(z, row_window<G>(a.dZ, first, elems), at);
+        }
+        if (a.dRn) take(d, row_window<S>(a.dRn, first, elems), at);
+        if (a.B) {
+            take(b, row_window<A>(a.B, first, elems), at);
+            if (a.flags & DUALGCN_GATE_FULL) take(g, row_window<A>(a.gate, first, elems), at);
+            gn = 1.f;
+            if (a.flags & DUALGCN_GATE_NODE)
+                gn = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(row_window<false>(a.gate, row0, rows), group * 4u, 0, 0));
+        }
+    }
+};
+
+// LAYER: layer norms; A: B and a full gate are bfloat16; S: the stream and its gradients are; G: dZ,
+// dB and a full gate's gradient are.
+template <int TPR, int Q, bool LAYER, bool A, bool S, bool G>
 __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_backward_kernel(BackwardArgs a) {
     constexpr bool TINY = TPR == 1;
+    // One quad a thread: the weights and the column sums stay in registers over the rows.  More: the
+    // weights are read again from the cache, and the sums of w1, b1, w2, b2 are kept in LDS, each thread
+    // at its own places (6 accesses of 16 bytes a quad, a small part of LDS's rate).
     constexpr bool kHold = Q <= 1;
+    constexpr bool kAhead = Q < 4;                   // registers for the next row's operands
+    extern __shared__ row_f32x4 kept[];              // !kHold: [slots wanted of the four][Q][kBlock]
     constexpr int kBlock = Shape<TPR, Q>::kBlock, kGroups = Shape<TPR, Q>::kGroups;
     __shared__ float sh[row_reduce_floats<TPR>()];
     __shared__ row_f32x4 join[kGroups > 1 ? kBlock : 1];
     int turn = 0;
     const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
     const int F = a.F;
-    const bool ragged = is_ragged<TPR, Q>(F);
+    const bool odd = F & 3, ragged = F != 4 * TPR * Q;
     const float inv_f = 1.f / static_cast<float>(F);
-    const bool layer = a.flags & DUALGCN_NORM_LAYER, post = a.flags & DUALGCN_NORM_POST;
-    const bool sig = a.flags & DUALGCN_GATE_SIGMOID;
+    const bool post = a.flags & DUALGCN_NORM_POST, sig = a.flags & DUALGCN_GATE_SIGMOID;
     const bool pre = a.dZ != nullptr, block = a.B != nullptr;
     QuadPlace at[Q];
 #pragma unroll
-    for (int q = 0; q < Q; ++q) at[q].set(4 * (l + q * TPR), F);
+    for (int q = 0; q < Q; ++q) at[q].set(static_cast<uint32_t>(g) * F, 4 * (l + q * TPR), F);
 
     row_f32x4 w1[Q], b1[Q], w2[Q], gc[Q];
-    auto vectors = [&]() {
+    auto vector_of_pre = [&]() {
+        if (pre) Vector(a.w2, F, 1.f).load<Q, TINY>(at, odd, w2);
+    };
+    auto vectors_of_post = [&]() {
         if (post) {
-            load_vector<Q, TINY>(a.w1, 1.f, at, ragged, w1);
-            load_vector<Q, TINY>(a.b1, 0.f, at, ragged, b1);
+            Vector(a.w1, F, 1.f).load<Q, TINY>(at, odd, w1);
+            if constexpr (LAYER) Vector(a.b1, F, 0.f).load<Q, TINY>(at, odd, b1);
         }
-        if (pre) load_vector<Q, TINY>(a.w2, 1.f, at, ragged, w2);
         if (a.flags & DUALGCN_GATE_FEATURE) {
-            load_vector<Q, TINY>(static_cast<const float *>(a.gate), 1.f, at, ragged, gc);
+            Vector(a.gate, F, 1.f).load<Q, TINY>(at, odd, gc);
             if (sig)
 #pragma unroll
                 for (int q = 0; q < Q; ++q)
@@ -277,145 +319,154 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_backward_kernel(
                     for (int i = 0; i < 4; ++i) gc[q][i] = sigmoid(gc[q][i]);
         }
     };
-    if constexpr (kHold) vectors();
+    if constexpr (kHold) {
+        vector_of_pre();
+        vectors_of_post();
+    }
 
-    row_f32x4 acc[kSlots][Q];
+    row_f32x4 acc[kHold ? 4 : 1][Q], acc_gate[Q];
+    // slot s's place among the wanted ones
+    auto place = [&](int s, int q) { return (__popc(a.want & ((1u << s) - 1u)) * Q + q) * kBlock + static_cast<int>(threadIdx.x); };
+    auto add = [&](int s, int q, row_f32x4 v) {
+        if constexpr (kHold) acc[s][q] += v;
+        else if (a.want >> s & 1) kept[place(s, q)] += v;
+    };
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s)
+    for (int q = 0; q < Q; ++q) {
+        acc_gate[q] = row_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 0; q < Q; ++q) acc[s][q] = row_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < 4; ++s) {
+            if constexpr (kHold) acc[s][q] = acc_gate[q];
+            else if (a.want >> s & 1) kept[place(s, q)] = acc_gate[q];
+        }
+    }
 
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + g; row < a.n;
-         row += static_cast<int64_t>(gridDim.x) * kGroups) {
-        const int64_t r0 = row * F;
-        RawRowQuad<S, TINY> raw_r[Q], raw_d[Q];
-        RawRowQuad<G, TINY> raw_z[Q];
-        RawRowQuad<A, TINY> raw_b[Q], raw_g[Q];
-        float gn = 1.f;
-        if (pre) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                raw_r[q].load(a.Rn, r0, at[q]);
-                raw_z[q].load(a.dZ, r0, at[q]);
-            }
-        }
-        if (a.dRn) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) raw_d[q].load(a.dRn, r0, at[q]);
-        }
-        if (block) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) raw_b[q].load(a.B, r0, at[q]);
-            if (a.flags & DUALGCN_GATE_FULL)
-#pragma unroll
-                for (int q = 0; q < Q; ++q) raw_g[q].load(a.gate, r0, at[q]);
-            if (a.flags & DUALGCN_GATE_NODE) gn = static_cast<const float *>(a.gate)[row];
-        }
-        if constexpr (!kHold) vectors();
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+    int64_t row0 = static_cast<int64_t>(blockIdx.x) * kGroups;
+    RowIn<Q, TINY, A, S, G> in, next;
+    if constexpr (kAhead) in.load(a, row0, kGroups, g, at);
+    for (; row0 < a.n; row0 += step) {
+        const int rows = static_cast<int>(min(static_cast<int64_t>(kGroups), a.n - row0));
+        const int64_t first = row0 * F, elems = static_cast<int64_t>(rows) * F;
+        // the next rows are on their way while these are worked on
+        if constexpr (kAhead) next.load(a, row0 + step, kGroups, g, at);
+        else in.load(a, row0, kGroups, g, at);
+        if constexpr (!kHold) vector_of_pre();
 
         row_f32x4 x[Q], t[Q], b[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            x[q] = pre ? raw_r[q].get(at[q], ragged) : row_f32x4{0.f, 0.f, 0.f, 0.f};
-            t[q] = pre ? raw_z[q].get(at[q], ragged) : row_f32x4{0.f, 0.f, 0.f, 0.f};
-            b[q] = block ? raw_b[q].get(at[q], ragged) : row_f32x4{0.f, 0.f, 0.f, 0.f};
+            x[q] = pre ? in.r[q].get(at[q], odd) : row_f32x4{0.f, 0.f, 0.f, 0.f};
+            t[q] = pre ? in.z[q].get(at[q], odd) : row_f32x4{0.f, 0.f, 0.f, 0.f};
+            b[q] = block ? in.b[q].get(at[q], odd) : row_f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        // both norms' statistics, in two reductions (one for RMS norms); the second takes the
+        // Behind a row's end, and in rows behind the last, every operand and weight is zero.
+        // Both norms' statistics, in two reductions (one for RMS norms); the second takes the
         // sums of t w2 and t w2 (x - m2) along
-        if (layer) {
+        if constexpr (LAYER) {
             float m[2] = {sum_of(x), sum_of(b)};
             row_reduce<TPR>(m, AddOp(), sh, turn);
             if (pre) centre(x, m[0] * inv_f, at, ragged);
             if (post) centre(b, m[1] * inv_f, at, ragged);
         }
-        float st[4] = {dot_of(x, x), dot_of(b, b), 0.f, 0.f};
         row_f32x4 tw[Q];
+        float s2 = 0.f, s3 = 0.f;
         if (pre) {
 #pragma unroll
             for (int q = 0; q < Q; ++q) tw[q] = t[q] * w2[q];
-            st[2] = sum_of(tw);
-            st[3] = dot_of(tw, x);
+            s2 = dot_of(tw, x);
+            if constexpr (LAYER) s3 = sum_of(tw);
         }
+        float st[LAYER ? 4 : 3];
+        st[0] = dot_of(x, x);
+        st[1] = dot_of(b, b);
+        st[2] = s2;
+        if constexpr (LAYER) st[3] = s3;
         row_reduce<TPR>(st, AddOp(), sh, turn);
 
         // the stream's gradient
         row_f32x4 d[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q)
-            d[q] = a.dRn ? raw_d[q].get(at[q], ragged) : row_f32x4{0.f, 0.f, 0.f, 0.f};
+            d[q] = a.dRn ? in.d[q].get(at[q], odd) : row_f32x4{0.f, 0.f, 0.f, 0.f};
         if (pre) {
             const float r2 = __builtin_amdgcn_rsqf(fmaf(st[0], inv_f, a.eps));
-            const float mt = layer ? st[2] * inv_f : 0.f;
-            const float mtu = r2 * st[3] * inv_f;
+            const float mtu = r2 * st[2] * inv_f;
+            if constexpr (LAYER) centre(tw, st[3] * inv_f, at, ragged);
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 x[q] *= r2;
-                acc[kW2][q] += t[q] * x[q];
-                acc[kB2][q] += t[q];
-                d[q] += r2 * (tw[q] - mt - x[q] * mtu);
+                add(kW2, q, t[q] * x[q]);
+                if constexpr (LAYER) add(kB2, q, t[q]);
+                d[q] += r2 * (tw[q] - x[q] * mtu);
             }
         }
+        if constexpr (!kHold) vectors_of_post();
         if (a.dR) {
+            const __amdgpu_buffer_rsrc_t w = row_window<S>(a.dR, first, elems);
 #pragma unroll
-            for (int q = 0; q < Q; ++q) store_quad<S>(a.dR, r0 + 4 * (l + q * TPR), at[q].count, d[q]);
+            for (int q = 0; q < Q; ++q) store_row_quad<S, TINY>(w, at[q], d[q], odd, a.streaming);
         }
         if (block) {
             const float r1 = post ? __builtin_amdgcn_rsqf(fmaf(st[1], inv_f, a.eps)) : 1.f;
             row_f32x4 v[Q];                            // scale * d * gate, the gradient of post(B)
             float sums[3] = {0.f, 0.f, 0.f};
-            const float gnode = a.flags & DUALGCN_GATE_NODE ? (sig ? sigmoid(gn) : gn) : 1.f;
+            const float gnode = sig ? sigmoid(in.gn) : in.gn;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 b[q] *= r1;
-                const row_f32x4 p = post ? b[q] * w1[q] + b1[q] : b[q];
-                row_f32x4 gate = row_f32x4{gnode, gnode, gnode, gnode};
-                if (a.flags & DUALGCN_GATE_FEATURE) gate = gc[q];
-                if (a.flags & DUALGCN_GATE_FULL) {
-                    gate = raw_g[q].get(at[q], ragged);
-                    if (sig)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) gate[i] = sigmoid(gate[i]);
-                }
+                row_f32x4 p = b[q];
+                if (post) p = LAYER ? b[q] * w1[q] + b1[q] : b[q] * w1[q];
                 d[q] *= a.scale;
-                v[q] = d[q] * gate;
                 row_f32x4 dg = d[q] * p;               // the gate's gradient
-                if (sig) dg *= gate * (1.f - gate);
-                if (ragged) {                          // p and gate are not zero behind the row's end
+                if (a.flags & (DUALGCN_GATE_FEATURE | DUALGCN_GATE_FULL)) {
+                    row_f32x4 gate;
+                    if (a.flags & DUALGCN_GATE_FEATURE) {
+                        gate = gc[q];
+                    } else {
+                        gate = in.g[q].get(at[q], odd);
+                        if (sig)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (i >= at[q].count) {
-                            dg[i] = 0.f;
-                            v[q][i] = 0.f;
-                        }
+                            for (int i = 0; i < 4; ++i) gate[i] = sigmoid(gate[i]);
                     }
+                    v[q] = d[q] * gate;
+                    if (sig) dg *= gate * (1.f - gate);
+                } else if (a.flags & DUALGCN_GATE_NODE) {
+                    v[q] = d[q] * gnode;
+                    if (sig) dg *= gnode * (1.f - gnode);
+                } else {
+                    v[q] = d[q];
                 }
-                acc[kGate][q] += dg;
+                acc_gate[q] += dg;
                 sums[2] += (dg[0] + dg[1]) + (dg[2] + dg[3]);
                 if (a.dgate && (a.flags & DUALGCN_GATE_FULL))
-                    store_quad<G>(a.dgate, r0 + 4 * (l + q * TPR), at[q].count, dg);
+                    store_row_quad<G, TINY>(row_window<G>(a.dgate, first, elems), at[q], dg, odd, a.streaming);
             }
             if (post) {
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {
-                    acc[kW1][q] += v[q] * b[q];
-                    acc[kB1][q] += v[q];
+                    add(kW1, q, v[q] * b[q]);
+                    if constexpr (LAYER) add(kB1, q, v[q]);
                     v[q] *= w1[q];
                 }
-                sums[0] = sum_of(v);
-                sums[1] = dot_of(v, b);
+                sums[0] = dot_of(v, b);
+                if constexpr (LAYER) sums[1] = sum_of(v);
             }
             if (post || (a.flags & DUALGCN_GATE_NODE)) row_reduce<TPR>(sums, AddOp(), sh, turn);
             if (post) {
-                const float ms = layer ? sums[0] * inv_f : 0.f, msu = sums[1] * inv_f;
+                const float msu = sums[0] * inv_f, ms = sums[1] * inv_f;
 #pragma unroll
-                for (int q = 0; q < Q; ++q) v[q] = r1 * (v[q] - ms - b[q] * msu);
+                for (int q = 0; q < Q; ++q) v[q] = r1 * (LAYER ? v[q] - ms - b[q] * msu : v[q] - b[q] * msu);
             }
-            if (a.dgate && (a.flags & DUALGCN_GATE_NODE) && l == 0) static_cast<float *>(a.dgate)[row] = sums[2];
+            if (a.dgate && (a.flags & DUALGCN_GATE_NODE) && l == 0 && g < rows)
+                static_cast<float *>(a.dgate)[row0 + g] = sums[2];
             if (a.dB) {
+                const __amdgpu_buffer_rsrc_t w = row_window<G>(a.dB, first, elems);
 #pragma unroll
-                for (int q = 0; q < Q; ++q) store_quad<G>(a.dB, r0 + 4 * (l + q * TPR), at[q].count, v[q]);
+                for (int q = 0; q < Q; ++q) store_row_quad<G, TINY>(w, at[q], v[q], odd, a.streaming);
             }
         }
+        if constexpr (kAhead) in = next;
     }
 
     // this workgroup's column sums: over its groups in order, then one row of partials a slot
@@ -427,7 +478,8 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_backward_kernel(
         const int64_t p0 = (static_cast<int64_t>(blockIdx.x) * wanted + k++) * F;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            row_f32x4 sum = acc[s][q];
+            row_f32x4 sum = acc_gate[q];
+            if (s < 4) sum = kHold ? acc[kHold ? s & 3 : 0][q] : kept[place(s & 3, q)];
             if constexpr (kGroups > 1) {
                 __syncthreads();
                 join[threadIdx.x] = sum;
@@ -441,9 +493,9 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_backward_kernel(
     }
 }
 
-// out[slot][c] = the sum over workgroups of the partial sums of column c: eight threads sum
-// consecutive eighths in order, in float64, and the eighths are added in order.
-constexpr int kSumSegs = 8;
+// out[slot][c] = the sum over workgroups of the partial sums of column c: 32 threads sum
+// consecutive parts in order, in float64, and the parts are added in order.
+constexpr int kSumSegs = 32;
 constexpr int kSumCols = kThreads / kSumSegs;
 struct SumOut {
     float *to[kSlots];               // the wanted slots, in order
@@ -481,73 +533,114 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(const float *__r
 
 // ------------------------------------------------------------------ dispatch
 
-// Rows a workgroup works on at a time (the groups of launch_norm_* for this width).
-int rows_per_step(int32_t F) {
-    return F < 4 ? kThreads : F <= 32 ? kThreads / 8 : F <= 64 ? kThreads / 16 : F <= 128 ? kThreads / 32
-                                                     : F <= 512 ? kThreads / 64 : 1;
+// f(threads of a row, quads of each) for rows of F.  Few threads with two or three quads each
+// work on more rows at a time than many with one (a wavefront's lifetime is mostly latency), and
+// the fewer places a row leaves empty the better; past that the registers bound the quads.
+// Forward of 2^27 elements, us, float32 / bfloat16 (floor 324 / 185): F = 192 (16, 3) 320 / 204, (64, 1)
+// 379 / 318; F = 300 (32, 3) 388 / 268, (128, 1) 411 / 402; F = 3,000 (256, 3) 343 / 215, (1024, 1) 498 / 489;
+// 65 to 128 features by the rows' lines: F = 96 (16, 2) 335 / 246, (32, 1) 382 / 319; F = 100 445 / 285, 373 / 304.
+template <int T, int Q, class Fn>
+void shape(Fn f) { f(std::integral_constant<int, T>(), std::integral_constant<int, Q>()); }
+
+template <class Fn>
+void with_forward_shape(int32_t F, Fn f) {
+    if (F < 4) shape<1, 1>(f);
+    else if (F <= 32) shape<8, 1>(f);
+    else if (F <= 64) shape<16, 1>(f);
+    else if (F <= 128 && F % 32) shape<32, 1>(f);
+    else if (F <= 128) shape<16, 2>(f);
+    else if (F <= 192) shape<16, 3>(f);
+    else if (F <= 256) shape<32, 2>(f);
+    else if (F <= 384) shape<32, 3>(f);
+    else if (F <= 512) shape<64, 2>(f);
+    else if (F <= 768) shape<64, 3>(f);
+    else if (F <= 1024) shape<128, 2>(f);
+    else if (F <= 1536) shape<128, 3>(f);
+    else if (F <= 2048) shape<256, 2>(f);
+    else if (F <= 3072) shape<256, 3>(f);
+    else if (F <= 4096) shape<512, 2>(f);
+    else if (F <= 6144) shape<512, 3>(f);
+    else shape<512, 4>(f);
 }
 
-int backward_blocks(int32_t n, int32_t F) {
-    const int64_t need = (static_cast<int64_t>(n) + rows_per_step(F) - 1) / rows_per_step(F);
-    return static_cast<int>(std::min<int64_t>(need, kMaxBlocks));
+// The backward pass has about twice the registers a quad.  2^26 elements, us, float32 / bfloat16 (floor
+// 278 / 139): F = 256 (64, 1) 285 / 163, (32, 2) 305 / 165; F = 600 (64, 3) 339 / 240, (256, 1) 340 / 307;
+// F = 3,000 (256, 3) 335 / 229, (1024, 1) 418 / 330.
+template <class Fn>
+void with_backward_shape(int32_t F, Fn f) {
+    if (F < 4) shape<1, 1>(f);
+    else if (F <= 32) shape<8, 1>(f);
+    else if (F <= 64) shape<16, 1>(f);
+    else if (F <= 128) shape<32, 1>(f);
+    else if (F <= 256) shape<64, 1>(f);
+    else if (F <= 384) shape<32, 3>(f);
+    else if (F <= 512) shape<64, 2>(f);
+    else if (F <= 768) shape<64, 3>(f);
+    else if (F <= 1024) shape<256, 1>(f);
+    else if (F <= 2048) shape<256, 2>(f);
+    else if (F <= 3072) shape<256, 3>(f);
+    else if (F <= 4096) shape<1024, 1>(f);
+    else if (F <= 6144) shape<512, 3>(f);
+    else shape<512, 4>(f);
 }
 
-template <int TPR, int Q>
-void launch_forward(const ForwardArgs &a, bool act, bool stream, hipStream_t s) {
-    const int64_t need = (static_cast<int64_t>(a.n) + Shape<TPR, Q>::kGroups - 1) / Shape<TPR, Q>::kGroups;
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(need, static_cast<int64_t>(device_cus()) * 8)));
-    const dim3 block(Shape<TPR, Q>::kBlock);
-    if (act && stream) hipLaunchKernelGGL((norm_residual_kernel<TPR, Q, true, true>), grid, block, 0, s, a);
-    else if (act) hipLaunchKernelGGL((norm_residual_kernel<TPR, Q, true, false>), grid, block, 0, s, a);
-    else if (stream) hipLaunchKernelGGL((norm_residual_kernel<TPR, Q, false, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((norm_residual_kernel<TPR, Q, false, false>), grid, block, 0, s, a);
+// f of up to four truth values as compile-time constants.
+template <class Fn>
+void with_flags(Fn f) { f(); }
+template <class Fn, class... More>
+void with_flags(Fn f, bool b, More... more) {
+    if (b) with_flags([&](auto... rest) { f(std::true_type(), rest...); }, more...);
+    else with_flags([&](auto... rest) { f(std::false_type(), rest...); }, more...);
 }
 
-template <int TPR, int Q, bool A, bool S>
-void launch_backward_g(const BackwardArgs &a, bool grad, dim3 grid, hipStream_t s) {
-    const dim3 block(Shape<TPR, Q>::kBlock);
-    if (grad) hipLaunchKernelGGL((norm_backward_kernel<TPR, Q, A, S, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((norm_backward_kernel<TPR, Q, A, S, false>), grid, block, 0, s, a);
+// Workgroups of a backward pass, each with a partial sum of every column.  Its wavefronts have two
+// rows in flight each, so two workgroups a CU fill the memory's queues with float32 operands
+// (F = 128, us at 2, 3, 4 a CU: 287 / 299 / 316), and four where every operand is bfloat16 (226 / 179 / 159).
+int backward_blocks(int32_t n, int32_t F, bool all_bf16) {
+    int groups = 1, per_cu = 1;
+    with_backward_shape(F, [&](auto tpr, auto quads) {
+        constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
+        groups = Shape<T, Q>::kGroups;
+        per_cu = T > 256 ? 1 : all_bf16 ? 5 - Q : 2;
+    });
+    const int64_t need = (static_cast<int64_t>(n) + groups - 1) / groups;
+    return static_cast<int>(std::min<int64_t>(need, std::min(kMaxBlocks, per_cu * device_cus())));
 }
 
-template <int TPR, int Q>
-void launch_backward(const BackwardArgs &a, bool act, bool stream, bool grad, int blocks, hipStream_t s) {
-    const dim3 grid(static_cast<unsigned>(blocks));
-    if (act && stream) launch_backward_g<TPR, Q, true, true>(a, grad, grid, s);
-    else if (act) launch_backward_g<TPR, Q, true, false>(a, grad, grid, s);
-    else if (stream) launch_backward_g<TPR, Q, false, true>(a, grad, grid, s);
-    else launch_backward_g<TPR, Q, false, false>(a, grad, grid, s);
-}
+// Outputs the L2s (8 x 4 MiB) would not keep for the next launch are stored past them.
+bool past_l2(int64_t elems) { return elems * 4 > int64_t{32} << 20; }
 
 }  // namespace
 
 int launch_norm_residual(const dualgcn_norm &p, const void *R, const void *B, void *Rn, void *Z, int32_t n,
                          int32_t F, hipStream_t s) {
     const ForwardArgs a{R, B, p.gate, Rn, Z, p.post_weight, p.post_bias, p.pre_weight, p.pre_bias, n, F,
-                        p.eps, p.scale, p.flags};
-    const bool act = p.flags & DUALGCN_IN_BF16, stream = p.flags & DUALGCN_STREAM_BF16;
-    if (F < 4) launch_forward<1, 1>(a, act, stream, s);
-    else if (F <= 32) launch_forward<8, 1>(a, act, stream, s);
-    else if (F <= 64) launch_forward<16, 1>(a, act, stream, s);
-    else if (F <= 128) launch_forward<32, 1>(a, act, stream, s);
-    else if (F <= 256) launch_forward<64, 1>(a, act, stream, s);
-    else if (F <= 512) launch_forward<64, 2>(a, act, stream, s);
-    else if (F <= 1024) launch_forward<256, 1>(a, act, stream, s);
-    else if (F <= 2048) launch_forward<256, 2>(a, act, stream, s);
-    else if (F <= 4096) launch_forward<512, 2>(a, act, stream, s);
-    else launch_forward<1024, 2>(a, act, stream, s);
+                        p.eps, p.scale, p.flags, past_l2(static_cast<int64_t>(n) * F)};
+    with_forward_shape(F, [&](auto tpr, auto quads) {
+        constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
+        const int64_t need = (static_cast<int64_t>(n) + Shape<T, Q>::kGroups - 1) / Shape<T, Q>::kGroups;
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(need, kMaxForwardBlocks)));
+        with_flags([&](auto layer, auto act, auto stream) {
+            hipLaunchKernelGGL((norm_residual_kernel<T, Q, decltype(layer)::value, decltype(act)::value, decltype(stream)::value>),
+                               grid, dim3(Shape<T, Q>::kBlock), 0, s, a);
+        }, (p.flags & DUALGCN_NORM_LAYER) != 0, (p.flags & DUALGCN_IN_BF16) != 0, (p.flags & DUALGCN_STREAM_BF16) != 0);
+    });
     return hip_status(hipGetLastError());
 }
 
 size_t norm_backward_workspace_bytes(int32_t n, int32_t F) {
-    return static_cast<size_t>(backward_blocks(n, F)) * kSlots * F * sizeof(float);
+    int groups = 1;
+    with_backward_shape(F, [&](auto tpr, auto quads) { groups = Shape<decltype(tpr)::value, decltype(quads)::value>::kGroups; });
+    const int64_t need = (static_cast<int64_t>(n) + groups - 1) / groups;
+    return static_cast<size_t>(std::min<int64_t>(need, kMaxBlocks)) * kSlots * F * sizeof(float);
 }
 
 int launch_norm_backward(const dualgcn_norm &p, const void *Rn, const void *B, const void *dZ, const void *dRn,
                          void *dR, void *dB, const dualgcn_norm_grads &g, int32_t n, int32_t F, void *workspace,
                          hipStream_t s) {
     BackwardArgs a{Rn, B, p.gate, dZ, dRn, dR, dB, g.gate, p.post_weight, p.post_bias, p.pre_weight,
-                   static_cast<float *>(workspace), n, F, p.eps, p.scale, p.flags, 0u};
+                   static_cast<float *>(workspace), n, F, p.eps, p.scale, p.flags, 0u,
+                   past_l2(static_cast<int64_t>(n) * F)};
     SumOut out{};
     int wanted = 0;
     float *const to[kSlots] = {g.post_weight, g.post_bias, g.pre_weight, g.pre_bias,
@@ -557,20 +650,24 @@ int launch_norm_backward(const dualgcn_norm &p, const void *Rn, const void *B, c
             a.want |= 1u << k;
             out.to[wanted++] = to[k];
         }
-    const bool act = p.flags & DUALGCN_IN_BF16, stream = p.flags & DUALGCN_STREAM_BF16;
-    const bool grad = p.flags & DUALGCN_GRAD_BF16;
-    const int blocks = backward_blocks(n, F);
-    if (F < 4) launch_backward<1, 1>(a, act, stream, grad, blocks, s);
-    else if (F <= 32) launch_backward<8, 1>(a, act, stream, grad, blocks, s);
-    else if (F <= 64) launch_backward<16, 1>(a, act, stream, grad, blocks, s);
-    else if (F <= 128) launch_backward<32, 1>(a, act, stream, grad, blocks, s);
-    else if (F <= 256) launch_backward<64, 1>(a, act, stream, grad, blocks, s);
-    else if (F <= 512) launch_backward<64, 2>(a, act, stream, grad, blocks, s);
-    else if (F <= 1024) launch_backward<256, 1>(a, act, stream, grad, blocks, s);
-    else if (F <= 2048) launch_backward<256, 2>(a, act, stream, grad, blocks, s);
-    else if (F <= 4096) launch_backward<512, 2>(a, act, stream, grad, blocks, s);
-    else launch_backward<1024, 2>(a, act, stream, grad, blocks, s);
-    const int st = hip_status(hipGetLastError());
+    const int blocks = backward_blocks(
+        n, F, (~p.flags & (DUALGCN_IN_BF16 | DUALGCN_STREAM_BF16 | DUALGCN_GRAD_BF16)) == 0);
+    int st = DUALGCN_OK;
+    with_backward_shape(F, [&](auto tpr, auto quads) {
+        constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
+        const size_t lds = Q > 1 ? sizeof(row_f32x4) * Q * Shape<T, Q>::kBlock * __builtin_popcount(a.want & 15u) : 0;
+        with_flags([&](auto layer, auto act, auto stream, auto grad) {
+            const auto kernel = &norm_backward_kernel<T, Q, decltype(layer)::value, decltype(act)::value,
+                                                      decltype(stream)::value, decltype(grad)::value>;
+            if (lds > 48 * 1024 && (st = hip_status(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                                         hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                                         static_cast<int>(lds)))))
+                return;
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(Shape<T, Q>::kBlock), lds, s, a);
+        }, (p.flags & DUALGCN_NORM_LAYER) != 0, (p.flags & DUALGCN_IN_BF16) != 0, (p.flags & DUALGCN_STREAM_BF16) != 0,
+           (p.flags & DUALGCN_GRAD_BF16) != 0);
+    });
+    if (!st) st = hip_status(hipGetLastError());
     if (st || !wanted) return st;
     hipLaunchKernelGGL(norm_columns_kernel, dim3((F + kSumCols - 1) / kSumCols, wanted), dim3(kThreads), 0, s,
                        a.partial, blocks, wanted, F, out);

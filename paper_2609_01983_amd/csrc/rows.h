@@ -20,57 +20,99 @@ __device__ __forceinline__ float bf16_to_float(unsigned short b) {
     return __uint_as_float(static_cast<uint32_t>(b) << 16);
 }
 
-// A lane's four consecutive columns of a row of F: `col` the first, `at` where they are read
-// (the row's last four where the row ends inside them, so that every load is whole and none is
-// under a condition: the compiler then keeps all loads of a row in flight), `shift` by how many
-// columns that is early, `count` how many of the four the row has (<= 0: none).
+// Consecutive rows as a buffer: accesses past its end read zeros and write nothing, so rows behind
+// the last and lanes without a column need no branch and no clamped address, and lanes address
+// it with 32 bits.
+template <bool BF>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_window(const void *base, int64_t first, int64_t elems) {
+    constexpr int kSize = BF ? 2 : 4;
+    return __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(const_cast<void *>(base)) + first * kSize, 0,
+                                             static_cast<int>(elems * kSize), 0x00020000);
+}
+
+constexpr uint32_t kNoQuad = 0x3FFFFFFFu;            // an element offset past every window
+constexpr int kNonTemporal = 2;                      // a buffer access's hint
+
+// A lane's four consecutive columns of a row of F that starts at element `row_at` of its window.
+// A row that ends inside them is read from its last four on (so that every load is whole) and
+// shifted; `part` is how many columns it then has, 0 elsewhere.
 struct QuadPlace {
-    int at, shift, count;
-    __device__ __forceinline__ void set(int col, int F) {
-        at = F < 4 ? 0 : (col < F - 4 ? col : F - 4);
-        shift = col - at;
-        count = F - col;
+    uint32_t at, col;                // element offsets in the window and in the row, or kNoQuad
+    int part, count;                 // count: columns of the row from the lane's first on (<= 0: none)
+    __device__ __forceinline__ void set(uint32_t row_at, int first, int F) {
+        count = F - first;
+        part = count > 0 && count < 4 ? count : 0;
+        const int c = part ? (F < 4 ? 0 : F - 4) : first;
+        at = count > 0 ? row_at + c : kNoQuad;
+        col = count > 0 ? c : kNoQuad;
     }
 };
 
-// Four elements as stored, and as float32.  TINY: rows of fewer than four elements.
+// Four elements as stored, and as float32.  TINY: rows of fewer than four elements.  odd: F is no
+// multiple of four (the same for every lane).
 template <bool BF, bool TINY>
 struct RawRowQuad {
     typename std::conditional<BF, row_u16x4, row_f32x4>::type v;
 
-    __device__ __forceinline__ void load(const void *base, int64_t row_at, const QuadPlace &q) {
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t w, uint32_t at, int count) {
         if constexpr (TINY) {
 #pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                v[i] = 0;
-                if (i < q.count) {
-                    if constexpr (BF) v[i] = static_cast<const unsigned short *>(base)[row_at + i];
-                    else v[i] = static_cast<const float *>(base)[row_at + i];
-                }
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t e = i < count ? at + i : kNoQuad;
+                if constexpr (BF) v[i] = __builtin_amdgcn_raw_buffer_load_b16(w, e * 2, 0, 0);
+                else v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(w, e * 4, 0, 0));
             }
-            v[3] = 0;
         } else if constexpr (BF) {
-            v = *reinterpret_cast<const row_u16x4_any *>(static_cast<const unsigned short *>(base) + row_at + q.at);
+            v = __builtin_bit_cast(row_u16x4, __builtin_amdgcn_raw_buffer_load_b64(w, at * 2, 0, 0));
         } else {
-            v = *reinterpret_cast<const row_f32x4_any *>(static_cast<const float *>(base) + row_at + q.at);
+            v = __builtin_bit_cast(row_f32x4, __builtin_amdgcn_raw_buffer_load_b128(w, at * 4, 0, 0));
         }
     }
-    // ragged: the row has fewer columns than its lanes have places (the same for every lane)
-    __device__ __forceinline__ row_f32x4 get(const QuadPlace &q, bool ragged) const {
+    __device__ __forceinline__ row_f32x4 get(const QuadPlace &q, bool odd) const {
         row_f32x4 f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (BF) f[i] = bf16_to_float(v[i]);
             else f[i] = v[i];
         }
-        if (!TINY && ragged) {
-            if (q.shift & 1) f = row_f32x4{f[1], f[2], f[3], 0.f};
-            if (q.shift & 2) f = row_f32x4{f[2], f[3], 0.f, 0.f};
-            if (q.shift >= 4) f = row_f32x4{0.f, 0.f, 0.f, 0.f};
+        if (!TINY && odd) {
+            if (q.part == 3) f = row_f32x4{f[1], f[2], f[3], 0.f};
+            if (q.part == 2) f = row_f32x4{f[2], f[3], 0.f, 0.f};
+            if (q.part == 1) f = row_f32x4{f[3], 0.f, 0.f, 0.f};
         }
         return f;
     }
 };
+
+// A lane's four values to its place in the window, bfloat16 rounded to nearest even.  stream: with a
+// non-temporal hint, for outputs that the caches would not keep.
+template <bool BF, bool TINY>
+__device__ __forceinline__ void store_row_quad(__amdgpu_buffer_rsrc_t w, const QuadPlace &q, row_f32x4 v, bool odd,
+                                               bool stream) {
+    const row_u16x4 h = __builtin_bit_cast(row_u16x4, __builtin_convertvector(v, row_bf16x4));
+    if constexpr (!TINY) {
+        const uint32_t at = odd && q.part ? kNoQuad : q.at;
+        if constexpr (BF) {
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            if (stream) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, h), w, at * 2, 0, kNonTemporal);
+            else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, h), w, at * 2, 0, 0);
+        } else {
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            if (stream) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), w, at * 4, 0, kNonTemporal);
+            else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), w, at * 4, 0, 0);
+        }
+    }
+    if (TINY || (odd && q.part)) {
+        const uint32_t at = TINY ? q.at : q.at + 4 - q.part;     // the lane's own first column
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            if (i < q.part) {
+                if constexpr (BF) __builtin_amdgcn_raw_buffer_store_b16(h[i], w, (at + i) * 2, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[i]), w, (at + i) * 4, 0, 0);
+            }
+        }
+    }
+}
 
 // Elements [at, at + count) of an array as float32, zeros from `count` on (count <= 0: nothing is
 // read); for places with no row of at least four elements around them.
