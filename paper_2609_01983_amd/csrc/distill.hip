@@ -70,8 +70,9 @@ struct Entries {
     int64_t at;
     int K, C, l;
     int id[kHeld];
-    float t[kHeld];                  // the logit; -inf: none
+    float t[kHeld];                  // the logit, -inf: none; its exponential from local_sum on, 0: none
     float m, inv;                    // largest logit; 1 / sum of the exponentials
+    float entropy;                   // this thread's share of sum p log2(p sum)
     bool taught;
 
     __device__ __forceinline__ void fetch(int64_t k, int &i, float &x) const {
@@ -93,10 +94,9 @@ struct Entries {
             if (l + h * TPR < K) fetch(l + h * TPR, id[h], t[h]);
         }
     }
+    // f of the entries that are not held: their classes and logits
     template <class F>
-    __device__ __forceinline__ void each(F f) const {
-#pragma unroll
-        for (int h = 0; h < kHeld; ++h) f(id[h], t[h]);
+    __device__ __forceinline__ void others(F f) const {
         for (int k = l + kHeld * TPR; k < K; k += TPR) {
             int i;
             float x;
@@ -104,49 +104,64 @@ struct Entries {
             f(i, x);
         }
     }
-    __device__ __forceinline__ float p(float x, float a) const { return exp2_fast((x - m) * a) * inv; }
-
-    // The row's largest logit and the sum of its exponentials; `entropy` receives sum p log2 p.
-    __device__ __forceinline__ void prepare(float a, float *sh, int &turn, float &entropy) {
-        float top[2] = {-INFINITY, 0.f};                 // second: does an entry count? (NaN does)
-        each([&](int, float x) {
-            top[0] = fmaxf(top[0], x);
-            if (!(x == -INFINITY)) top[1] = 1.f;
-        });
-        row_reduce<TPR>(top, MaxOp(), sh, turn);
-        m = top[0];
-        taught = top[1] > 0.f;
-        entropy = 0.f;
-        inv = 0.f;
-        if (!taught) return;                             // the same for all threads of the row
-        float s[2] = {0.f, 0.f};
-        each([&](int, float x) {
-            if (!(x == -INFINITY)) {
-                const float z = (x - m) * a, e = exp2_fast(z);
-                s[0] += e;
-                if (!(e == 0.f)) s[1] = fmaf(e, z, s[1]);
-            }
-        });
-        row_reduce<TPR>(s, AddOp(), sh, turn);
-        inv = 1.f / s[0];
-        entropy = s[1] * inv - __builtin_amdgcn_logf(s[0]);
+    // f of the classes and exponentials (0: none) of all entries, after local_sum
+    template <class F>
+    __device__ __forceinline__ void each(float a, F f) const {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) f(id[h], t[h]);
+        others([&](int i, float x) { f(i, exponential(x, a)); });
+    }
+    __device__ __forceinline__ float exponential(float x, float a) const {
+        return x == -INFINITY ? 0.f : exp2_fast((x - m) * a);
     }
 
-    // P of the classes [c0, c1) into tile[id - c0] (zeros before); clear() undoes it.
+    // The row's largest logit and the sum of its exponentials, in two steps around the reductions that
+    // the row's own logits need too: v[0] and v[1] join `max`, v[0] joins `sum`.
+    __device__ __forceinline__ void local_max(float *v) const {
+        v[0] = -INFINITY;
+        v[1] = 0.f;                                      // does an entry count? (NaN does)
+        auto one = [&](int, float x) {
+            v[0] = fmaxf(v[0], x);
+            if (!(x == -INFINITY)) v[1] = 1.f;
+        };
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) one(id[h], t[h]);
+        others(one);
+    }
+    __device__ __forceinline__ void local_sum(const float *max, float a, float *v) {
+        m = max[0];
+        taught = max[1] > 0.f;
+        v[0] = 0.f;
+        entropy = 0.f;
+        auto one = [&](float x) {
+            const float e = exponential(x, a);
+            v[0] += e;
+            entropy = fmaf(e, e == 0.f ? 0.f : (x - m) * a, entropy);    // no 0 * infinity
+            return e;
+        };
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) t[h] = one(t[h]);
+        others([&](int, float x) { one(x); });
+    }
+    __device__ __forceinline__ void have(float sum) {
+        inv = __builtin_amdgcn_rcpf(sum);
+        entropy *= inv;
+    }
+
+    // P of the classes [c0, c1) into tile[id - c0] (zeros before); clear() undoes it.  have() first.
     __device__ __forceinline__ void scatter(float *tile, int c0, int c1, float a, int *flag) const {
         bool twice = false;
-        each([&](int i, float x) {
-            if (!(x == -INFINITY) && i >= c0 && i < c1) {
-                const float v = p(x, a);
-                if (!(v == 0.f))
-                    twice |= __hip_atomic_exchange(tile + (i - c0), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) != 0.f;
-            }
+        each(a, [&](int i, float e) {
+            const float v = e * inv;
+            if (!(v == 0.f) && static_cast<uint32_t>(i - c0) < static_cast<uint32_t>(c1 - c0))
+                twice |= __hip_atomic_exchange(tile + (i - c0), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) != 0.f;
         });
         if constexpr (TPR > 64) {
+            // the flag is set again only after the next row's reductions, which all threads reach
+            // after they have read it here
             if (twice) *flag = 1;
             __syncthreads();
             twice = *flag != 0;
-            __syncthreads();
         } else {
             row_sync<TPR>();
             const uint64_t all = __ballot(twice);
@@ -154,26 +169,31 @@ struct Entries {
             twice = (TPR == 64 ? all : all >> first & ((uint64_t{1} << (TPR & 63)) - 1)) != 0;
         }
         if (twice) {                                     // the same for all threads of the row
-            clear(tile, c0, c1);
+            clear(tile, c0, c1, a);
             row_sync<TPR>();
             if (l == 0) {
                 for (int k = 0; k < K; ++k) {
                     int i;
                     float x;
                     fetch(k, i, x);
-                    if (!(x == -INFINITY) && i >= c0 && i < c1) tile[i - c0] += p(x, a);
+                    if (i >= c0 && i < c1) tile[i - c0] += exponential(x, a) * inv;
                 }
                 if constexpr (TPR > 64) *flag = 0;
             }
+            row_sync<TPR>();
         }
-        row_sync<TPR>();
     }
-    __device__ __forceinline__ void clear(float *tile, int c0, int c1) const {
-        each([&](int i, float x) {
-            if (!(x == -INFINITY) && i >= c0 && i < c1) tile[i - c0] = 0.f;
+    __device__ __forceinline__ void clear(float *tile, int c0, int c1, float a) const {
+        each(a, [&](int i, float e) {
+            if (!(e == 0.f) && static_cast<uint32_t>(i - c0) < static_cast<uint32_t>(c1 - c0)) tile[i - c0] = 0.f;
         });
     }
 };
+
+// Has a quad of P anything?  (P is never negative, and a NaN's bits are not zero.)
+__device__ __forceinline__ bool some(row_f32x4 P) {
+    return (__float_as_uint(P[0]) | __float_as_uint(P[1]) | __float_as_uint(P[2]) | __float_as_uint(P[3])) != 0;
+}
 
 // A thread's sums of the loss over its rows, joined over the workgroup in a fixed order.
 template <int BLOCK>
@@ -233,91 +253,89 @@ __global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_rows_kern
         en.load(a, row, l);
         const int lab = a.labels && row < a.n ? a.labels[row] : -1;
         const bool labeled = lab >= 0 && lab < C;
-        float entropy;
-        en.prepare(a.temp_a, sh, turn, entropy);
-        row_f32x4 o[Q];
-        if (!en.taught && !labeled) {                    // zeros, whatever the logits
+        float top[3];
+        en.local_max(top);
+        top[2] = -FLT_MAX;                               // all of the row -inf: the sums are 0, G NaN
+        row_f32x4 y[Q], o[Q], e1[Q];
 #pragma unroll
-            for (int q = 0; q < Q; ++q) o[q] = row_f32x4{0.f, 0.f, 0.f, 0.f};
-        } else {
-            row_f32x4 y[Q];
-            float m[1] = {-FLT_MAX};                     // all of the row -inf: the sums are 0, G NaN
+        for (int q = 0; q < Q; ++q) {
+            y[q] = raw[q].get(at[q], odd);
+            if (ragged)
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                y[q] = raw[q].get(at[q], odd);
-                if (ragged)
+                for (int i = 0; i < 4; ++i)
+                    if (i >= at[q].count) y[q][i] = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (i >= at[q].count) y[q][i] = -INFINITY;
+            for (int i = 0; i < 4; ++i) top[2] = fmaxf(top[2], y[q][i]);
+        }
+        row_reduce<TPR>(top, MaxOp(), sh, turn);
+        float s[3];                                      // the entries', at T, at 1
+        en.local_sum(top, a.temp_a, s);
+        s[1] = s[2] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) m[0] = fmaxf(m[0], y[q][i]);
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[q][i] -= top[2];
+                o[q][i] = exp2_fast(y[q][i] * a.temp_a);
+                s[1] += o[q][i];
             }
-            row_reduce<TPR>(m, MaxOp(), sh, turn);
-            row_f32x4 e1[Q];
-            float s[3] = {0.f, 0.f, 0.f};                // at T, at 1, the label's y - m
+        if (labeled && !same)
 #pragma unroll
             for (int q = 0; q < Q; ++q)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    y[q][i] -= m[0];
-                    o[q][i] = exp2_fast(y[q][i] * a.temp_a);
-                    s[0] += o[q][i];
+                    e1[q][i] = exp2_fast(y[q][i] * kLog2e);
+                    s[2] += e1[q][i];
                 }
-            if (labeled) {
-                if (!same)
+        row_reduce<TPR>(s, AddOp(), sh, turn);
+        if (same) s[2] = s[1];
+        const float ct = en.taught ? a.soft : 0.f;
+        // at T = 1 the label's share of the softmax joins the teacher's
+        const float it = (same && labeled ? ct + a.hard : ct) * __builtin_amdgcn_rcpf(s[1]);
 #pragma unroll
-                    for (int q = 0; q < Q; ++q)
+        for (int q = 0; q < Q; ++q) o[q] *= it;
+        float loss_s = 0.f, loss_h = 0.f;                // this thread's share, in powers of two
+        if (labeled) {
+            const float i1 = a.hard * __builtin_amdgcn_rcpf(s[2]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            e1[q][i] = exp2_fast(y[q][i] * kLog2e);
-                            s[1] += e1[q][i];
-                        }
+            for (int q = 0; q < Q; ++q) {
+                if (!same) o[q] += e1[q] * i1;
 #pragma unroll
-                for (int q = 0; q < Q; ++q)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (4 * (l + q * TPR) + i == lab) s[2] = y[q][i];
+                for (int i = 0; i < 4; ++i)
+                    if (4 * (l + q * TPR) + i == lab) {
+                        o[q][i] -= a.hard;
+                        loss_h = y[q][i];
+                    }
             }
-            row_reduce<TPR>(s, AddOp(), sh, turn);
-            if (en.taught) en.scatter(tile, 0, C, a.temp_a, &flag);
-            if (same) s[1] = s[0];
-            const float ct = en.taught ? a.soft : 0.f;
-            // at T = 1 the label's share of the softmax joins the teacher's
-            const float it = ct / s[0] + (same && labeled ? a.hard / s[0] : 0.f);
-            float cross[1] = {0.f};
+        }
+        if (en.taught) {
+            en.have(s[0]);
+            en.scatter(tile, 0, C, a.temp_a, &flag);
 #pragma unroll
-            for (int q = 0; q < Q; ++q) o[q] *= it;
-            if (labeled) {
-                const float i1 = a.hard / s[1];
-#pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    if (!same) o[q] += e1[q] * i1;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (4 * (l + q * TPR) + i == lab) o[q][i] -= a.hard;
-                }
-            }
-            if (en.taught) {
-#pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    const row_f32x4 P = tiles[g][l + q * TPR];
+            for (int q = 0; q < Q; ++q) {
+                const row_f32x4 P = tiles[g][l + q * TPR];
+                if (some(P)) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         // no 0 * infinity where the class has no P
-                        cross[0] = fmaf(P[i], P[i] == 0.f ? 0.f : y[q][i], cross[0]);
+                        loss_s = fmaf(P[i], P[i] == 0.f ? 0.f : y[q][i], loss_s);
                         o[q][i] = fmaf(-ct, P[i], o[q][i]);
                     }
                 }
-                row_reduce<TPR>(cross, AddOp(), sh, turn);
-                if constexpr (TPR <= 64) row_sync<TPR>();    // P is read before it is cleared
-                en.clear(tile, 0, C);
-                row_sync<TPR>();
             }
-            if (l == 0) {
-                if (en.taught) soft += entropy - static_cast<double>(a.temp_a) * cross[0] + __builtin_amdgcn_logf(s[0]);
-                if (labeled) hard += __builtin_amdgcn_logf(s[1]) - static_cast<double>(kLog2e) * s[2];
-            }
+            row_sync<TPR>();                             // P is read before it is cleared
+            en.clear(tile, 0, C, a.temp_a);
+            if constexpr (TPR <= 64) row_sync<TPR>();    // else the next row's reductions come between
+            soft += en.entropy - static_cast<double>(a.temp_a) * loss_s;
+            if (l == 0) soft += __builtin_amdgcn_logf(s[1]) - __builtin_amdgcn_logf(s[0]);
         }
+        if (labeled) {
+            hard -= static_cast<double>(kLog2e) * loss_h;
+            if (l == 0) hard += __builtin_amdgcn_logf(s[2]);
+        }
+        if (!en.taught && !labeled)                      // zeros, whatever the logits
+#pragma unroll
+            for (int q = 0; q < Q; ++q) o[q] = row_f32x4{0.f, 0.f, 0.f, 0.f};
         if (a.g_bf16) {
             const __amdgpu_buffer_rsrc_t w = row_window<true>(a.G, row0 * C, elems);
 #pragma unroll
@@ -333,146 +351,259 @@ __global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_rows_kern
 
 // ------------------------------------------------------------------ long rows
 //
-// A row that the registers do not hold is swept twice: a running maximum and sums, then the
-// gradient, piece by piece of kPiece classes (their P in LDS).  A workgroup takes a row; where
-// there are few rows, `splits` workgroups share each: a first launch leaves their maxima and sums
-// in `stats`, the second joins them.
-constexpr int kLong = 512;                           // threads
-constexpr int kLongQ = 8;                            // quads a thread and piece
-constexpr int kPiece = 4 * kLong * kLongQ;           // 16,384 classes, 64 KiB of P
+// A workgroup takes a row, and its P is scattered to LDS piece by piece.  Up to 32,768 logits stay in
+// the workgroup's registers as they are stored, so that they are read once.  Longer rows are swept twice: a running
+// maximum and sums, then the gradient.  Where there are few rows, `splits` workgroups share each: a
+// first launch leaves their maxima and sums in `stats`, the second joins them.
+constexpr int kSweep = 512;                          // threads of a sweep
+constexpr int kSweepQ = 8;                           // quads a thread and piece
+constexpr int kHeldQ = 4;                            // the same where the row is held
 
 struct RowStats {
     float m, st, s1;
 };
 
 // Quad q of this thread in the piece at class c, none from class c1 on (a whole number of quads, or
-// the row's end).
-__device__ __forceinline__ void place(QuadPlace &at, int c, int q, int c1, int C) {
-    const int first = c + 4 * (static_cast<int>(threadIdx.x) + q * kLong);
-    at.set(0, first < c1 ? first : C, C);
+// the row's end).  Behind the row's end the window needs no compare.  ODD: C is no multiple of four.
+template <int THREADS, bool ODD>
+__device__ __forceinline__ QuadPlace place(int thread, int c, int q, int c1, int C) {
+    const int first = c + 4 * (thread + q * THREADS);
+    QuadPlace at;
+    if constexpr (ODD) {
+        at.set(0, first < c1 ? first : C, C);
+    } else {
+        at.count = c1 - first;
+        at.part = 0;
+        at.col = at.at = c1 == C || first < c1 ? first : kNoQuad;
+    }
+    return at;
 }
 
-// Classes [c0, c1) of a row: maximum and sums at T and at 1, over the workgroup.
-template <bool YBF>
+// A quad's logits as float32, -infinity behind the row's or split's end.
+template <bool YBF, bool ODD>
+__device__ __forceinline__ row_f32x4 logits(const RawRowQuad<YBF, false> &raw, const QuadPlace &at, bool cut) {
+    row_f32x4 y = raw.get(at, ODD);
+    if (cut)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i >= at.count) y[i] = -INFINITY;
+    return y;
+}
+
+// What the gradient of a row is made of.
+template <bool ODD>
+struct RowGrad {
+    float m, a, ct, ch, it, i1;      // i1: at T = 1 the label's share is in `it`
+    int lab;
+    bool labeled, two;               // two: a softmax of its own for the label
+    __device__ __forceinline__ RowGrad(const Args &args, const RowStats &s, bool taught, int lab_)
+        : m(s.m), a(args.temp_a), lab(lab_) {
+        labeled = lab >= 0 && lab < args.C;
+        two = labeled && a != kLog2e;
+        ct = taught ? args.soft : 0.f;
+        ch = labeled ? args.hard : 0.f;
+        it = (two ? ct : ct + ch) * __builtin_amdgcn_rcpf(s.st);
+        i1 = two ? ch * __builtin_amdgcn_rcpf(s.s1) : 0.f;
+    }
+    // one quad, stored; its share of the loss (sum of P (y - m), the label's y - m) is added
+    __device__ __forceinline__ void quad(const Args &args, int64_t row, const QuadPlace &at, row_f32x4 y, int col,
+                                         row_f32x4 P, float &cross, float &label) const {
+        row_f32x4 o;
+        y -= m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = exp2_fast(y[i] * a) * it;
+        if (two)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(exp2_fast(y[i] * kLog2e), i1, o[i]);
+        if (labeled && static_cast<uint32_t>(lab - col) < 4u && at.count > 0)    // places behind c1 are another split's
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i == lab) {
+                    o[i] -= ch;
+                    label += y[i];
+                }
+        if (some(P))
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                cross = fmaf(P[i], P[i] == 0.f ? 0.f : y[i], cross);
+                o[i] = fmaf(-ct, P[i], o[i]);
+            }
+        if (args.g_bf16)
+            store_row_quad<true, false>(row_window<true>(args.G, row * args.C, args.C), at, o, ODD, args.streaming);
+        else
+            store_row_quad<false, false>(row_window<false>(args.G, row * args.C, args.C), at, o, ODD, args.streaming);
+    }
+};
+
+// Zeros to the classes [c0, c1) of a row.
+template <int THREADS, bool ODD>
+__device__ __forceinline__ void put_zeros(const Args &a, int64_t row, int c0, int c1) {
+    const row_f32x4 z = {0.f, 0.f, 0.f, 0.f};
+    for (int c = c0; c < c1; c += 4 * THREADS) {
+        const QuadPlace at = place<THREADS, ODD>(threadIdx.x, c, 0, c1, a.C);
+        if (a.g_bf16) store_row_quad<true, false>(row_window<true>(a.G, row * a.C, a.C), at, z, ODD, a.streaming);
+        else store_row_quad<false, false>(row_window<false>(a.G, row * a.C, a.C), at, z, ODD, a.streaming);
+    }
+}
+
+// A value that the optimiser takes for a new one: what was computed from it before is not kept in
+// registers for its next use (a held row leaves none for its exponentials or places).
+template <class T>
+__device__ __forceinline__ T anew(T v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// A row that QUADS quads of THREADS threads hold.  The second bound keeps a CU's registers full.
+template <bool YBF, bool TBF, bool ODD, int THREADS, int QUADS>
+__global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(Args a) {
+    __shared__ float sh[row_reduce_floats<THREADS>()];
+    __shared__ row_f32x4 tiles[THREADS * kHeldQ];
+    __shared__ int flag;
+    int turn = 0;
+    const int C = a.C;
+    constexpr int kPiece = 4 * THREADS * kHeldQ;
+    float *tile = reinterpret_cast<float *>(tiles);
+#pragma unroll
+    for (int q = 0; q < kHeldQ; ++q) tiles[threadIdx.x + q * THREADS] = row_f32x4{0.f, 0.f, 0.f, 0.f};
+    if (threadIdx.x == 0) flag = 0;
+    __syncthreads();
+    double soft = 0.0, hard = 0.0;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const __amdgpu_buffer_rsrc_t wy = row_window<YBF>(a.Y, row * C, C);
+        RawRowQuad<YBF, false> raw[QUADS];
+        int thread = anew(static_cast<int>(threadIdx.x));
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q) {
+            const QuadPlace at = place<THREADS, ODD>(thread, 0, q, C, C);
+            raw[q].load(wy, at.at, at.count);
+        }
+        Entries<THREADS, TBF> en;
+        en.load(a, row, threadIdx.x);
+        const int lab = a.labels ? a.labels[row] : -1;
+        const bool labeled = lab >= 0 && lab < C, two = labeled && a.temp_a != kLog2e;
+        float top[3];
+        en.local_max(top);
+        top[2] = -FLT_MAX;
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q)
+            if (4 * q * THREADS < C) {                   // uniform
+                const row_f32x4 y = logits<YBF, ODD>(raw[q], place<THREADS, ODD>(thread, 0, q, C, C), 4 * (q + 1) * THREADS > C);
+                top[2] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), top[2]);
+            }
+        row_reduce<THREADS>(top, MaxOp(), sh, turn);
+        float s[3];
+        en.local_sum(top, a.temp_a, s);
+        s[1] = s[2] = 0.f;
+        thread = anew(thread);
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q)
+            if (4 * q * THREADS < C) {
+                raw[q].v = anew(raw[q].v);
+                row_f32x4 y = logits<YBF, ODD>(raw[q], place<THREADS, ODD>(thread, 0, q, C, C), 4 * (q + 1) * THREADS > C);
+                y -= top[2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[1] += exp2_fast(y[i] * a.temp_a);
+                if (two)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[2] += exp2_fast(y[i] * kLog2e);
+                if (q % 2) __builtin_amdgcn_sched_barrier(0);    // registers for two quads' work, not for all
+            }
+        row_reduce<THREADS>(s, AddOp(), sh, turn);
+        if (!en.taught && !labeled) {                    // zeros, whatever the logits
+            put_zeros<THREADS, ODD>(a, row, 0, C);
+            continue;
+        }
+        en.have(s[0]);
+        const RowGrad<ODD> grad(a, RowStats{top[2], s[1], s[2]}, en.taught, lab);
+        float cross = 0.f, label = 0.f;
+#pragma unroll
+        for (int q0 = 0; q0 < QUADS; q0 += kHeldQ) {
+            const int c = 4 * q0 * THREADS;
+            thread = anew(thread);
+            if (c < C) {
+                if (en.taught) en.scatter(tile, c, min(C, c + kPiece), a.temp_a, &flag);
+#pragma unroll
+                for (int q = q0; q < q0 + kHeldQ && q < QUADS; ++q)
+                    if (4 * q * THREADS < C) {
+                        raw[q].v = anew(raw[q].v);
+                        const QuadPlace at = place<THREADS, ODD>(thread, 0, q, C, C);
+                        grad.quad(a, row, at, raw[q].get(at, ODD), 4 * (thread + q * THREADS),
+                                  tiles[threadIdx.x + (q - q0) * THREADS], cross, label);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                if (en.taught) {
+                    __syncthreads();
+                    en.clear(tile, c, min(C, c + kPiece), a.temp_a);
+                    __syncthreads();
+                }
+            }
+        }
+        if (en.taught) {
+            soft += en.entropy - static_cast<double>(a.temp_a) * cross;
+            if (threadIdx.x == 0) soft += __builtin_amdgcn_logf(s[1]) - __builtin_amdgcn_logf(s[0]);
+        }
+        if (labeled) {
+            hard -= static_cast<double>(kLog2e) * label;
+            if (threadIdx.x == 0) hard += __builtin_amdgcn_logf(two ? s[2] : s[1]);
+        }
+    }
+    write_partial<THREADS>(soft, hard, a.partial + 2 * static_cast<int64_t>(blockIdx.x));
+}
+
+// Classes [c0, c1) of a row: maximum and sums at T and (one) at 1, over the workgroup.
+template <bool YBF, bool ODD>
 __device__ __forceinline__ RowStats sweep_stats(const Args &a, int64_t row, int c0, int c1, bool one, float *sh,
                                                 int &turn) {
+    constexpr int kPiece = 4 * kSweep * kSweepQ;
     float m = -FLT_MAX, st = 0.f, s1 = 0.f;
     const __amdgpu_buffer_rsrc_t w = row_window<YBF>(a.Y, row * a.C, a.C);
     for (int c = c0; c < c1; c += kPiece) {
-        RawRowQuad<YBF, false> raw[kLongQ];
-        QuadPlace at[kLongQ];
+        RawRowQuad<YBF, false> raw[kSweepQ];
 #pragma unroll
-        for (int q = 0; q < kLongQ; ++q) {
-            place(at[q], c, q, c1, a.C);
-            raw[q].load(w, at[q].at, at[q].count);
+        for (int q = 0; q < kSweepQ; ++q) {
+            const QuadPlace at = place<kSweep, ODD>(threadIdx.x, c, q, c1, a.C);
+            raw[q].load(w, at.at, at.count);
         }
-        row_f32x4 y[kLongQ];
+        row_f32x4 y[kSweepQ];
         float top = m;
 #pragma unroll
-        for (int q = 0; q < kLongQ; ++q) {
-            y[q] = raw[q].get(at[q], a.C & 3);
-            if (c + kPiece > c1)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i >= at[q].count) y[q][i] = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, y[q][i]);
+        for (int q = 0; q < kSweepQ; ++q) {
+            y[q] = logits<YBF, ODD>(raw[q], place<kSweep, ODD>(threadIdx.x, c, q, c1, a.C), c + kPiece > c1);
+            top = fmaxf(fmaxf(fmaxf(y[q][0], y[q][1]), fmaxf(y[q][2], y[q][3])), top);
         }
         st *= exp2_fast((m - top) * a.temp_a);
         s1 *= exp2_fast((m - top) * kLog2e);
         m = top;
 #pragma unroll
-        for (int q = 0; q < kLongQ; ++q)
+        for (int q = 0; q < kSweepQ; ++q)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st += exp2_fast((y[q][i] - m) * a.temp_a);
         if (one)
 #pragma unroll
-            for (int q = 0; q < kLongQ; ++q)
+            for (int q = 0; q < kSweepQ; ++q)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s1 += exp2_fast((y[q][i] - m) * kLog2e);
     }
     float all[1] = {m};
-    row_reduce<kLong>(all, MaxOp(), sh, turn);
+    row_reduce<kSweep>(all, MaxOp(), sh, turn);
     float s[2] = {st * exp2_fast((m - all[0]) * a.temp_a), s1 * exp2_fast((m - all[0]) * kLog2e)};
-    row_reduce<kLong>(s, AddOp(), sh, turn);
+    row_reduce<kSweep>(s, AddOp(), sh, turn);
     return RowStats{all[0], s[0], s[1]};
-}
-
-__device__ __forceinline__ void put(const Args &a, int64_t row, const QuadPlace &at, row_f32x4 o) {
-    const bool odd = a.C & 3;
-    if (a.g_bf16) store_row_quad<true, false>(row_window<true>(a.G, row * a.C, a.C), at, o, odd, a.streaming);
-    else store_row_quad<false, false>(row_window<false>(a.G, row * a.C, a.C), at, o, odd, a.streaming);
-}
-
-// The gradient of classes [c0, c1) and their part of the loss: sum of P (y - m), the
-// label's y - m (both on every thread).
-template <bool YBF, bool TBF>
-__device__ __forceinline__ float2 sweep_grad(const Args &a, int64_t row, int c0, int c1, const RowStats &s,
-                                             const Entries<kLong, TBF> &en, int lab, row_f32x4 *tile, int *flag, float *sh, int &turn) {
-    const __amdgpu_buffer_rsrc_t wy = row_window<YBF>(a.Y, row * a.C, a.C);
-    const bool odd = a.C & 3, labeled = lab >= 0 && lab < a.C, same = a.temp_a == kLog2e;
-    const float ct = en.taught ? a.soft : 0.f, ch = labeled ? a.hard : 0.f;
-    const float it = ct / s.st, i1 = ch / (same ? s.st : s.s1);
-    float part[2] = {0.f, 0.f};
-    for (int c = c0; c < c1; c += kPiece) {
-        const int end = min(c1, c + kPiece);
-        RawRowQuad<YBF, false> raw[kLongQ];
-        QuadPlace at[kLongQ];
-#pragma unroll
-        for (int q = 0; q < kLongQ; ++q) {
-            place(at[q], c, q, c1, a.C);
-            raw[q].load(wy, at[q].at, at[q].count);
-        }
-        if (en.taught) en.scatter(reinterpret_cast<float *>(tile), c, end, a.temp_a, flag);
-#pragma unroll
-        for (int q = 0; q < kLongQ; ++q) {
-            const int col = c + 4 * (static_cast<int>(threadIdx.x) + q * kLong);
-            const row_f32x4 y = raw[q].get(at[q], odd);
-            row_f32x4 o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float d = y[i] - s.m, e = exp2_fast(d * a.temp_a);
-                o[i] = e * it;
-                if (labeled) {
-                    o[i] = fmaf(same ? e : exp2_fast(d * kLog2e), i1, o[i]);
-                    if (col + i == lab && i < at[q].count) {   // places behind c1 are another split's
-                        o[i] -= ch;
-                        part[1] += d;
-                    }
-                }
-            }
-            if (en.taught) {
-                const row_f32x4 P = tile[threadIdx.x + q * kLong];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    part[0] = fmaf(P[i], P[i] == 0.f ? 0.f : y[i] - s.m, part[0]);
-                    o[i] = fmaf(-ct, P[i], o[i]);
-                }
-            }
-            put(a, row, at[q], o);
-        }
-        if (en.taught) {
-            __syncthreads();
-            en.clear(reinterpret_cast<float *>(tile), c, end);
-            __syncthreads();
-        }
-    }
-    row_reduce<kLong>(part, AddOp(), sh, turn);
-    return make_float2(part[0], part[1]);
 }
 
 // Classes of a split: whole quads.
 __host__ __device__ __forceinline__ int split_width(int C, int splits) { return ((C + splits - 1) / splits + 3) / 4 * 4; }
 
-// First launch of split rows: statistics of split blockIdx.x of row blockIdx.y (and rows 65,535 on).
-template <bool YBF>
-__global__ __launch_bounds__(kLong) void distill_stats_kernel(Args a) {
-    __shared__ float sh[row_reduce_floats<kLong>()];
+// First launch of split rows: statistics of split blockIdx.x of row blockIdx.y.
+template <bool YBF, bool ODD>
+__global__ __launch_bounds__(kSweep) void distill_stats_kernel(Args a) {
+    __shared__ float sh[row_reduce_floats<kSweep>()];
     int turn = 0;
     const int splits = gridDim.x, width = split_width(a.C, splits);
     const int c0 = min(a.C, static_cast<int>(blockIdx.x) * width), c1 = min(a.C, c0 + width);
     for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
-        const RowStats s = sweep_stats<YBF>(a, row, c0, c1, a.labels != nullptr, sh, turn);
+        const RowStats s = sweep_stats<YBF, ODD>(a, row, c0, c1, a.labels != nullptr, sh, turn);
         if (threadIdx.x == 0) {
             float *o = a.stats + (row * splits + blockIdx.x) * 3;
             o[0] = s.m;
@@ -484,37 +615,39 @@ __global__ __launch_bounds__(kLong) void distill_stats_kernel(Args a) {
 
 // The gradient of rows of any length.  With one split the workgroup sweeps its rows' statistics
 // itself; else they come from `stats`.
-template <bool YBF, bool TBF>
-__global__ __launch_bounds__(kLong) void distill_long_kernel(Args a) {
-    __shared__ float sh[row_reduce_floats<kLong>()];
-    __shared__ row_f32x4 tile[kLong * kLongQ];
+template <bool YBF, bool TBF, bool ODD>
+__global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
+    constexpr int kPiece = 4 * kSweep * kSweepQ;
+    __shared__ float sh[row_reduce_floats<kSweep>()];
+    __shared__ row_f32x4 tiles[kSweep * kSweepQ];
     __shared__ int flag;
     int turn = 0;
+    float *tile = reinterpret_cast<float *>(tiles);
     const int splits = gridDim.x, width = split_width(a.C, splits);
     const int c0 = min(a.C, static_cast<int>(blockIdx.x) * width), c1 = min(a.C, c0 + width);
 #pragma unroll
-    for (int q = 0; q < kLongQ; ++q) tile[threadIdx.x + q * kLong] = row_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int q = 0; q < kSweepQ; ++q) tiles[threadIdx.x + q * kSweep] = row_f32x4{0.f, 0.f, 0.f, 0.f};
     if (threadIdx.x == 0) flag = 0;
     __syncthreads();
     double soft = 0.0, hard = 0.0;
     for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
-        Entries<kLong, TBF> en;
+        Entries<kSweep, TBF> en;
         en.load(a, row, threadIdx.x);
         const int lab = a.labels ? a.labels[row] : -1;
         const bool labeled = lab >= 0 && lab < a.C;
-        float entropy;
-        en.prepare(a.temp_a, sh, turn, entropy);
+        float top[2], sum[1];
+        en.local_max(top);
+        row_reduce<kSweep>(top, MaxOp(), sh, turn);
+        en.local_sum(top, a.temp_a, sum);
+        row_reduce<kSweep>(sum, AddOp(), sh, turn);
         if (!en.taught && !labeled) {
-            for (int c = c0; c < c1; c += 4 * kLong) {
-                QuadPlace at;
-                place(at, c, 0, c1, a.C);
-                put(a, row, at, row_f32x4{0.f, 0.f, 0.f, 0.f});
-            }
+            put_zeros<kSweep, ODD>(a, row, c0, c1);
             continue;
         }
+        en.have(sum[0]);
         RowStats s;
         if (splits == 1) {
-            s = sweep_stats<YBF>(a, row, 0, a.C, labeled && a.temp_a != kLog2e, sh, turn);
+            s = sweep_stats<YBF, ODD>(a, row, 0, a.C, labeled && a.temp_a != kLog2e, sh, turn);
         } else {
             s = RowStats{-FLT_MAX, 0.f, 0.f};
             const float *in = a.stats + row * splits * 3;
@@ -524,21 +657,42 @@ __global__ __launch_bounds__(kLong) void distill_long_kernel(Args a) {
                 s.s1 = fmaf(in[3 * k + 2], exp2_fast((in[3 * k] - s.m) * kLog2e), s.s1);
             }
         }
-        const float2 part = sweep_grad<YBF, TBF>(a, row, c0, c1, s, en, lab, tile, &flag, sh, turn);
-        if (threadIdx.x == 0) {
-            if (en.taught) {
-                soft -= static_cast<double>(a.temp_a) * part.x;
-                if (blockIdx.x == 0) soft += static_cast<double>(entropy) + __builtin_amdgcn_logf(s.st);
+        const RowGrad<ODD> grad(a, s, en.taught, lab);
+        const __amdgpu_buffer_rsrc_t wy = row_window<YBF>(a.Y, row * a.C, a.C);
+        float cross = 0.f, label = 0.f;
+        for (int c = c0; c < c1; c += kPiece) {
+            RawRowQuad<YBF, false> raw[kSweepQ];
+#pragma unroll
+            for (int q = 0; q < kSweepQ; ++q) {
+                const QuadPlace at = place<kSweep, ODD>(threadIdx.x, c, q, c1, a.C);
+                raw[q].load(wy, at.at, at.count);
             }
-            if (labeled) {
-                hard -= static_cast<double>(kLog2e) * part.y;
-                if (blockIdx.x == 0)
-                    hard += __builtin_amdgcn_logf(a.temp_a == kLog2e ? s.st : s.s1);
+            if (en.taught) en.scatter(tile, c, min(c1, c + kPiece), a.temp_a, &flag);
+#pragma unroll
+            for (int q = 0; q < kSweepQ; ++q) {
+                const QuadPlace at = place<kSweep, ODD>(threadIdx.x, c, q, c1, a.C);
+                grad.quad(a, row, at, raw[q].get(at, ODD), c + 4 * (static_cast<int>(threadIdx.x) + q * kSweep),
+                          tiles[threadIdx.x + q * kSweep], cross, label);
+            }
+            if (en.taught) {
+                __syncthreads();
+                en.clear(tile, c, min(c1, c + kPiece), a.temp_a);
+                __syncthreads();
             }
         }
+        // each split of a row adds its classes; the first one what the row has once
+        if (en.taught) {
+            soft -= static_cast<double>(a.temp_a) * cross;
+            if (blockIdx.x == 0) soft += en.entropy;
+            if (blockIdx.x == 0 && threadIdx.x == 0) soft += __builtin_amdgcn_logf(s.st) - __builtin_amdgcn_logf(sum[0]);
+        }
+        if (labeled) {
+            hard -= static_cast<double>(kLog2e) * label;
+            if (blockIdx.x == 0 && threadIdx.x == 0) hard += __builtin_amdgcn_logf(a.temp_a == kLog2e ? s.st : s.s1);
+        }
     }
-    write_partial<kLong>(soft, hard,
-                         a.partial + 2 * (static_cast<int64_t>(blockIdx.y) * splits + blockIdx.x));
+    write_partial<kSweep>(soft, hard,
+                          a.partial + 2 * (static_cast<int64_t>(blockIdx.y) * splits + blockIdx.x));
 }
 
 // loss = {soft + hard, soft, hard} from the workgroups' sums, by a fixed tree.
@@ -571,7 +725,7 @@ __global__ __launch_bounds__(kThreads) void distill_loss_kernel(const double *__
 
 // ------------------------------------------------------------------ dispatch
 
-constexpr int kRegisterClasses = 8192;               // widest row in registers
+constexpr int kRowClasses = 2048;                    // widest row of distill_rows_kernel
 constexpr int kMaxBlocks = 8192;
 constexpr int kSplitBlocks = 512;                    // workgroups that fill the chip (two a CU)
 constexpr int kMinSplit = 4096;                      // classes a split has at least
@@ -595,25 +749,54 @@ int launch_rows(const Args &a, bool tbf, hipStream_t s) {
     return blocks;
 }
 
+template <bool YBF, bool ODD, int THREADS, int QUADS>
+int launch_held(const Args &a, bool tbf, hipStream_t s) {
+    const int blocks = row_blocks(a.n, 1);
+    if (tbf) hipLaunchKernelGGL((distill_held_kernel<YBF, true, ODD, THREADS, QUADS>), dim3(blocks), dim3(THREADS), 0, s, a);
+    else hipLaunchKernelGGL((distill_held_kernel<YBF, false, ODD, THREADS, QUADS>), dim3(blocks), dim3(THREADS), 0, s, a);
+    return blocks;
+}
+
+// Rows past those of distill_rows_kernel.  Few threads with many quads each leave room for more rows
+// on a CU (2^27 elements, us, float32 / bfloat16, floor 186 / 93: C = 8,192 (256, 8) 204 / 160, (512, 4) 251 / 181,
+// (1024, 4) twice that); past 32,768 classes two workgroups a CU hold less than the sweep's second reading of
+// a row from the caches costs (2^28 elements: C = 65,536 swept 457 / 297, held by 1,024 threads 582 / 360).
+template <bool YBF, bool ODD>
+int launch_long(const Args &a, bool tbf, hipStream_t s) {
+    const int C = a.C, splits = splits_of(a.n, C);
+    if (splits == 1) {
+        if (C <= 4096) return launch_held<YBF, ODD, 256, 4>(a, tbf, s);
+        if (C <= 8192) return launch_held<YBF, ODD, 256, 8>(a, tbf, s);
+        if (C <= 16384) return launch_held<YBF, ODD, 256, 16>(a, tbf, s);
+        if (C <= 32768) return launch_held<YBF, ODD, 512, 16>(a, tbf, s);
+    }
+    const dim3 grid(splits, row_blocks(a.n, 1));
+    if (splits > 1) hipLaunchKernelGGL((distill_stats_kernel<YBF, ODD>), grid, dim3(kSweep), 0, s, a);
+    if (tbf) hipLaunchKernelGGL((distill_sweep_kernel<YBF, true, ODD>), grid, dim3(kSweep), 0, s, a);
+    else hipLaunchKernelGGL((distill_sweep_kernel<YBF, false, ODD>), grid, dim3(kSweep), 0, s, a);
+    return static_cast<int>(grid.x * grid.y);
+}
+
+// Few lanes a row with several quads each share a wavefront's instructions between more rows
+// (2^27 elements, us, float32 / bfloat16: C = 128 (16, 2) 238 / 203, (32, 1) 309 / 295; C = 256 (16, 4) 217 / 169, (64, 1)
+// 317 / 306).
 template <bool YBF>
 int launch_any(const Args &a, bool tbf, hipStream_t s) {
     const int C = a.C;
     if (C < 4) return launch_rows<1, 1, YBF>(a, tbf, s);
+    if (C <= 16) return launch_rows<4, 1, YBF>(a, tbf, s);
     if (C <= 32) return launch_rows<8, 1, YBF>(a, tbf, s);
-    if (C <= 64) return launch_rows<16, 1, YBF>(a, tbf, s);
-    if (C <= 128) return launch_rows<32, 1, YBF>(a, tbf, s);
-    if (C <= 256) return launch_rows<64, 1, YBF>(a, tbf, s);
-    if (C <= 512) return launch_rows<64, 2, YBF>(a, tbf, s);
+    if (C <= 64) return launch_rows<8, 2, YBF>(a, tbf, s);
+    if (C <= 128) return launch_rows<16, 2, YBF>(a, tbf, s);
+    if (C <= 192) return launch_rows<16, 3, YBF>(a, tbf, s);
+    if (C <= 256) return launch_rows<16, 4, YBF>(a, tbf, s);
+    if (C <= 384) return launch_rows<32, 3, YBF>(a, tbf, s);
+    if (C <= 512) return launch_rows<32, 4, YBF>(a, tbf, s);
+    if (C <= 768) return launch_rows<64, 3, YBF>(a, tbf, s);
     if (C <= 1024) return launch_rows<64, 4, YBF>(a, tbf, s);
-    if (C <= 2048) return launch_rows<256, 2, YBF>(a, tbf, s);
-    if (C <= 4096) return launch_rows<256, 4, YBF>(a, tbf, s);
-    if (C <= kRegisterClasses) return launch_rows<512, 4, YBF>(a, tbf, s);
-    const int splits = splits_of(a.n, C);
-    const dim3 grid(splits, row_blocks(a.n, 1));
-    if (splits > 1) hipLaunchKernelGGL(distill_stats_kernel<YBF>, grid, dim3(kLong), 0, s, a);
-    if (tbf) hipLaunchKernelGGL((distill_long_kernel<YBF, true>), grid, dim3(kLong), 0, s, a);
-    else hipLaunchKernelGGL((distill_long_kernel<YBF, false>), grid, dim3(kLong), 0, s, a);
-    return static_cast<int>(grid.x * grid.y);
+    if (C <= 1536) return launch_rows<128, 3, YBF>(a, tbf, s);
+    if (C <= kRowClasses) return launch_rows<128, 4, YBF>(a, tbf, s);
+    return C & 3 ? launch_long<YBF, true>(a, tbf, s) : launch_long<YBF, false>(a, tbf, s);
 }
 
 }  // namespace
@@ -621,7 +804,7 @@ int launch_any(const Args &a, bool tbf, hipStream_t s) {
 size_t distill_workspace_bytes(int32_t n, int32_t C) {
     // partial sums of the loss, then the statistics of split rows (rows that are split are few)
     size_t bytes = 2 * sizeof(double) * kMaxBlocks;
-    if (C > kRegisterClasses && splits_of(n, C) > 1) bytes += sizeof(float) * 3 * static_cast<size_t>(n) * splits_of(n, C);
+    if (C > kRowClasses && splits_of(n, C) > 1) bytes += sizeof(float) * 3 * static_cast<size_t>(n) * splits_of(n, C);
     return (bytes + 255) / 256 * 256;
 }
 
