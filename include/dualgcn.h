@@ -567,7 +567,8 @@ int dualgcn_distill_xent(const void *Y, const int32_t *ids, const void *teacher,
  * 128 consecutive features of a row (the last block of a row may be shorter).  A scale is the
  * least power of two, 2^-126 or more, that brings the block's largest finite magnitude to 448 or
  * below (1 for a block without one), so that the division is exact; elements are rounded once, to nearest
- * even.  Infinities and NaN become NaN.  n >= 1, F >= 1.  Asynchronous.
+ * even.  Infinities and NaN become NaN.  n >= 1, 1 <= F < 2^20 (larger: DUALGCN_ERR_UNSUPPORTED).
+ * Asynchronous.
  *
  * dualgcn_quantize_weight_fp8 -- W (device, float32 F_in x F_out row-major) with a scale for each
  * 128 x 128 block, in the layout dualgcn_update_fp8 reads: with `transpose` not 0, Q is

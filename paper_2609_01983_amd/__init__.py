@@ -562,6 +562,8 @@ def _rows(t, name):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.is_contiguous() and
             (t.dtype is torch.float32 or t.dtype is torch.bfloat16)):
         _float_or_bf16(t, name)
+    if t.shape[0] > 0x7FFFFFFF or t.shape[1] > 0x7FFFFFFF:
+        raise ValueError(f"{name} has more than 2^31 - 1 rows or columns")
     return t.dtype is torch.bfloat16
 
 
@@ -726,6 +728,8 @@ def distill_xent(Y, ids, teacher, labels=None, temperature=1.0, soft_scale=None,
     if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
         raise ValueError("ids must be an [n, K] tensor")
     K = ids.shape[1]
+    if max(C, K) > 0x7FFFFFFF:
+        raise ValueError("more than 2^31 - 1 classes or entries")
     _shaped(ids, torch.int32, (n, K), "ids")
     if _rows(teacher, "teacher"):
         flags |= TEACHER_BF16
@@ -787,6 +791,8 @@ def quantize_weight_fp8(W, transpose=True, Q=None, scales=None, stream=None):
     if W.dim() != 2:
         raise ValueError("W must be [F_in, F_out]")
     F_in, F_out = W.shape
+    if max(F_in, F_out) > 0x7FFFFFFF:
+        raise ValueError("more than 2^31 - 1 rows or columns")
     s = _queue(stream, W, Q, scales)
     shape = (F_out, F_in) if transpose else (F_in, F_out)
     Q, scales = _fp8_out(W, shape, (_fp8_blocks(shape[0]), _fp8_blocks(shape[1])), Q, scales, stream)
@@ -803,6 +809,8 @@ def update_fp8(X, sx, W, sw, T=None, out_bf16=False, stream=None):
         raise ValueError("X must be an [n, F_in] tensor and W an [F_out, F_in] tensor")
     n, F_in = X.shape
     F_out = W.shape[0]
+    if max(n, F_in, F_out) > 0x7FFFFFFF:
+        raise ValueError("more than 2^31 - 1 rows or columns")
     _shaped(X, torch.float8_e4m3fn, (n, F_in), "X")
     _shaped(W, torch.float8_e4m3fn, (F_out, F_in), "W")
     _shaped(sx, torch.float32, (n, _fp8_blocks(F_in)), "sx")

@@ -669,6 +669,7 @@ int dualgcn_quantize_fp8(const void *X, int32_t n, int32_t F, uint32_t flags, vo
     dgc::TraceRange trace("dualgcn_quantize_fp8");
     if (!X || !Q || !scales || n < 1 || F < 1 || (flags & ~DUALGCN_IN_BF16)) return DUALGCN_ERR_INVALID_ARG;
     const bool bf = flags & DUALGCN_IN_BF16;
+    if (F >= (1 << 20)) return DUALGCN_ERR_UNSUPPORTED;
     if (!elem_aligned(X, bf) || !elem_aligned(scales, false)) return DUALGCN_ERR_INVALID_ARG;
     const size_t un = static_cast<size_t>(n), elems = un * F;
     const Span in[] = {{X, elems * (bf ? 2 : 4)}};

@@ -446,14 +446,6 @@ __device__ __forceinline__ void put_zeros(const Args &a, int64_t row, int c0, in
     }
 }
 
-// A value that the optimiser takes for a new one: what was computed from it before is not kept in
-// registers for its next use (a held row leaves none for its exponentials or places).
-template <class T>
-__device__ __forceinline__ T anew(T v) {
-    asm volatile("" : "+v"(v));
-    return v;
-}
-
 // A row that QUADS quads of THREADS threads hold.  The second bound keeps a CU's registers full.
 template <bool YBF, bool TBF, bool ODD, int THREADS, int QUADS>
 __global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(Args a) {
@@ -725,7 +717,7 @@ __global__ __launch_bounds__(kThreads) void distill_loss_kernel(const double *__
 
 // ------------------------------------------------------------------ dispatch
 
-constexpr int kRowClasses = 2048;                    // widest row of distill_rows_kernel
+constexpr int kRowClasses = 1024;                    // widest row of distill_rows_kernel
 constexpr int kMaxBlocks = 8192;
 constexpr int kSplitBlocks = 512;                    // workgroups that fill the chip (two a CU)
 constexpr int kMinSplit = 4096;                      // classes a split has at least
@@ -765,7 +757,9 @@ template <bool YBF, bool ODD>
 int launch_long(const Args &a, bool tbf, hipStream_t s) {
     const int C = a.C, splits = splits_of(a.n, C);
     if (splits == 1) {
-        if (C <= 4096) return launch_held<YBF, ODD, 256, 4>(a, tbf, s);
+        if (C <= 2048) return launch_held<YBF, ODD, 64, 8>(a, tbf, s);
+        // (float32 / bfloat16 at C = 3,000: (256, 4) 212 / 165, (128, 8) 227 / 140)
+        if (C <= 4096) return launch_held<YBF, ODD, YBF ? 128 : 256, YBF ? 8 : 4>(a, tbf, s);
         if (C <= 8192) return launch_held<YBF, ODD, 256, 8>(a, tbf, s);
         if (C <= 16384) return launch_held<YBF, ODD, 256, 16>(a, tbf, s);
         if (C <= 32768) return launch_held<YBF, ODD, 512, 16>(a, tbf, s);
@@ -793,9 +787,7 @@ int launch_any(const Args &a, bool tbf, hipStream_t s) {
     if (C <= 384) return launch_rows<32, 3, YBF>(a, tbf, s);
     if (C <= 512) return launch_rows<32, 4, YBF>(a, tbf, s);
     if (C <= 768) return launch_rows<64, 3, YBF>(a, tbf, s);
-    if (C <= 1024) return launch_rows<64, 4, YBF>(a, tbf, s);
-    if (C <= 1536) return launch_rows<128, 3, YBF>(a, tbf, s);
-    if (C <= kRowClasses) return launch_rows<128, 4, YBF>(a, tbf, s);
+    if (C <= kRowClasses) return launch_rows<64, 4, YBF>(a, tbf, s);
     return C & 3 ? launch_long<YBF, true>(a, tbf, s) : launch_long<YBF, false>(a, tbf, s);
 }
 

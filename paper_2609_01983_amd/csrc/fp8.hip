@@ -64,48 +64,64 @@ __device__ __forceinline__ uint32_t to_e4m3(row_f32x4 v) {
     return static_cast<uint32_t>(r);
 }
 
-typedef uint32_t u32_any __attribute__((aligned(1)));
-
-// 16 lanes a block of 128, two quads a lane (a lane's elements 4 l and 64 + 4 l on).
+// A workgroup takes 16 rows, 16 lanes each, and up to eight blocks of them (blockIdx.y); a lane has
+// the elements from 4 l and 64 + 4 l on of a block, and two blocks' loads are in flight.
 constexpr int kQuantThreads = 256;
 constexpr int kQuantLanes = 16;
-template <bool BF>
+constexpr int kQuantRows = kQuantThreads / kQuantLanes;
+constexpr int kQuantBlocks = 8;
+template <bool BF, bool TINY>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(const void *__restrict__ X, uint8_t *__restrict__ Q,
-                                                                 float *__restrict__ scales, int64_t items,
-                                                                 int32_t F, int32_t blocks) {
-    const int l = threadIdx.x % kQuantLanes;
-    constexpr int kPer = kQuantThreads / kQuantLanes;
-    for (int64_t it = static_cast<int64_t>(blockIdx.x) * kPer + threadIdx.x / kQuantLanes; it < items;
-         it += static_cast<int64_t>(gridDim.x) * kPer) {
-        const int64_t row = it / blocks;
-        const int b = static_cast<int>(it - row * blocks);
-        const int64_t r0 = row * F;
-        row_f32x4 v[2];
-        float amax = 0.f;
+                                                                 float *__restrict__ scales, int32_t n, int32_t F,
+                                                                 int32_t blocks) {
+    const int l = threadIdx.x % kQuantLanes, g = threadIdx.x / kQuantLanes;
+    const bool odd = F & 3;
+    const int b0 = blockIdx.y * kQuantBlocks, b1 = min(blocks, b0 + kQuantBlocks);
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kQuantRows; row0 < n;
+         row0 += static_cast<int64_t>(gridDim.x) * kQuantRows) {
+        const int64_t rows = min(static_cast<int64_t>(kQuantRows), n - row0);
+        const __amdgpu_buffer_rsrc_t wx = row_window<BF>(X, row0 * F, rows * F);
+        const __amdgpu_buffer_rsrc_t wq = __builtin_amdgcn_make_buffer_rsrc(Q + row0 * F, 0, static_cast<int>(rows * F), 0x00020000);
+        for (int b = b0; b < b1; b += 2) {
+            QuadPlace at[2][2];
+            RawRowQuad<BF, TINY> raw[2][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int col = b * kBlock + 64 * h + 4 * l;
-            v[h] = load_quad<BF>(X, r0 + col, F - col);
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) amax = fmaxf(amax, finite_abs(v[h][i]));
-        }
-        amax = lanes_reduce<kQuantLanes>(amax, MaxOp());
-        const int k = scale_exponent(amax);
-        const float inv = power_of_two(-k);
+                for (int h = 0; h < 2; ++h) {
+                    const int first = (b + j) * kBlock + 64 * h + 4 * l;
+                    at[j][h].set(static_cast<uint32_t>(g) * F, b + j < b1 ? first : F, F);
+                    raw[j][h].load(wx, at[j][h].at, at[j][h].count);
+                }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int col = b * kBlock + 64 * h + 4 * l, count = F - col;
-            const uint32_t q = to_e4m3(v[h] * inv);
-            uint8_t *p = Q + r0 + col;
-            if (count >= 4) {
-                *reinterpret_cast<u32_any *>(p) = q;
-            } else {
+            for (int j = 0; j < 2; ++j) {
+                row_f32x4 v[2];
+                float amax = 0.f;
 #pragma unroll
-                for (int i = 0; i < 3; ++i)
-                    if (i < count) p[i] = static_cast<uint8_t>(q >> 8 * i);
+                for (int h = 0; h < 2; ++h) {
+                    v[h] = raw[j][h].get(at[j][h], odd);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) amax = fmaxf(amax, finite_abs(v[h][i]));
+                }
+                amax = lanes_reduce<kQuantLanes>(amax, MaxOp());
+                const int k = scale_exponent(amax);
+                const float inv = power_of_two(-k);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t q = to_e4m3(v[h] * inv);
+                    const QuadPlace &p = at[j][h];
+                    const bool part = TINY || (odd && p.part);
+                    if constexpr (!TINY) __builtin_amdgcn_raw_buffer_store_b32(q, wq, part ? kNoQuad : p.at, 0, 0);
+                    if (part) {
+                        const uint32_t to = TINY ? p.at : p.at + 4 - p.part;
+#pragma unroll
+                        for (int i = 0; i < 3; ++i)
+                            if (i < p.part) __builtin_amdgcn_raw_buffer_store_b8(static_cast<uint8_t>(q >> 8 * i), wq, to + i, 0, 0);
+                    }
+                }
+                if (l == 0 && g < rows && b + j < b1) scales[(row0 + g) * blocks + b + j] = power_of_two(k);
             }
         }
-        if (l == 0) scales[it] = power_of_two(k);
     }
 }
 
@@ -172,11 +188,15 @@ struct ProductArgs {
 
 // A lane's 32 bytes of block b of row `row` (X8 or W8 with rows of K): chunks of 16 at 16 g and
 // 64 + 16 g of the block, four steps of eight k each.  Both operands give a step the same k, so a
-// block's sum is right whatever their order.  Chunks behind the row's end are read at its start
-// and zeroed by get().
+// block's sum is right whatever their order.  Chunks behind the row's end are zeroed by get().
 constexpr int kSteps = kBlock / 32;
 struct Fragment {
     u32x4 lo, hi;
+    // from a window that starts at the block's first byte of the tile's first row; `at`: the row's offset + 16 g
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t w, uint32_t at) {
+        lo = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w, at, 0, 0));
+        hi = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w, at + 64, 0, 0));
+    }
     __device__ __forceinline__ void load(const uint8_t *base, int64_t row, int K, int b, int g) {
         const uint8_t *r = base + row * K;
         const int k = b * kBlock + 16 * g;
@@ -184,9 +204,13 @@ struct Fragment {
         hi = *reinterpret_cast<const u32x4 *>(r + (k + 64 < K ? k + 64 : 0));
     }
     __device__ __forceinline__ void get(int K, int b, int g, bf16x8 (&out)[kSteps]) const {
-        const int k = b * kBlock + 16 * g;
-        const u32x4 zero = {0, 0, 0, 0};
-        const u32x4 x = k < K ? lo : zero, y = k + 64 < K ? hi : zero;
+        u32x4 x = lo, y = hi;
+        if (K % kBlock) {                                // uniform
+            const int k = b * kBlock + 16 * g;
+            const u32x4 zero = {0, 0, 0, 0};
+            x = k < K ? lo : zero;
+            y = k + 64 < K ? hi : zero;
+        }
         out[0] = widen(x[0], x[1]);
         out[1] = widen(x[2], x[3]);
         out[2] = widen(y[0], y[1]);
@@ -211,12 +235,15 @@ constexpr int kRowsPerBlock = kWaves * kRows;
 // so that the 16 rows a read touches start in 16 different groups of four banks
 __host__ __device__ __forceinline__ int lds_row(int blocks) { return blocks * kBlock + 8; }
 
+// Workgroup w takes slice w % slices of the columns and the row tiles w / slices, + gridDim.x / slices, ...:
+// the slices of a tile run side by side and read its X from the caches.
 template <int CT>
-__global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a) {
+__global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_t slices) {
     extern __shared__ uint4 lds[];
     __bf16 *w = reinterpret_cast<__bf16 *>(lds);
     const int ld = lds_row(a.blocks);
-    const int c0 = blockIdx.y * 16 * CT;
+    const int c0 = static_cast<int>(blockIdx.x) % slices * 16 * CT;
+    const int64_t stride = gridDim.x / slices;
     // W of the columns [c0, c0 + 16 CT), zeros past F_out and past F_in: 16 bytes of W8 are two
     // steps of a lane group, [block][step][g][8]
     const int per_row = a.blocks * kBlock / 16;
@@ -233,47 +260,53 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a) {
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = lane & 15, g = lane >> 4;
+    // the columns' scales: tiles of 16 columns from `turn` on are in the next block of 128
     const float *sw = a.sw + static_cast<int64_t>(c0 / kBlock) * a.blocks;
+    const int turn = (kBlock - c0 % kBlock) / 16;
+    const int64_t next_sw = c0 / kBlock + 1 < (a.N + kBlock - 1) / kBlock ? a.blocks : 0;
     const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
     const int last = min(a.N, c0 + 16 * CT);
 
-    auto row_of = [&](int64_t tile, int t) {
-        const int64_t row = tile * kRowsPerBlock + wave * kRows + t * 16 + r;
-        return row < a.n ? row : static_cast<int64_t>(a.n) - 1;
-    };
-    Fragment cur[kRowTiles], nxt[kRowTiles];
+    // A tile's rows as windows, from block b on: rows behind the last are zeros, and lanes address
+    // them with 32 bits (256 rows of at most 1,024 bytes).
+    Fragment in[kRowTiles];
     float sc[kRowTiles], sn[kRowTiles];
-    int64_t tile = blockIdx.x;                       // the grid has at most one workgroup a tile and slice
+    uint32_t at[kRowTiles];
 #pragma unroll
-    for (int t = 0; t < kRowTiles; ++t) {
-        const int64_t row = row_of(tile, t);
-        cur[t].load(a.X, row, a.K, 0, g);
-        sc[t] = a.sx[row * a.blocks];
-    }
-    for (; tile < tiles; tile += gridDim.x) {
+    for (int t = 0; t < kRowTiles; ++t) at[t] = wave * kRows + t * 16 + r;
+    auto request = [&](int64_t tile, int b) {
+        const int64_t row0 = tile * kRowsPerBlock;
+        const int64_t rows = max(int64_t{0}, min(static_cast<int64_t>(kRowsPerBlock), a.n - row0));
+        const __amdgpu_buffer_rsrc_t wx = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t *>(a.X) + row0 * a.K + b * kBlock, 0,
+            rows ? static_cast<int>(rows * a.K - b * kBlock) : 0, 0x00020000);
+        const __amdgpu_buffer_rsrc_t ws = row_window<false>(a.sx, row0 * a.blocks + b, rows ? rows * a.blocks - b : 0);
+#pragma unroll
+        for (int t = 0; t < kRowTiles; ++t) {
+            in[t].load(wx, at[t] * a.K + 16 * g);
+            sn[t] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ws, at[t] * a.blocks * 4, 0, 0));
+        }
+    };
+    int64_t tile = blockIdx.x / slices;              // the grid has at most one workgroup a tile and slice
+    request(tile, 0);
+    for (; tile < tiles; tile += stride) {
         f32x4 acc[kRowTiles][CT];
 #pragma unroll
         for (int t = 0; t < kRowTiles; ++t)
 #pragma unroll
             for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int b = 0; b < a.blocks; ++b) {
-            // the next block of this tile, or the first of the next tile (past the last: rows n - 1)
-            const bool more = b + 1 < a.blocks;
-            const int nb = more ? b + 1 : 0;
-            const int64_t nt = more ? tile : tile + gridDim.x;
-#pragma unroll
-            for (int t = 0; t < kRowTiles; ++t) {
-                const int64_t row = row_of(nt, t);
-                nxt[t].load(a.X, row, a.K, nb, g);
-                sn[t] = a.sx[row * a.blocks + nb];
-            }
             bf16x8 x[kRowTiles][kSteps];
-            float f[kRowTiles];
 #pragma unroll
             for (int t = 0; t < kRowTiles; ++t) {
-                cur[t].get(a.K, b, g, x[t]);
-                f[t] = sc[t] * sw[b];
+                in[t].get(a.K, b, g, x[t]);
+                sc[t] = sn[t];
             }
+            // the next block of this tile, or the first of the next tile (past the last: zeros), into the
+            // registers that the widened ones have left
+            const bool more = b + 1 < a.blocks;
+            request(more ? tile : tile + stride, more ? b + 1 : 0);
+            const float sw0 = sw[b], sw1 = sw[next_sw + b];
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 const __bf16 *p = w + (16 * c + r) * ld + b * kBlock + 8 * g;
@@ -286,23 +319,31 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a) {
 #pragma unroll
                     for (int t = 0; t < kRowTiles; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[t][k], s[t], 0, 0, 0);
                 }
+                const float swc = c < turn ? sw0 : sw1;
 #pragma unroll
-                for (int t = 0; t < kRowTiles; ++t)
+                for (int t = 0; t < kRowTiles; ++t) {
+                    const float f = sc[t] * swc;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t][c][i] = fmaf(f[t], s[t][i], acc[t][c][i]);
-            }
-#pragma unroll
-            for (int t = 0; t < kRowTiles; ++t) {
-                cur[t] = nxt[t];
-                sc[t] = sn[t];
+                    for (int i = 0; i < 4; ++i) acc[t][c][i] = fmaf(f, s[t][i], acc[t][c][i]);
+                }
             }
         }
+        const int64_t row0 = tile * kRowsPerBlock;
+        const int64_t elems = min(static_cast<int64_t>(kRowsPerBlock), a.n - row0) * a.N;
+        const int own = anew(4 * g);                 // the places are worked out here, not kept over the tiles
 #pragma unroll
-        for (int t = 0; t < kRowTiles; ++t) {
-            const int64_t row = tile * kRowsPerBlock + wave * kRows + t * 16 + r;
+        for (int t = 0; t < kRowTiles; ++t)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) store_tile(a, row, c0 + 16 * c + 4 * g, last, acc[t][c]);
-        }
+            for (int c = 0; c < CT; ++c) {
+                const int col = c0 + 16 * c + own;
+                QuadPlace to;
+                to.count = last - col;
+                to.part = to.count > 0 && to.count < 4 ? to.count : 0;
+                to.at = to.count > 0 ? at[t] * a.N + col - (to.part ? 4 - to.part : 0) : kNoQuad;
+                to.col = 0;
+                if (a.out_bf16) store_row_quad<true, false>(row_window<true>(a.T, row0 * a.N, elems), to, acc[t][c], a.N & 3, false);
+                else store_row_quad<false, false>(row_window<false>(a.T, row0 * a.N, elems), to, acc[t][c], a.N & 3, false);
+            }
     }
 }
 
@@ -344,28 +385,56 @@ int allow_lds(const void *kernel, size_t bytes) {
     return hip_status(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
 }
 
+// At most kMostCols tiles of 16 columns a slice: what the accumulators and (by F_in) a CU's LDS hold.
+constexpr int kMostCols = 8;
+constexpr size_t kLds = 160 * 1024;
+constexpr int64_t kOver = 2;                         // workgroups for each place on the chip, at most
+
 template <int CT>
-int launch_product(const ProductArgs &a, hipStream_t s) {
+int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
     const size_t lds = static_cast<size_t>(16 * CT) * lds_row(a.blocks) * sizeof(uint16_t);
     const int st = allow_lds(reinterpret_cast<const void *>(&product_kernel<CT>), lds);
     if (st) return st;
-    const int per_cu = std::max<int>(1, std::min<int>(2, static_cast<int>((160 * 1024) / lds)));
     const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
-    const int slices = (a.N + 16 * CT - 1) / (16 * CT);
-    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(tiles, static_cast<int64_t>(device_cus()) * per_cu / slices));
-    hipLaunchKernelGGL(product_kernel<CT>, dim3(static_cast<unsigned>(grid), slices), dim3(kThreads), lds, s, a);
+    // registers: up to 128 a thread for four tiles of columns, hence two workgroups a CU
+    const int64_t resident = static_cast<int64_t>(device_cus()) * (CT <= 4 && 2 * lds <= kLds ? 2 : 1);
+    const int64_t per = std::max<int64_t>(1, std::min<int64_t>(tiles, kOver * resident / slices));
+    hipLaunchKernelGGL(product_kernel<CT>, dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices);
     return hip_status(hipGetLastError());
+}
+
+// Slices of equal width: as few as fit, then as narrow as those need.
+int launch_slices(const ProductArgs &a, int most, hipStream_t s) {
+    const int cols = (a.N + 15) / 16;
+    while (most > 1 && static_cast<size_t>(16 * most) * lds_row(a.blocks) * sizeof(uint16_t) > kLds) --most;
+    const int slices = (cols + most - 1) / most;
+    switch ((cols + slices - 1) / slices) {
+        case 1: return launch_product<1>(a, slices, s);
+        case 2: return launch_product<2>(a, slices, s);
+        case 3: return launch_product<3>(a, slices, s);
+        case 4: return launch_product<4>(a, slices, s);
+        case 5: return launch_product<5>(a, slices, s);
+        case 6: return launch_product<6>(a, slices, s);
+        case 7: return launch_product<7>(a, slices, s);
+        default: return launch_product<8>(a, slices, s);
+    }
 }
 
 }  // namespace
 
 int launch_quantize(const void *X, bool bf16, int32_t n, int32_t F, void *Q, float *scales, hipStream_t s) {
     const int32_t blocks = (F + kBlock - 1) / kBlock;
-    const int64_t items = static_cast<int64_t>(n) * blocks;
-    constexpr int kPer = kQuantThreads / kQuantLanes;
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((items + kPer - 1) / kPer, static_cast<int64_t>(device_cus()) * 8)));
-    if (bf16) hipLaunchKernelGGL(quantize_kernel<true>, grid, dim3(kQuantThreads), 0, s, X, static_cast<uint8_t *>(Q), scales, items, F, blocks);
-    else hipLaunchKernelGGL(quantize_kernel<false>, grid, dim3(kQuantThreads), 0, s, X, static_cast<uint8_t *>(Q), scales, items, F, blocks);
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((static_cast<int64_t>(n) + kQuantRows - 1) / kQuantRows, 1 << 20)),
+                    (blocks + kQuantBlocks - 1) / kQuantBlocks);
+    uint8_t *q = static_cast<uint8_t *>(Q);
+    const dim3 block(kQuantThreads);
+    if (F < 4) {
+        if (bf16) hipLaunchKernelGGL((quantize_kernel<true, true>), grid, block, 0, s, X, q, scales, n, F, blocks);
+        else hipLaunchKernelGGL((quantize_kernel<false, true>), grid, block, 0, s, X, q, scales, n, F, blocks);
+    } else {
+        if (bf16) hipLaunchKernelGGL((quantize_kernel<true, false>), grid, block, 0, s, X, q, scales, n, F, blocks);
+        else hipLaunchKernelGGL((quantize_kernel<false, false>), grid, block, 0, s, X, q, scales, n, F, blocks);
+    }
     return hip_status(hipGetLastError());
 }
 
@@ -384,10 +453,12 @@ int launch_update_fp8(const void *X, const float *sx, const void *W, const float
         hipLaunchKernelGGL(product_few_kernel, dim3((F_out + 15) / 16, (n + 15) / 16), dim3(kThreads), 0, s, a);
         return hip_status(hipGetLastError());
     }
-    if (F_out <= 32 || static_cast<int64_t>(n) * ((F_out + 127) / 128) <= int64_t{kRowsPerBlock} * 256)
-        return launch_product<2>(a, s);
-    // W of 128 columns fits a workgroup's LDS up to F_in = 512
-    return a.blocks <= 4 ? launch_product<8>(a, s) : launch_product<4>(a, s);
+    // few tiles: narrower slices until they are about as many as the CUs
+    const int64_t tiles = (static_cast<int64_t>(n) + kRowsPerBlock - 1) / kRowsPerBlock;
+    const int64_t share = device_cus() / tiles;                          // slices there may be
+    const int cols = (F_out + 15) / 16;
+    const int most = share <= 1 ? kMostCols : std::max<int>(1, static_cast<int>(std::min<int64_t>(kMostCols, (cols + share - 1) / share)));
+    return launch_slices(a, most, s);
 }
 
 }  // namespace dgc

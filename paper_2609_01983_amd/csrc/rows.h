@@ -166,6 +166,14 @@ __device__ __forceinline__ void store_quad(void *base, int64_t at, int count, ro
 // The value of a float32 as it is when stored in bfloat16.
 __device__ __forceinline__ float through_bf16(float f) { return static_cast<float>(static_cast<__bf16>(f)); }
 
+// A value that the optimiser takes for a new one: what was computed from it before is not kept in
+// registers for its next use.
+template <class T>
+__device__ __forceinline__ T anew(T v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 struct AddOp {
     __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
