@@ -222,7 +222,7 @@ template <int TPR, int Q, bool YBF, bool TBF>
 __global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_rows_kernel(Args a) {
     constexpr bool TINY = TPR == 1;
     constexpr int kBlock = TPR > 64 ? TPR : kThreads, kGroups = kBlock / TPR;
-    __shared__ float sh[row_reduce_floats<TPR>()];
+    __shared__ row_f32x4 sh[row_reduce_quads<TPR>()];
     __shared__ row_f32x4 tiles[kGroups][TPR * Q];
     __shared__ int flag;
     int turn = 0;
@@ -449,7 +449,7 @@ __device__ __forceinline__ void put_zeros(const Args &a, int64_t row, int c0, in
 // A row that QUADS quads of THREADS threads hold.  The second bound keeps a CU's registers full.
 template <bool YBF, bool TBF, bool ODD, int THREADS, int QUADS>
 __global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(Args a) {
-    __shared__ float sh[row_reduce_floats<THREADS>()];
+    __shared__ row_f32x4 sh[row_reduce_quads<THREADS>()];
     __shared__ row_f32x4 tiles[THREADS * kHeldQ];
     __shared__ int flag;
     int turn = 0;
@@ -545,7 +545,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(Args a) {
 
 // Classes [c0, c1) of a row: maximum and sums at T and (one) at 1, over the workgroup.
 template <bool YBF, bool ODD>
-__device__ __forceinline__ RowStats sweep_stats(const Args &a, int64_t row, int c0, int c1, bool one, float *sh,
+__device__ __forceinline__ RowStats sweep_stats(const Args &a, int64_t row, int c0, int c1, bool one, row_f32x4 *sh,
                                                 int &turn) {
     constexpr int kPiece = 4 * kSweep * kSweepQ;
     float m = -FLT_MAX, st = 0.f, s1 = 0.f;
@@ -590,7 +590,7 @@ __host__ __device__ __forceinline__ int split_width(int C, int splits) { return 
 // First launch of split rows: statistics of split blockIdx.x of row blockIdx.y.
 template <bool YBF, bool ODD>
 __global__ __launch_bounds__(kSweep) void distill_stats_kernel(Args a) {
-    __shared__ float sh[row_reduce_floats<kSweep>()];
+    __shared__ row_f32x4 sh[row_reduce_quads<kSweep>()];
     int turn = 0;
     const int splits = gridDim.x, width = split_width(a.C, splits);
     const int c0 = min(a.C, static_cast<int>(blockIdx.x) * width), c1 = min(a.C, c0 + width);
@@ -610,7 +610,7 @@ __global__ __launch_bounds__(kSweep) void distill_stats_kernel(Args a) {
 template <bool YBF, bool TBF, bool ODD>
 __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
     constexpr int kPiece = 4 * kSweep * kSweepQ;
-    __shared__ float sh[row_reduce_floats<kSweep>()];
+    __shared__ row_f32x4 sh[row_reduce_quads<kSweep>()];
     __shared__ row_f32x4 tiles[kSweep * kSweepQ];
     __shared__ int flag;
     int turn = 0;

@@ -100,7 +100,7 @@ __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)
 // x on entry, (x - mean) r on return; the row's threads share the statistics
 template <int TPR, int Q, bool LAYER>
 __device__ __forceinline__ void normalise(row_f32x4 (&x)[Q], const QuadPlace (&at)[Q], bool ragged, float inv_f,
-                                          float eps, float *sh, int &turn) {
+                                          float eps, row_f32x4 *sh, int &turn) {
     if constexpr (LAYER) {
         float m[1] = {sum_of(x)};
         row_reduce<TPR>(m, AddOp(), sh, turn);
@@ -131,7 +131,7 @@ template <int TPR, int Q, bool LAYER, bool A, bool S>
 __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(ForwardArgs a) {
     constexpr bool TINY = TPR == 1;
     constexpr int kGroups = Shape<TPR, Q>::kGroups;
-    __shared__ float sh[row_reduce_floats<TPR>()];
+    __shared__ row_f32x4 sh[row_reduce_quads<TPR>()];
     int turn = 0;
     const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
     const int F = a.F;
@@ -288,7 +288,7 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_backward_kernel(
     constexpr bool kAhead = Q < 4;                   // registers for the next row's operands
     extern __shared__ row_f32x4 kept[];              // !kHold: [slots wanted of the four][Q][kBlock]
     constexpr int kBlock = Shape<TPR, Q>::kBlock, kGroups = Shape<TPR, Q>::kGroups;
-    __shared__ float sh[row_reduce_floats<TPR>()];
+    __shared__ row_f32x4 sh[row_reduce_quads<TPR>()];
     __shared__ row_f32x4 join[kGroups > 1 ? kBlock : 1];
     int turn = 0;
     const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
@@ -577,6 +577,7 @@ void with_backward_shape(int32_t F, Fn f) {
     else if (F <= 512) shape<64, 2>(f);
     else if (F <= 768) shape<64, 3>(f);
     else if (F <= 1024) shape<256, 1>(f);
+    else if (F <= 1536) shape<128, 3>(f);
     else if (F <= 2048) shape<256, 2>(f);
     else if (F <= 3072) shape<256, 3>(f);
     else if (F <= 4096) shape<1024, 1>(f);
@@ -601,7 +602,7 @@ int backward_blocks(int32_t n, int32_t F, bool all_bf16) {
     with_backward_shape(F, [&](auto tpr, auto quads) {
         constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
         groups = Shape<T, Q>::kGroups;
-        per_cu = T > 256 ? 1 : all_bf16 ? 5 - Q : 2;
+        per_cu = T > 256 ? 1 : T == 128 ? 4 : all_bf16 ? 5 - Q : 2;
     });
     const int64_t need = (static_cast<int64_t>(n) + groups - 1) / groups;
     return static_cast<int>(std::min<int64_t>(need, std::min(kMaxBlocks, per_cu * device_cus())));

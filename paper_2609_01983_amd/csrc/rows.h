@@ -208,36 +208,36 @@ __device__ __forceinline__ float lanes_reduce(float v, Op op) {
 }
 
 // The same over THREADS threads of a row: lanes of one wavefront up to 64, the whole workgroup
-// (of THREADS threads) above, through `sh` (two buffers of THREADS / 64 * N floats, taken in turn:
-// `turn` is the caller's counter).  N values are reduced at once; every thread gets the results.
+// (of THREADS threads) above, through `sh` (two buffers of a quad for each wavefront, taken in turn:
+// `turn` is the caller's counter).  Up to four values are reduced at once; every thread gets the results:
+// it reads one wavefront's quad and joins them by lane exchanges (a read of every wavefront's
+// values instead took most of a wide row's time: 16 wavefronts, 48 reads a thread).
 template <int THREADS, int N, class Op>
-__device__ __forceinline__ void row_reduce(float (&v)[N], Op op, float *sh, int &turn) {
+__device__ __forceinline__ void row_reduce(float (&v)[N], Op op, row_f32x4 *sh, int &turn) {
+    static_assert(N <= 4, "row_reduce: too many values");
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = lanes_reduce<(THREADS < 64 ? THREADS : 64)>(v[i], op);
     if constexpr (THREADS > 64) {
         constexpr int kWaves = THREADS / 64;
-        constexpr int kMost = 4;                      // values a buffer has room for
-        static_assert(N <= kMost, "row_reduce: too many values");
-        float *b = sh + (turn & 1) * kWaves * kMost;
+        row_f32x4 *b = sh + (turn & 1) * kWaves;
         ++turn;
         if ((threadIdx.x & 63) == 0) {
+            row_f32x4 mine = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < N; ++i) b[(threadIdx.x >> 6) * kMost + i] = v[i];
+            for (int i = 0; i < N; ++i) mine[i] = v[i];
+            b[threadIdx.x >> 6] = mine;
         }
         __syncthreads();
+        const row_f32x4 one = b[threadIdx.x & (kWaves - 1)];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float s = b[i];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) s = op(s, b[w * kMost + i]);
-            v[i] = s;
-        }
+        for (int i = 0; i < N; ++i) v[i] = lanes_reduce<kWaves>(one[i], op);
     }
 }
 
 template <int THREADS>
-constexpr int row_reduce_floats() {
-    return THREADS > 64 ? 2 * (THREADS / 64) * 4 : 1;
+constexpr int row_reduce_quads() {
+    static_assert((THREADS & (THREADS - 1)) == 0 && THREADS <= 1024, "threads of a row");
+    return THREADS > 64 ? 2 * (THREADS / 64) : 1;
 }
 
 }  // namespace dgc
