@@ -231,39 +231,50 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kRowTiles = 2;
 constexpr int kRows = 16 * kRowTiles;                // of a wavefront
 constexpr int kRowsPerBlock = kWaves * kRows;
-// bfloat16 elements of a W row in LDS: whole blocks, in the order the lanes read them, and 8 more
-// so that the 16 rows a read touches start in 16 different groups of four banks
-__host__ __device__ __forceinline__ int lds_row(int blocks) { return blocks * kBlock + 8; }
+// bfloat16 elements of a tile of 16 columns in LDS: [block][step][g][column][8], so that a wavefront's
+// read of an operand is 1,024 consecutive bytes (rows of W side by side, padded by 16 bytes, had half
+// of their reads' cycles in bank conflicts).
+__host__ __device__ __forceinline__ int lds_tile(int blocks) { return blocks * kBlock * 16; }
 
-// Workgroup w takes slice w % slices of the columns and the row tiles w / slices, + gridDim.x / slices, ...:
-// the slices of a tile run side by side and read its X from the caches.
+// The slices of a row tile run at one time on one XCD and read its X from that L2: workgroups go to
+// the XCDs in turn, so number w has XCD w % 8, slice w / 8 % slices, and the tiles w / (8 slices) 8 + w % 8, ...
+// (with the slices of a tile on different XCDs, X came from beyond the L2 once a slice: 2^20 rows
+// 512 -> 512 933 us against 822, 1,024 -> 256 1,120 against 842).
+constexpr int kXcds = 8;
+constexpr int kMostBlocks = 8;                       // F_in up to 1,024
 template <int CT>
 __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_t slices) {
     extern __shared__ uint4 lds[];
     __bf16 *w = reinterpret_cast<__bf16 *>(lds);
-    const int ld = lds_row(a.blocks);
-    const int c0 = static_cast<int>(blockIdx.x) % slices * 16 * CT;
+    const int tile_elems = lds_tile(a.blocks);
+    const int c0 = static_cast<int>(blockIdx.x) / kXcds % slices * 16 * CT;
     const int64_t stride = gridDim.x / slices;
     // W of the columns [c0, c0 + 16 CT), zeros past F_out and past F_in: 16 bytes of W8 are two
-    // steps of a lane group, [block][step][g][8]
+    // steps of a lane group
     const int per_row = a.blocks * kBlock / 16;
     for (int i = threadIdx.x; i < 16 * CT * per_row; i += kThreads) {
-        const int c = i / per_row, chunk = i % per_row, k = chunk * 16;
+        const int c = i / (16 * per_row) * 16 + i % 16, chunk = i / 16 % per_row, k = chunk * 16;
         u32x4 v = {0, 0, 0, 0};
         if (c0 + c < a.N && k < a.K) v = *reinterpret_cast<const u32x4 *>(a.W + static_cast<int64_t>(c0 + c) * a.K + k);
         const int b = chunk / 8, half = chunk % 8 / 4, g = chunk % 4;
-        __bf16 *to = w + c * ld + b * kBlock + half * 64 + g * 8;
+        __bf16 *to = w + c / 16 * tile_elems + (((b * kSteps + 2 * half) * 4 + g) * 16 + c % 16) * 8;
         *reinterpret_cast<bf16x8 *>(to) = widen(v[0], v[1]);
-        *reinterpret_cast<bf16x8 *>(to + 32) = widen(v[2], v[3]);
+        *reinterpret_cast<bf16x8 *>(to + 4 * 16 * 8) = widen(v[2], v[3]);
+    }
+    // the columns' scales by LDS too: a load of them among those of X would wait for the next block's X,
+    // the loads being answered in order
+    __shared__ float column_scales[2][kMostBlocks];
+    if (static_cast<int>(threadIdx.x) < 2 * a.blocks) {
+        const int next = threadIdx.x / a.blocks, b = threadIdx.x % a.blocks;
+        const int row = min(c0 / kBlock + next, (a.N + kBlock - 1) / kBlock - 1);
+        column_scales[next][b] = a.sw[static_cast<int64_t>(row) * a.blocks + b];
     }
     __syncthreads();
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = lane & 15, g = lane >> 4;
     // the columns' scales: tiles of 16 columns from `turn` on are in the next block of 128
-    const float *sw = a.sw + static_cast<int64_t>(c0 / kBlock) * a.blocks;
     const int turn = (kBlock - c0 % kBlock) / 16;
-    const int64_t next_sw = c0 / kBlock + 1 < (a.N + kBlock - 1) / kBlock ? a.blocks : 0;
     const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
     const int last = min(a.N, c0 + 16 * CT);
 
@@ -287,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_
             sn[t] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ws, at[t] * a.blocks * 4, 0, 0));
         }
     };
-    int64_t tile = blockIdx.x / slices;              // the grid has at most one workgroup a tile and slice
+    int64_t tile = static_cast<int64_t>(blockIdx.x) / (kXcds * slices) * kXcds + blockIdx.x % kXcds;
     request(tile, 0);
     for (; tile < tiles; tile += stride) {
         f32x4 acc[kRowTiles][CT];
@@ -306,16 +317,16 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_
             // registers that the widened ones have left
             const bool more = b + 1 < a.blocks;
             request(more ? tile : tile + stride, more ? b + 1 : 0);
-            const float sw0 = sw[b], sw1 = sw[next_sw + b];
+            const float sw0 = column_scales[0][b], sw1 = column_scales[1][b];
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
-                const __bf16 *p = w + (16 * c + r) * ld + b * kBlock + 8 * g;
+                const __bf16 *p = w + c * tile_elems + b * kSteps * 512 + lane * 8;
                 f32x4 s[kRowTiles];
 #pragma unroll
                 for (int t = 0; t < kRowTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) {
-                    const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(p + 32 * k);
+                    const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(p + 512 * k);
 #pragma unroll
                     for (int t = 0; t < kRowTiles; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[t][k], s[t], 0, 0, 0);
                 }
@@ -387,18 +398,23 @@ int allow_lds(const void *kernel, size_t bytes) {
 
 // At most kMostCols tiles of 16 columns a slice: what the accumulators and (by F_in) a CU's LDS hold.
 constexpr int kMostCols = 8;
-constexpr size_t kLds = 160 * 1024;
-constexpr int64_t kOver = 2;                         // workgroups for each place on the chip, at most
+constexpr size_t kLds = 160 * 1024 - 2 * kMostBlocks * sizeof(float);   // beside the scales
+// Workgroups for each place on the chip, at most.  Where W takes up to 64 KB of LDS it is laid out quickly and
+// many short-lived workgroups keep the memory busier; a larger one has to serve many rows.  us with 2 and 16:
+// 2^22 rows 256 -> 128 676, 650; 2^22 256 -> 64 460, 429; 2^20 256 -> 256 334, 294; and past 64 KB
+// 2^21 384 -> 128 406, 414; 2^21 512 -> 128 451, 481; 2^20 1,024 -> 256 839, 903.
+inline int64_t over(size_t lds) { return lds <= 64 * 1024 ? 16 : 2; }
 
 template <int CT>
 int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
-    const size_t lds = static_cast<size_t>(16 * CT) * lds_row(a.blocks) * sizeof(uint16_t);
+    const size_t lds = static_cast<size_t>(CT) * lds_tile(a.blocks) * sizeof(uint16_t);
     const int st = allow_lds(reinterpret_cast<const void *>(&product_kernel<CT>), lds);
     if (st) return st;
     const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
     // registers: up to 128 a thread for four tiles of columns, hence two workgroups a CU
     const int64_t resident = static_cast<int64_t>(device_cus()) * (CT <= 4 && 2 * lds <= kLds ? 2 : 1);
-    const int64_t per = std::max<int64_t>(1, std::min<int64_t>(tiles, kOver * resident / slices));
+    // row tiles at a time, a whole number for each XCD
+    const int64_t per = std::max<int64_t>(1, (std::min<int64_t>(tiles, over(lds) * resident / slices) + kXcds - 1) / kXcds) * kXcds;
     hipLaunchKernelGGL(product_kernel<CT>, dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices);
     return hip_status(hipGetLastError());
 }
@@ -406,7 +422,7 @@ int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
 // Slices of equal width: as few as fit, then as narrow as those need.
 int launch_slices(const ProductArgs &a, int most, hipStream_t s) {
     const int cols = (a.N + 15) / 16;
-    while (most > 1 && static_cast<size_t>(16 * most) * lds_row(a.blocks) * sizeof(uint16_t) > kLds) --most;
+    while (most > 1 && static_cast<size_t>(most) * lds_tile(a.blocks) * sizeof(uint16_t) > kLds) --most;
     const int slices = (cols + most - 1) / most;
     switch ((cols + slices - 1) / slices) {
         case 1: return launch_product<1>(a, slices, s);

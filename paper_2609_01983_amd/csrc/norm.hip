@@ -557,7 +557,7 @@ void with_forward_shape(int32_t F, Fn f) {
     else if (F <= 1024) shape<128, 2>(f);
     else if (F <= 1536) shape<128, 3>(f);
     else if (F <= 2048) shape<256, 2>(f);
-    else if (F <= 3072) shape<256, 3>(f);
+    else if (F <= 4 * 256 * 3) shape<256, 3>(f);
     else if (F <= 4096) shape<512, 2>(f);
     else if (F <= 6144) shape<512, 3>(f);
     else shape<512, 4>(f);
@@ -579,7 +579,7 @@ void with_backward_shape(int32_t F, Fn f) {
     else if (F <= 1024) shape<256, 1>(f);
     else if (F <= 1536) shape<128, 3>(f);
     else if (F <= 2048) shape<256, 2>(f);
-    else if (F <= 3072) shape<256, 3>(f);
+    else if (F <= 4 * 256 * 3) shape<256, 3>(f);
     else if (F <= 4096) shape<1024, 1>(f);
     else if (F <= 6144) shape<512, 3>(f);
     else shape<512, 4>(f);
