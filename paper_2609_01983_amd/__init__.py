@@ -737,12 +737,15 @@ def distill_xent(Y, ids, teacher, labels=None, temperature=1.0, soft_scale=None,
     if labels is not None:
         _shaped(labels, torch.int32, (n,), "labels")
     s = _queue(stream, Y, ids, teacher, labels, G, loss, workspace)
-    if soft_scale is None:
-        kept = (ids >= 0) & (ids < C) & (teacher != float("-inf"))
-        soft_scale = 1.0 / max(1, int(kept.any(1).sum().item()))
-    if hard_scale is None:
-        hard_scale = 0.0 if labels is None else \
-            1.0 / max(1, int(((labels >= 0) & (labels < C)).sum().item()))
+    if hard_scale is None and labels is None:
+        hard_scale = 0.0
+    if soft_scale is None or hard_scale is None:
+        with torch.cuda.stream(stream):              # the operands are ready on the call's stream
+            if soft_scale is None:
+                kept = (ids >= 0) & (ids < C) & (teacher != float("-inf"))
+                soft_scale = 1.0 / max(1, int(kept.any(1).sum().item()))
+            if hard_scale is None:
+                hard_scale = 1.0 / max(1, int(((labels >= 0) & (labels < C)).sum().item()))
     gdt = torch.float32
     if grad_bf16:
         gdt = torch.bfloat16

@@ -183,6 +183,23 @@ def test_default_scales(dg, device):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_default_scales_wait_for_the_stream(dg, device):
+    Y, ids, teacher, labels = _inputs(device, 60, 10, 3)
+    want = dg.distill_xent(Y, ids, teacher, labels)
+    late, late_labels = torch.full_like(ids, -1), torch.full_like(labels, -1)
+    busy = torch.eye(4096, device=device)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy = busy @ busy
+        late.copy_(ids)
+        late_labels.copy_(labels)
+    got = dg.distill_xent(Y, late, teacher, late_labels, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_views_streams_and_graphs(dg, device):
     for n, C in ((37, 45), (19, 700), (5, 30001)):
         Y, ids, teacher, labels = _inputs(device, n, C, 6)
