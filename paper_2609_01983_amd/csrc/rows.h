@@ -30,7 +30,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_window(const void *base, i
                                              static_cast<int>(elems * kSize), 0x00020000);
 }
 
-constexpr uint32_t kNoQuad = 0x3FFFFFFFu;            // an element offset past every window
+constexpr uint32_t kNoQuad = 0x3FFFFF00u;            // an element offset past every window, also in bytes and with a quad's places
 constexpr int kNonTemporal = 2;                      // a buffer access's hint
 
 // A lane's four consecutive columns of a row of F that starts at element `row_at` of its window.
