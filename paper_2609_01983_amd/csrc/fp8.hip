@@ -239,16 +239,20 @@ __host__ __device__ __forceinline__ int lds_tile(int blocks) { return blocks * k
 // The slices of a row tile run at one time on one XCD and read its X from that L2: workgroups go to
 // the XCDs in turn, so number w has XCD w % 8, slice w / 8 % slices, and the tiles w / (8 slices) 8 + w % 8, ...
 // (with the slices of a tile on different XCDs, X came from beyond the L2 once a slice: 2^20 rows
-// 512 -> 512 933 us against 822, 1,024 -> 256 1,120 against 842).
+// 512 -> 512 933 us against 822, 1,024 -> 256 1,120 against 842).  `side` is that 8, or 1 where the
+// tiles are too few to give each XCD its share.
 constexpr int kXcds = 8;
 constexpr int kMostBlocks = 8;                       // F_in up to 1,024
 template <int CT>
-__global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_t slices) {
+__global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_t slices, int32_t side) {
     extern __shared__ uint4 lds[];
     __bf16 *w = reinterpret_cast<__bf16 *>(lds);
     const int tile_elems = lds_tile(a.blocks);
-    const int c0 = static_cast<int>(blockIdx.x) / kXcds % slices * 16 * CT;
+    const int c0 = static_cast<int>(blockIdx.x) / side % slices * 16 * CT;
     const int64_t stride = gridDim.x / slices;
+    const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
+    int64_t tile = static_cast<int64_t>(blockIdx.x) / (side * slices) * side + blockIdx.x % side;
+    if (tile >= tiles) return;                       // the grid has a whole number of tiles for each XCD
     // W of the columns [c0, c0 + 16 CT), zeros past F_out and past F_in: 16 bytes of W8 are two
     // steps of a lane group
     const int per_row = a.blocks * kBlock / 16;
@@ -275,7 +279,6 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_
     const int r = lane & 15, g = lane >> 4;
     // the columns' scales: tiles of 16 columns from `turn` on are in the next block of 128
     const int turn = (kBlock - c0 % kBlock) / 16;
-    const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
     const int last = min(a.N, c0 + 16 * CT);
 
     // A tile's rows as windows, from block b on: rows behind the last are zeros, and lanes address
@@ -298,7 +301,6 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_
             sn[t] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ws, at[t] * a.blocks * 4, 0, 0));
         }
     };
-    int64_t tile = static_cast<int64_t>(blockIdx.x) / (kXcds * slices) * kXcds + blockIdx.x % kXcds;
     request(tile, 0);
     for (; tile < tiles; tile += stride) {
         f32x4 acc[kRowTiles][CT];
@@ -405,6 +407,11 @@ constexpr size_t kLds = 160 * 1024 - 2 * kMostBlocks * sizeof(float);   // besid
 // 2^21 384 -> 128 406, 414; 2^21 512 -> 128 451, 481; 2^20 1,024 -> 256 839, 903.
 inline int64_t over(size_t lds) { return lds <= 64 * 1024 ? 16 : 2; }
 
+// Row tiles from which the slices of one share an XCD.  Fewer leave XCDs idle or with an uneven share (us side
+// by side and over the XCDs in turn, 1,024 -> 1,024: 1,000 rows 27.8 and 15.8, 16,000 rows 63.6 and 62.2;
+// past that the shared L2 wins).
+constexpr int64_t kSideTiles = 64;
+
 template <int CT>
 int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
     const size_t lds = static_cast<size_t>(CT) * lds_tile(a.blocks) * sizeof(uint16_t);
@@ -414,8 +421,9 @@ int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
     // registers: up to 128 a thread for four tiles of columns, hence two workgroups a CU
     const int64_t resident = static_cast<int64_t>(device_cus()) * (CT <= 4 && 2 * lds <= kLds ? 2 : 1);
     // row tiles at a time, a whole number for each XCD
-    const int64_t per = std::max<int64_t>(1, (std::min<int64_t>(tiles, over(lds) * resident / slices) + kXcds - 1) / kXcds) * kXcds;
-    hipLaunchKernelGGL(product_kernel<CT>, dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices);
+    const int side = tiles >= kSideTiles ? kXcds : 1;
+    const int64_t per = std::max<int64_t>(1, (std::min<int64_t>(tiles, over(lds) * resident / slices) + side - 1) / side) * side;
+    hipLaunchKernelGGL(product_kernel<CT>, dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices, side);
     return hip_status(hipGetLastError());
 }
 
