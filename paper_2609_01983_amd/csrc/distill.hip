@@ -25,6 +25,7 @@ namespace dgc {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMaxBlocks = 8192;                     // workgroups, hence partial sums of the loss
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr double kLn2 = 0.69314718055994530942;
 
@@ -688,27 +689,31 @@ __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
 }
 
 // loss = {soft + hard, soft, hard} from the workgroups' sums, by a fixed tree.
-__global__ __launch_bounds__(kThreads) void distill_loss_kernel(const double *__restrict__ partial, int32_t count,
-                                                                double soft, double hard, float *__restrict__ loss) {
-    __shared__ double sh[2][kThreads];
+// 16 bytes a load, eight in flight a thread (8,192 workgroups: 13 us with one load at a time).
+constexpr int kLossThreads = 1024;
+typedef double f64x2 __attribute__((ext_vector_type(2)));
+__global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(const double *__restrict__ partial, int32_t count,
+                                                                    double soft, double hard, float *__restrict__ loss) {
+    __shared__ f64x2 sh[kLossThreads];
     const int t = threadIdx.x;
-    double a = 0.0, b = 0.0;
-    for (int i = t; i < count; i += kThreads) {
-        a += partial[2 * i];
-        b += partial[2 * i + 1];
+    constexpr int kLoads = kMaxBlocks / kLossThreads;
+    f64x2 v[kLoads], sum = {0.0, 0.0};
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+        const int i = t + j * kLossThreads;
+        v[j] = i < count ? reinterpret_cast<const f64x2 *>(partial)[i] : f64x2{0.0, 0.0};
     }
-    sh[0][t] = a;
-    sh[1][t] = b;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) sum += v[j];
+    sh[t] = sum;
     __syncthreads();
-    for (int h = kThreads / 2; h > 0; h >>= 1) {
-        if (t < h) {
-            sh[0][t] += sh[0][t + h];
-            sh[1][t] += sh[1][t + h];
-        }
+#pragma unroll
+    for (int h = kLossThreads / 2; h > 0; h >>= 1) {
+        if (t < h) sh[t] += sh[t + h];
         __syncthreads();
     }
     if (t == 0) {
-        const double s = soft * kLn2 * sh[0][0], r = hard * kLn2 * sh[1][0];
+        const double s = soft * kLn2 * sh[0][0], r = hard * kLn2 * sh[0][1];
         loss[0] = static_cast<float>(s + r);
         loss[1] = static_cast<float>(s);
         loss[2] = static_cast<float>(r);
@@ -718,7 +723,6 @@ __global__ __launch_bounds__(kThreads) void distill_loss_kernel(const double *__
 // ------------------------------------------------------------------ dispatch
 
 constexpr int kRowClasses = 1024;                    // widest row of distill_rows_kernel
-constexpr int kMaxBlocks = 8192;
 constexpr int kSplitBlocks = 512;                    // workgroups that fill the chip (two a CU)
 constexpr int kMinSplit = 4096;                      // classes a split has at least
 
@@ -810,7 +814,7 @@ int launch_distill(const void *Y, bool y_bf16, const int32_t *ids, const void *t
     const int blocks = y_bf16 ? launch_any<true>(a, t_bf16, s) : launch_any<false>(a, t_bf16, s);
     const int st = hip_status(hipGetLastError());
     if (st) return st;
-    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kThreads), 0, s, partial, blocks,
+    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kLossThreads), 0, s, partial, blocks,
                        static_cast<double>(soft) * T * T, static_cast<double>(hard), loss);
     return hip_status(hipGetLastError());
 }
