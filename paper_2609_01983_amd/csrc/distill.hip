@@ -642,13 +642,16 @@ __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
         if (splits == 1) {
             s = sweep_stats<YBF, ODD>(a, row, 0, a.C, labeled && a.temp_a != kLog2e, sh, turn);
         } else {
-            s = RowStats{-FLT_MAX, 0.f, 0.f};
-            const float *in = a.stats + row * splits * 3;
-            for (int k = 0; k < splits; ++k) s.m = fmaxf(s.m, in[3 * k]);
-            for (int k = 0; k < splits; ++k) {
-                s.st = fmaf(in[3 * k + 1], exp2_fast((in[3 * k] - s.m) * a.temp_a), s.st);
-                s.s1 = fmaf(in[3 * k + 2], exp2_fast((in[3 * k] - s.m) * kLog2e), s.s1);
-            }
+            // a split a thread (one after the other they took most of a single row's time)
+            const bool there = static_cast<int>(threadIdx.x) < splits;
+            const float *in = a.stats + (row * splits + (there ? threadIdx.x : 0)) * 3;
+            const float m = there ? in[0] : -FLT_MAX;
+            float all[1] = {m};
+            row_reduce<kSweep>(all, MaxOp(), sh, turn);
+            float sums[2] = {there ? in[1] * exp2_fast((m - all[0]) * a.temp_a) : 0.f,
+                             there ? in[2] * exp2_fast((m - all[0]) * kLog2e) : 0.f};
+            row_reduce<kSweep>(sums, AddOp(), sh, turn);
+            s = RowStats{all[0], sums[0], sums[1]};
         }
         const RowGrad<ODD> grad(a, s, en.taught, lab);
         const __amdgpu_buffer_rsrc_t wy = row_window<YBF>(a.Y, row * a.C, a.C);
@@ -724,6 +727,7 @@ __global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(const double
 
 constexpr int kRowClasses = 1024;                    // widest row of distill_rows_kernel
 constexpr int kSplitBlocks = 512;                    // workgroups that fill the chip (two a CU)
+static_assert(kSplitBlocks <= kSweep, "a row's splits are joined by one thread each");
 constexpr int kMinSplit = 4096;                      // classes a split has at least
 
 int splits_of(int32_t n, int32_t C) {
