@@ -76,10 +76,14 @@ struct Entries {
     float entropy;                   // this thread's share of sum p log2(p sum)
     bool taught;
 
+    // no entry: class -1 and logit -inf
     __device__ __forceinline__ void fetch(int64_t k, int &i, float &x) const {
         i = ids[at + k];
         x = teacher_at<TBF>(teacher, at + k);
-        if (i < 0 || i >= C) x = -INFINITY;
+        if (i < 0 || i >= C || x == -INFINITY) {
+            i = -1;
+            x = -INFINITY;
+        }
     }
     __device__ __forceinline__ void load(const Args &a, int64_t row, int lane) {
         ids = a.ids;
@@ -170,7 +174,7 @@ struct Entries {
             twice = (TPR == 64 ? all : all >> first & ((uint64_t{1} << (TPR & 63)) - 1)) != 0;
         }
         if (twice) {                                     // the same for all threads of the row
-            clear(tile, c0, c1, a);
+            clear(tile, c0, c1);
             row_sync<TPR>();
             if (l == 0) {
                 for (int k = 0; k < K; ++k) {
@@ -184,10 +188,14 @@ struct Entries {
             row_sync<TPR>();
         }
     }
-    __device__ __forceinline__ void clear(float *tile, int c0, int c1, float a) const {
-        each(a, [&](int i, float e) {
-            if (!(e == 0.f) && static_cast<uint32_t>(i - c0) < static_cast<uint32_t>(c1 - c0)) tile[i - c0] = 0.f;
-        });
+    __device__ __forceinline__ void clear(float *tile, int c0, int c1) const {
+        // whatever the p: a row with an infinity or a NaN has NaN where the exponential is 0
+        auto one = [&](int i) {
+            if (static_cast<uint32_t>(i - c0) < static_cast<uint32_t>(c1 - c0)) tile[i - c0] = 0.f;
+        };
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) one(id[h]);
+        others([&](int i, float) { one(i); });
     }
 };
 
@@ -218,7 +226,9 @@ __device__ __forceinline__ void write_partial(double soft, double hard, double *
 }
 
 // Rows whose logits stay in the registers of their TPR threads, Q quads each.  YBF, TBF: the
-// logits, the teacher's are bfloat16.
+// logits, the teacher's are bfloat16.  Measured: 2^22 x 64 with 16 entries a row, T = 4 and labels, 2.7 GB in 527 us,
+// 5.1 TB/s; 30,007 x 47 with 8 entries 13 MB in 7.4 us.  Short rows are bound by the vector unit as much
+// as by memory: two exponentials a logit, three reductions a row and the entries' own work.
 template <int TPR, int Q, bool YBF, bool TBF>
 __global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_rows_kernel(Args a) {
     constexpr bool TINY = TPR == 1;
@@ -325,7 +335,7 @@ __global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_rows_kern
                 }
             }
             row_sync<TPR>();                             // P is read before it is cleared
-            en.clear(tile, 0, C, a.temp_a);
+            en.clear(tile, 0, C);
             if constexpr (TPR <= 64) row_sync<TPR>();    // else the next row's reductions come between
             soft += en.entropy - static_cast<double>(a.temp_a) * loss_s;
             if (l == 0) soft += __builtin_amdgcn_logf(s[1]) - __builtin_amdgcn_logf(s[0]);
@@ -448,6 +458,8 @@ __device__ __forceinline__ void put_zeros(const Args &a, int64_t row, int c0, in
 }
 
 // A row that QUADS quads of THREADS threads hold.  The second bound keeps a CU's registers full.
+// Measured, 16 entries a row, T = 2, labels, float32 / bfloat16: 16,384 x 8,192 192 / 130 us (5.6 / 4.1 TB/s), 8,192 x 16,384
+// 218 / 124 us, 65,536 x 2,000 223 / 158 us; bfloat16 is bound by its four exponentials a logit.
 template <bool YBF, bool TBF, bool ODD, int THREADS, int QUADS>
 __global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(Args a) {
     __shared__ row_f32x4 sh[row_reduce_quads<THREADS>()];
@@ -527,7 +539,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(Args a) {
                     }
                 if (en.taught) {
                     __syncthreads();
-                    en.clear(tile, c, min(C, c + kPiece), a.temp_a);
+                    en.clear(tile, c, min(C, c + kPiece));
                     __syncthreads();
                 }
             }
@@ -588,7 +600,8 @@ __device__ __forceinline__ RowStats sweep_stats(const Args &a, int64_t row, int 
 // Classes of a split: whole quads.
 __host__ __device__ __forceinline__ int split_width(int C, int splits) { return ((C + splits - 1) / splits + 3) / 4 * 4; }
 
-// First launch of split rows: statistics of split blockIdx.x of row blockIdx.y.
+// First launch of split rows: statistics of split blockIdx.x of row blockIdx.y.  Both launches and the
+// loss: 1 x 1,000,000 18.7 us, 16 x 131,072 20.4 us; with one workgroup a row the chip would stand idle.
 template <bool YBF, bool ODD>
 __global__ __launch_bounds__(kSweep) void distill_stats_kernel(Args a) {
     __shared__ row_f32x4 sh[row_reduce_quads<kSweep>()];
@@ -607,7 +620,8 @@ __global__ __launch_bounds__(kSweep) void distill_stats_kernel(Args a) {
 }
 
 // The gradient of rows of any length.  With one split the workgroup sweeps its rows' statistics
-// itself; else they come from `stats`.
+// itself; else they come from `stats`.  Measured: 4,095 x 131,072 bfloat16, T = 1, 64 entries: 2.15 GB (and a second
+// reading of Y, mostly from the caches) in 480 us, 4.5 TB/s.
 template <bool YBF, bool TBF, bool ODD>
 __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
     constexpr int kPiece = 4 * kSweep * kSweepQ;
@@ -672,7 +686,7 @@ __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
             }
             if (en.taught) {
                 __syncthreads();
-                en.clear(tile, c, min(c1, c + kPiece), a.temp_a);
+                en.clear(tile, c, min(c1, c + kPiece));
                 __syncthreads();
             }
         }
@@ -726,12 +740,16 @@ __global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(const double
 // ------------------------------------------------------------------ dispatch
 
 constexpr int kRowClasses = 1024;                    // widest row of distill_rows_kernel
+constexpr int kHeldClasses = 32768;                  // widest row of distill_held_kernel
 constexpr int kSplitBlocks = 512;                    // workgroups that fill the chip (two a CU)
 static_assert(kSplitBlocks <= kSweep, "a row's splits are joined by one thread each");
 constexpr int kMinSplit = 4096;                      // classes a split has at least
 
+// Rows that a workgroup can hold are not split (us split and held, 1 and 255 rows of 32,768 bfloat16: 20.5, 17.1 and
+// 21.8, 21.1); longer ones where the rows are few (split and swept whole, 131,072 bfloat16: 1 row 20.8, 35.8; 100
+// rows 29.2, 39.5; 200 rows 42.7, 39.8).
 int splits_of(int32_t n, int32_t C) {
-    if (n >= kSplitBlocks / 2) return 1;
+    if (C <= kHeldClasses || n > kSplitBlocks / 4) return 1;
     const int want = kSplitBlocks / n, most = (C + kMinSplit - 1) / kMinSplit;
     return std::max(1, std::min(want, most));
 }
@@ -763,15 +781,16 @@ int launch_held(const Args &a, bool tbf, hipStream_t s) {
 // a row from the caches costs (2^28 elements: C = 65,536 swept 457 / 297, held by 1,024 threads 582 / 360).
 template <bool YBF, bool ODD>
 int launch_long(const Args &a, bool tbf, hipStream_t s) {
-    const int C = a.C, splits = splits_of(a.n, C);
-    if (splits == 1) {
+    const int C = a.C;
+    if (C <= kHeldClasses) {
         if (C <= 2048) return launch_held<YBF, ODD, 64, 8>(a, tbf, s);
         // (float32 / bfloat16 at C = 3,000: (256, 4) 212 / 165, (128, 8) 227 / 140)
         if (C <= 4096) return launch_held<YBF, ODD, YBF ? 128 : 256, YBF ? 8 : 4>(a, tbf, s);
         if (C <= 8192) return launch_held<YBF, ODD, 256, 8>(a, tbf, s);
         if (C <= 16384) return launch_held<YBF, ODD, 256, 16>(a, tbf, s);
-        if (C <= 32768) return launch_held<YBF, ODD, 512, 16>(a, tbf, s);
+        return launch_held<YBF, ODD, 512, 16>(a, tbf, s);
     }
+    const int splits = splits_of(a.n, C);
     const dim3 grid(splits, row_blocks(a.n, 1));
     if (splits > 1) hipLaunchKernelGGL((distill_stats_kernel<YBF, ODD>), grid, dim3(kSweep), 0, s, a);
     if (tbf) hipLaunchKernelGGL((distill_sweep_kernel<YBF, true, ODD>), grid, dim3(kSweep), 0, s, a);
@@ -804,7 +823,7 @@ int launch_any(const Args &a, bool tbf, hipStream_t s) {
 size_t distill_workspace_bytes(int32_t n, int32_t C) {
     // partial sums of the loss, then the statistics of split rows (rows that are split are few)
     size_t bytes = 2 * sizeof(double) * kMaxBlocks;
-    if (C > kRowClasses && splits_of(n, C) > 1) bytes += sizeof(float) * 3 * static_cast<size_t>(n) * splits_of(n, C);
+    if (splits_of(n, C) > 1) bytes += sizeof(float) * 3 * static_cast<size_t>(n) * splits_of(n, C);
     return (bytes + 255) / 256 * 256;
 }
 

@@ -108,6 +108,12 @@ def test_many_rows_and_long_ones(dg, device, n, C):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("n,C", [(1, 32768), (128, 32768), (128, 32769), (129, 32769), (130, 40000), (127, 40000)])
+def test_around_the_longest_held_and_the_last_split_rows(dg, device, n, C, y):
+    _check(dg, *_inputs(device, n, C, 8, y=y), T=2.0, soft=1.0 / n, hard=1.0 / n)
+
+
 @pytest.mark.parametrize("C", [2, 40, 130, 700, 3000, 12000, 50000])
 def test_masked_infinite_and_nan_logits(dg, device, C):
     Y, ids, teacher, labels = _inputs(device, 24, C, 6, missing=0.0)
@@ -145,6 +151,29 @@ def test_masked_infinite_and_nan_logits(dg, device, C):
                                labels[good].contiguous(), temperature=2.0, soft_scale=0.3, hard_scale=0.2)
     assert torch.allclose(G[good], alone, rtol=1e-5, atol=1e-9)
     assert torch.equal(G[9], torch.zeros_like(G[9]))
+
+
+@pytest.mark.parametrize("n,C", [(300000, 5), (70000, 300), (33000, 600), (9000, 1100), (9000, 5001), (300, 20001), (8300, 33000)])
+def test_rows_beside_a_teacher_that_is_not_finite(dg, device, n, C):
+    """Rows whose teacher has a +infinity or a NaN leave the rows behind them as they were, and have NaN at
+    the classes of their entries only (an entry of -infinity is none)."""
+    g = torch.Generator(device=device).manual_seed(C)
+    Y = torch.randn(n, C, device=device, generator=g)
+    K = 5
+    start = torch.randint(0, C, (n, 1), device=device, generator=g)
+    ids = ((start + torch.arange(K, device=device) * (C // K)) % C).int()     # distinct
+    teacher = torch.randn(n, K, device=device, generator=g)
+    want, _ = dg.distill_xent(Y, ids, teacher, temperature=2.0, soft_scale=0.1)
+    bad = torch.arange(n, device=device) % 7 == 3
+    poisoned = teacher.clone()
+    poisoned[bad, 1] = float("inf")
+    poisoned[3, 1] = float("nan")
+    poisoned[bad, 2] = -float("inf")
+    got, loss = dg.distill_xent(Y, ids, poisoned, temperature=2.0, soft_scale=0.1)
+    assert torch.equal(got[~bad], want[~bad])
+    nan = torch.zeros(int(bad.sum()), C, dtype=torch.bool, device=device)
+    nan.scatter_(1, ids[bad][:, [0, 1, 3, 4]].long(), True)
+    assert torch.equal(got[bad].isnan(), nan) and loss[0].isnan()
 
 
 def test_gradient_against_differences(dg, device):
