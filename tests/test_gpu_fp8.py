@@ -156,7 +156,7 @@ def test_update_fp8(dg, device, n, F_in, F_out, out_bf16):
 
 # rows around the point from which the slices of a row tile share an XCD, in numbers that are no
 # multiple of eight tiles
-@pytest.mark.parametrize("n", [1793, 16128, 16640, 18433])
+@pytest.mark.parametrize("n", [500, 512, 1793, 16128, 16640, 18433])
 @pytest.mark.parametrize("F_in,F_out", [(256, 300), (1024, 161)])
 def test_shared_slices(dg, device, n, F_in, F_out):
     _check(dg, _operands(device, n, F_in, F_out))
