@@ -8,7 +8,9 @@
  * the update phase X W of a layer (Sec. 1), also fused with the aggregation of the
  * layer before it; for training, the loss gradient and
  * the backward products of a layer; the values of other aggregators on the same
- * structure; and plans saved and loaded across runs.
+ * structure; and plans saved and loaded across runs.  For deep GCNs: the norms, gate and
+ * residual scale between two blocks and their gradients, the loss of a student
+ * against its teacher's top logits, and the update phase from 8-bit operands.
  *
  * Conventions for every entry point
  *   - Pointers named *_h are host memory; every other array pointer is device
@@ -450,8 +452,8 @@ int dualgcn_backward_data(const void *G, const float *W, const void *M, float *d
 
 /*
  * The norms of a residual block.  The vectors are float32[F] (device); a NULL weight is all
- * ones, a NULL bias all zeros; only layer norms take biases.  gate goes by the flags (at most one of the three kinds; NULL
- * without any).  eps is at least 2^-126 and scale finite.
+ * ones, a NULL bias all zeros; only layer norms take biases.  gate goes by the flags (at most
+ * one of the three kinds; NULL without any).  eps is at least 2^-126 and scale finite.
  */
 typedef struct dualgcn_norm {
     const float *post_weight, *post_bias;   /* the norm after the block (DUALGCN_NORM_POST) */
@@ -508,7 +510,8 @@ int dualgcn_norm_residual_backward_workspace(int32_t n, int32_t F, size_t *bytes
  * The rows' statistics are computed again from Rn and B.  Sums over the rows are formed in
  * float32 by each workgroup and joined in float64 in a fixed order (in `workspace`, device,
  * 256-byte aligned, at least dualgcn_norm_residual_backward_workspace bytes), so results do not
- * depend on timing.  Outputs overlap nothing but as said for dR.  Limits as for
+ * depend on timing.  Calls that may run at the same time need a workspace each.  Outputs overlap
+ * nothing but as said for dR.  Limits as for
  * dualgcn_norm_residual.  DUALGCN_OUT_BF16 has no meaning here and is ignored.  Asynchronous.
  */
 int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, const void *B, const void *dZ,
@@ -546,7 +549,8 @@ int dualgcn_distill_workspace(int32_t n, int32_t C, int32_t K, size_t *bytes);
  * float32 arithmetic, the loss joined in float64 in a fixed order; G does not depend on timing.
  * n >= 1, 1 <= C < 2^20, 1 <= K <= 4096 (larger: DUALGCN_ERR_UNSUPPORTED), temperature in
  * [2^-14, 2^14], finite scales; outputs overlap nothing.  `workspace` (device, 256-byte aligned)
- * holds at least dualgcn_distill_workspace bytes.  Asynchronous.
+ * holds at least dualgcn_distill_workspace bytes; calls that may run at the same time need one
+ * each.  Asynchronous.
  */
 int dualgcn_distill_xent(const void *Y, const int32_t *ids, const void *teacher, const int32_t *labels,
                          int32_t n, int32_t C, int32_t K, float temperature, float soft_scale,
@@ -566,9 +570,9 @@ int dualgcn_distill_xent(const void *Y, const int32_t *ids, const void *teacher,
  * into Q (device, n x F bytes) and scales (device, float32[n][ceil(F / 128)]), a scale for each
  * 128 consecutive features of a row (the last block of a row may be shorter).  A scale is the
  * least power of two, 2^-126 or more, that brings the block's largest finite magnitude to 448 or
- * below (1 for a block without one), so that the division is exact; elements are rounded once, to nearest
- * even.  Infinities and NaN become NaN.  n >= 1, 1 <= F < 2^20 (larger: DUALGCN_ERR_UNSUPPORTED).
- * Asynchronous.
+ * below (1 for a block without one), so that the division is exact; elements are rounded once, to
+ * nearest even.  Infinities and NaN become NaN.  n >= 1, 1 <= F < 2^20 (larger:
+ * DUALGCN_ERR_UNSUPPORTED).  Asynchronous.
  *
  * dualgcn_quantize_weight_fp8 -- W (device, float32 F_in x F_out row-major) with a scale for each
  * 128 x 128 block, in the layout dualgcn_update_fp8 reads: with `transpose` not 0, Q is
@@ -590,9 +594,9 @@ int dualgcn_quantize_weight_fp8(const float *W, int32_t F_in, int32_t F_out, int
  * F_out x F_in row-major: W transposed) with sw (float32[ceil(F_out / 128)][ceil(F_in / 128)], one
  * for each 128 x 128 block); T (device, n x F_out row-major, float32, or bfloat16 with
  * DUALGCN_OUT_BF16).  The scales may be any float32 numbers.  Products of a block (of the e4m3
- * numbers widened to bfloat16, which is exact) are summed by the matrix cores in float32, multiplied by the two scales and added in float32, block after
- * block, in an order that depends on the shape only.  The gradient G W^T is the same call on a
- * quantised G and W not transposed.
+ * numbers widened to bfloat16, which is exact) are summed by the matrix cores in float32,
+ * multiplied by the two scales and added in float32, block after block, in an order that depends
+ * on the shape only.  The gradient G W^T is the same call on a quantised G and W not transposed.
  * n >= 1; F_in a multiple of 16, at most 1024; 1 <= F_out <= 65536 (else
  * DUALGCN_ERR_UNSUPPORTED); X and W 16-byte aligned; T overlaps no operand.  No workspace.
  * Asynchronous.

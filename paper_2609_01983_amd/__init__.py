@@ -9,6 +9,12 @@ is missing, importing this package raises ImportError: there is no fallback.
     Y = spmm(plan, X)                           # Y = A X
     T = update(X, W)                            # T = X W, bf16 matrix cores
     H = gcn_layer(plan, X, W, relu=True)        # H = relu(A (X W)), X W in bf16 MFMA
+
+Between the blocks of a deep GCN, in training from a teacher, and in serving from 8 bits:
+
+    R, Z = norm_residual(R, B, gate=gate)       # R + gate * norm(B), and its norm
+    G, loss = distill_xent(Y, ids, teacher)     # against the teacher's top logits, and dloss/dY
+    T = update_fp8(*quantize_fp8(Z), *W8)       # T = Z W, e4m3 with a scale for each 128
 """
 import collections
 import ctypes

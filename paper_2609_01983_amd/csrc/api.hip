@@ -7,6 +7,7 @@
 #include <string>
 #include <new>
 
+#include "deep.h"
 #include "internal.h"
 
 namespace dgc {

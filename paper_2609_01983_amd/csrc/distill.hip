@@ -620,8 +620,8 @@ __global__ __launch_bounds__(kSweep) void distill_stats_kernel(Args a) {
 }
 
 // The gradient of rows of any length.  With one split the workgroup sweeps its rows' statistics
-// itself; else they come from `stats`.  Measured: 4,095 x 131,072 bfloat16, T = 1, 64 entries: 2.15 GB (and a second
-// reading of Y, mostly from the caches) in 480 us, 4.5 TB/s.
+// itself; else they come from `stats`.  Measured: 4,095 x 131,072 bfloat16, T = 1, 64 entries: 2.15 GB in 479 us,
+// 4.5 TB/s, and a second reading of Y, 1.07 GB, from beyond the L2 and for the most part not from HBM.
 template <bool YBF, bool TBF, bool ODD>
 __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
     constexpr int kPiece = 4 * kSweep * kSweepQ;

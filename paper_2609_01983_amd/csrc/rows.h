@@ -3,7 +3,7 @@
 // over the 2^k lanes that share a row.
 #pragma once
 
-#include "internal.h"
+#include "deep.h"
 
 #include <type_traits>
 
