@@ -251,7 +251,7 @@ __host__ __device__ __forceinline__ int lds_tile(int blocks) { return blocks * k
 // tiles are too few to give each XCD its share.
 constexpr int kXcds = 8;
 constexpr int kMostBlocks = 8;                       // F_in up to 1,024
-template <int CT>
+template <int CT, bool ALONE>
 __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_t slices, int32_t side) {
     extern __shared__ uint4 lds[];
     __bf16 *w = reinterpret_cast<__bf16 *>(lds);
@@ -328,26 +328,31 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_
             const bool more = b + 1 < a.blocks;
             request(more ? tile : tile + stride, more ? b + 1 : 0);
             const float sw0 = column_scales[0][b], sw1 = column_scales[1][b];
+            auto multiply = [&](auto steps) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const __bf16 *p = w + c * tile_elems + b * kSteps * 512 + lane * 8;
-                f32x4 s[kRowTiles];
+                for (int c = 0; c < CT; ++c) {
+                    const __bf16 *p = w + c * tile_elems + b * kSteps * 512 + lane * 8;
+                    f32x4 s[kRowTiles];
 #pragma unroll
-                for (int t = 0; t < kRowTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int t = 0; t < kRowTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(p + 512 * k);
+                    for (int k = 0; k < decltype(steps)::value; ++k) {
+                        const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(p + 512 * k);
 #pragma unroll
-                    for (int t = 0; t < kRowTiles; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[t][k], s[t], 0, 0, 0);
+                        for (int t = 0; t < kRowTiles; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[t][k], s[t], 0, 0, 0);
+                    }
+                    const float swc = c < turn ? sw0 : sw1;
+#pragma unroll
+                    for (int t = 0; t < kRowTiles; ++t) {
+                        const float f = sc[t] * swc;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][c][i] = fmaf(f, s[t][i], acc[t][c][i]);
+                    }
                 }
-                const float swc = c < turn ? sw0 : sw1;
-#pragma unroll
-                for (int t = 0; t < kRowTiles; ++t) {
-                    const float f = sc[t] * swc;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t][c][i] = fmaf(f, s[t][i], acc[t][c][i]);
-                }
-            }
+            };
+            // a last block of up to 64 elements has them all in its first two steps
+            if (ALONE && a.K - b * kBlock <= 64) multiply(std::integral_constant<int, kSteps / 2>());
+            else multiply(std::integral_constant<int, kSteps>());
         }
         const int64_t row0 = tile * kRowsPerBlock;
         const int64_t elems = min(static_cast<int64_t>(kRowsPerBlock), a.n - row0) * a.N;
@@ -421,10 +426,10 @@ inline int64_t over(size_t lds) { return lds <= 64 * 1024 ? 16 : 2; }
 // past that the shared L2 wins).
 constexpr int64_t kSideTiles = 64;
 
-template <int CT>
+template <int CT, bool ALONE>
 int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
     const size_t lds = static_cast<size_t>(CT) * lds_tile(a.blocks) * sizeof(uint16_t);
-    const int st = allow_lds(reinterpret_cast<const void *>(&product_kernel<CT>), lds);
+    const int st = allow_lds(reinterpret_cast<const void *>(&product_kernel<CT, ALONE>), lds);
     if (st) return st;
     const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
     // registers: up to 128 a thread for four tiles of columns, hence two workgroups a CU
@@ -432,8 +437,20 @@ int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
     // row tiles at a time, a whole number for each XCD
     const int side = tiles >= kSideTiles ? kXcds : 1;
     const int64_t per = std::max<int64_t>(1, (std::min<int64_t>(tiles, over(lds) * resident / slices) + side - 1) / side) * side;
-    hipLaunchKernelGGL(product_kernel<CT>, dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices, side);
+    hipLaunchKernelGGL((product_kernel<CT, ALONE>), dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices, side);
     return hip_status(hipGetLastError());
+}
+
+// ALONE: W leaves no room for a second workgroup on a CU, so the kernel may take all registers, which the
+// compiler fills with W's fragments ahead of their products, and a short last block is skipped by half (us
+// ALONE and not: 200,003 rows 528 -> 200 92, 98; 512 -> 200 73, 78; 2^20 1,024 -> 256 804, 820, 512 -> 512 830, 822; with
+// room for two 2^22 256 -> 128 669, 649; 2^20 128 -> 64 86, 80).
+template <int CT>
+int launch_tiles(const ProductArgs &a, int slices, hipStream_t s) {
+    [[maybe_unused]] const bool alone = 2 * static_cast<size_t>(CT) * lds_tile(a.blocks) * sizeof(uint16_t) > kLds;
+    if constexpr (CT > 2)                            // (two tiles of 1,024 leave room)
+        if (alone) return launch_product<CT, true>(a, slices, s);
+    return launch_product<CT, false>(a, slices, s);
 }
 
 // Slices of equal width: as few as fit, then as narrow as those need.
@@ -442,14 +459,14 @@ int launch_slices(const ProductArgs &a, int most, hipStream_t s) {
     while (most > 1 && static_cast<size_t>(most) * lds_tile(a.blocks) * sizeof(uint16_t) > kLds) --most;
     const int slices = (cols + most - 1) / most;
     switch ((cols + slices - 1) / slices) {
-        case 1: return launch_product<1>(a, slices, s);
-        case 2: return launch_product<2>(a, slices, s);
-        case 3: return launch_product<3>(a, slices, s);
-        case 4: return launch_product<4>(a, slices, s);
-        case 5: return launch_product<5>(a, slices, s);
-        case 6: return launch_product<6>(a, slices, s);
-        case 7: return launch_product<7>(a, slices, s);
-        default: return launch_product<8>(a, slices, s);
+        case 1: return launch_tiles<1>(a, slices, s);
+        case 2: return launch_tiles<2>(a, slices, s);
+        case 3: return launch_tiles<3>(a, slices, s);
+        case 4: return launch_tiles<4>(a, slices, s);
+        case 5: return launch_tiles<5>(a, slices, s);
+        case 6: return launch_tiles<6>(a, slices, s);
+        case 7: return launch_tiles<7>(a, slices, s);
+        default: return launch_tiles<8>(a, slices, s);
     }
 }
 
