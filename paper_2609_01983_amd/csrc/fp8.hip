@@ -230,10 +230,10 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int64_t row, in
 
 // Workgroups of eight wavefronts, 32 rows each, with W of CT tiles of 16 columns in LDS.  Measured:
 // 2^22 rows 256 -> 128 float32 640 us, 3.25 GB, 5.0 TB/s, bound by memory; 2^19 rows 1,024 -> 1,024 1.59 ms, 690 TFLOP/s,
-// and 200,003 rows 528 -> 200 90 us, 470 TFLOP/s: the matrix unit and LDS (which have equal shares: 1 KB of W
+// and 200,003 rows 528 -> 200 82 us, 515 TFLOP/s: the matrix unit and LDS (which have equal shares: 1 KB of W
 // for two products) are each busy about a third of the time, and the wavefronts wait for each other's
-// turns.  Requests of X two to four blocks ahead, or W's reads a tile ahead of its products, made wide
-// products 2% faster and narrow ones 3 to 15% slower.
+// turns.  Requests of X two to four blocks ahead, or W's reads ordered a tile ahead of its products, made
+// wide products 2% faster and narrow ones 3 to 15% slower.
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kRowTiles = 2;
