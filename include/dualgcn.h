@@ -474,13 +474,15 @@ typedef struct dualgcn_norm {
  *
  * R, Rn: n x F row-major, float32, or bfloat16 with DUALGCN_STREAM_BF16; B: n x F, float32, or
  * bfloat16 with DUALGCN_IN_BF16; Z: n x F, float32, or bfloat16 with DUALGCN_OUT_BF16 (what
- * dualgcn_update reads with DUALGCN_IN_BF16).  The second norm takes Rn as it is stored.
+ * dualgcn_update reads with DUALGCN_IN_BF16).  The second norm takes Rn as it is stored: a step of
+ * a bfloat16 Rn is up to 2^-7 of an element of Z.
  *   B NULL   the norm before the first block: Z = pre(R); Rn must be NULL and no flag of the
  *            post norm or a gate set.
  *   Z NULL   the last block, or a block whose next one takes the stream as it is.
  * Rn may be R (the stream is updated in place); no other output may overlap an operand or
- * another output (DUALGCN_ERR_INVALID_ARG).  float32 arithmetic; every output element is written
- * by one thread, and the order of every sum is fixed.  n >= 1, 1 <= F <= 8192 (larger F:
+ * another output (DUALGCN_ERR_INVALID_ARG).  float32 arithmetic, but that a bfloat16 Rn beside a
+ * float32 Z is formed in float64 and rounded once (formed in float32, a sum next to the middle of two
+ * bfloat16 numbers may be stored as either).  Every output element is written by one thread, and the order of every sum is fixed.  n >= 1, 1 <= F <= 8192 (larger F:
  * DUALGCN_ERR_UNSUPPORTED); rows may start at any element.  No workspace.  Asynchronous.
  */
 int dualgcn_norm_residual(const dualgcn_norm *norm, const void *R, const void *B, void *Rn, void *Z,

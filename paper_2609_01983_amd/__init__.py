@@ -624,7 +624,8 @@ def norm_residual(R, B=None, *, post_norm=True, post_weight=None, post_bias=None
     biases (None: ones and zeros); post_norm=False leaves the block as it is, pre_norm=False
     makes no Z.  gate: None, float32 [F] (one for each feature), float32 [n, 1] (one for each
     node), or [n, F] in B's type; with gate_sigmoid it holds logits.  Z is float32, or bfloat16
-    with norm_bf16 (what `update` takes).  Rn may be R (in place).  Returns (Rn, Z)."""
+    with norm_bf16 (what `update` takes).  Z norms Rn as it is stored; a bfloat16 Rn beside a float32 Z
+    is summed in float64 and rounded once.  Rn may be R (in place).  Returns (Rn, Z)."""
     _rows(R, "R")
     n, F = shape = R.shape
     if B is None:

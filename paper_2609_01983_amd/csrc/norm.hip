@@ -14,6 +14,10 @@
 // ([.] for the layer norm only).  The statistics are computed again from B and R', which the
 // backward pass reads in any case: that costs two reductions in registers and no bytes.
 //
+// Z norms the stream as it is stored.  Where the stream is bfloat16 and Z float32, the last bits of a sum that lies
+// beside the middle of two bfloat16 numbers decide over half a percent of an element of Z (of float32 sums, one
+// element in 6,000 was not the formula's): there the sum is formed in float64 and rounded once.
+//
 // Both passes are bound by memory (about one flop a byte): a row stays in the registers of
 // its threads from the load to the store, so every operand is read and every output written
 // once.  The threads of a row are as many as hold it in few quads: 8 to 64 lanes of a
@@ -113,6 +117,45 @@ __device__ __forceinline__ void normalise(row_f32x4 (&x)[Q], const QuadPlace (&a
     for (int q = 0; q < Q; ++q) x[q] *= r;
 }
 
+__device__ __forceinline__ double sigmoid(double x) { return 1.0 / (1.0 + exp(-x)); }
+
+// 1 / sqrt(x) of a float64: the hardware's estimate (2^-23) and two of Newton's steps; 0 of infinity
+__device__ __forceinline__ double inverse_root(double x) {
+    double r = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) r = fma(0.5 * r, fma(-x * r, r, 1.0), r);
+    return x == INFINITY ? 0.0 : r;
+}
+
+// normalise() in float64
+template <int TPR, int Q, bool LAYER>
+__device__ __forceinline__ void normalise(row_f64x4 (&x)[Q], const QuadPlace (&at)[Q], bool ragged, double inv_f,
+                                          double eps, row_f32x4 *sh, int &turn) {
+    if constexpr (LAYER) {
+        double m = 0.0;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) m += (x[q][0] + x[q][1]) + (x[q][2] + x[q][3]);
+        m = row_sum<TPR>(m, sh, turn) * inv_f;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            x[q] -= m;
+            if (ragged)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i >= at[q].count) x[q][i] = 0.0;
+        }
+    }
+    double s = 0.0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = fma(x[q][i], x[q][i], s);
+    s = row_sum<TPR>(s, sh, turn);
+    const double r = inverse_root(fma(s, inv_f, eps));
+#pragma unroll
+    for (int q = 0; q < Q; ++q) x[q] *= r;
+}
+
 // ------------------------------------------------------------------ forward
 
 struct ForwardArgs {
@@ -123,14 +166,16 @@ struct ForwardArgs {
     float eps, scale;
     uint32_t flags;
     bool streaming;                  // outputs past the L2s: stored with a non-temporal hint
+    double inv_f;                    // 1 / F
 };
 
-// LAYER: layer norms; A: B and a full gate are bfloat16; S: the stream is.  Behind a row's end every
-// operand and weight is zero, so RMS norms need no masks; a mean taken off is cut there.
+// LAYER: layer norms; A: B and a full gate are bfloat16; S: the stream is; EXACT (S, B there, a float32 Z): the stream's
+// sum is formed in float64.  Behind a row's end every operand and weight is zero, so RMS norms need no masks; a
+// mean taken off is cut there.
 // Measured: 2^21 x 256, both RMS norms and a gate a feature, float32 in, bfloat16 Z: 7.5 GB in 1.29 ms, 5.8 TB/s
 // (a copy of that size: 5.2 to 5.5); one row of 256: 2.0 us, the launch itself.  The weights' vectors are
 // read again by each workgroup, from the caches.
-template <int TPR, int Q, bool LAYER, bool A, bool S>
+template <int TPR, int Q, bool LAYER, bool A, bool S, bool EXACT>
 __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(ForwardArgs a) {
     constexpr bool TINY = TPR == 1;
     constexpr int kGroups = Shape<TPR, Q>::kGroups;
@@ -171,15 +216,22 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(
 #pragma unroll
         for (int q = 0; q < Q; ++q) x[q] = rr[q].get(at[q], odd);
         if (a.B) {
-            row_f32x4 v[Q], w[Q], c[Q];
+            typedef typename std::conditional<EXACT, row_f64x4, row_f32x4>::type Sum4;
+            typedef typename std::conditional<EXACT, double, float>::type Sum;
+            Sum4 v[Q];
+            row_f32x4 w[Q], c[Q];
 #pragma unroll
-            for (int q = 0; q < Q; ++q) v[q] = rb[q].get(at[q], odd);
+            for (int q = 0; q < Q; ++q) v[q] = __builtin_convertvector(rb[q].get(at[q], odd), Sum4);
             if (post) {
                 Vector(a.w1, F, 1.f).load<Q, TINY>(at, odd, w);
                 if constexpr (LAYER) Vector(a.b1, F, 0.f).load<Q, TINY>(at, odd, c);
-                normalise<TPR, Q, LAYER>(v, at, ragged, inv_f, a.eps, sh, turn);
+                if constexpr (EXACT) normalise<TPR, Q, LAYER>(v, at, ragged, a.inv_f, static_cast<double>(a.eps), sh, turn);
+                else normalise<TPR, Q, LAYER>(v, at, ragged, inv_f, a.eps, sh, turn);
 #pragma unroll
-                for (int q = 0; q < Q; ++q) v[q] = LAYER ? v[q] * w[q] + c[q] : v[q] * w[q];
+                for (int q = 0; q < Q; ++q) {
+                    v[q] *= __builtin_convertvector(w[q], Sum4);
+                    if constexpr (LAYER) v[q] += __builtin_convertvector(c[q], Sum4);
+                }
             }
             if (a.flags & (DUALGCN_GATE_FEATURE | DUALGCN_GATE_FULL)) {
                 if (a.flags & DUALGCN_GATE_FEATURE) {
@@ -188,23 +240,32 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(
 #pragma unroll
                     for (int q = 0; q < Q; ++q) w[q] = rg[q].get(at[q], odd);
                 }
-                if (sig)
 #pragma unroll
-                    for (int q = 0; q < Q; ++q)
+                for (int q = 0; q < Q; ++q) {
+                    Sum4 gate = __builtin_convertvector(w[q], Sum4);
+                    if (sig)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[q][i] = sigmoid(w[q][i]);
-#pragma unroll
-                for (int q = 0; q < Q; ++q) v[q] *= w[q];
+                        for (int i = 0; i < 4; ++i) {
+                            gate[i] = sigmoid(gate[i]);
+                            if constexpr (EXACT) __builtin_amdgcn_sched_barrier(0);    // registers for one exponential at a time
+                        }
+                    v[q] *= gate;
+                }
             }
-            const float scale = a.scale * (sig && (a.flags & DUALGCN_GATE_NODE) ? sigmoid(gn) : gn);
+            const Sum node = gn;
+            const Sum scale = a.scale * (sig && (a.flags & DUALGCN_GATE_NODE) ? sigmoid(node) : node);
             const __amdgpu_buffer_rsrc_t wn = row_window<S>(a.Rn, first, elems);
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[q][i] = fmaf(scale, v[q][i], x[q][i]);
                     // the next norm (and the backward pass) take the stream as it is stored
-                    if constexpr (S) x[q][i] = through_bf16(x[q][i]);
+                    if constexpr (EXACT) {
+                        x[q][i] = round_to_bf16(fma(scale, v[q][i], static_cast<double>(x[q][i])));
+                    } else {
+                        x[q][i] = fmaf(scale, v[q][i], x[q][i]);
+                        if constexpr (S) x[q][i] = through_bf16(x[q][i]);
+                    }
                 }
                 store_row_quad<S, TINY>(wn, at[q], x[q], odd, a.streaming);
             }
@@ -216,7 +277,7 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(
             normalise<TPR, Q, LAYER>(x, at, ragged, inv_f, a.eps, sh, turn);
 #pragma unroll
             for (int q = 0; q < Q; ++q) x[q] = LAYER ? x[q] * w[q] + c[q] : x[q] * w[q];
-            if (a.flags & DUALGCN_OUT_BF16) {
+            if (!EXACT && (a.flags & DUALGCN_OUT_BF16)) {
                 const __amdgpu_buffer_rsrc_t wz = row_window<true>(a.Z, first, elems);
 #pragma unroll
                 for (int q = 0; q < Q; ++q) store_row_quad<true, TINY>(wz, at[q], x[q], odd, a.streaming);
@@ -572,6 +633,23 @@ void with_forward_shape(int32_t F, Fn f) {
     else shape<512, 4>(f);
 }
 
+// Float64 sums, bound by the vector unit (conversions, and a row's statistics): the widths by powers of two, so that
+// fewer instances do.  2^27 elements, bfloat16 in, float32 Z, RMS and a gate a feature, us: F = 64 289, 128 290, 256 290, 1,024
+// 306, 4,096 339; 192 385, 700 416 (float32 sums of all widths, whose stream was not the formula's: 226 to 293).
+template <class Fn>
+void with_exact_shape(int32_t F, Fn f) {
+    if (F < 4) shape<1, 1>(f);
+    else if (F <= 32) shape<8, 1>(f);
+    else if (F <= 64) shape<8, 2>(f);
+    else if (F <= 128) shape<16, 2>(f);
+    else if (F <= 256) shape<32, 2>(f);
+    else if (F <= 512) shape<64, 2>(f);
+    else if (F <= 1024) shape<128, 2>(f);
+    else if (F <= 2048) shape<256, 2>(f);
+    else if (F <= 4096) shape<512, 2>(f);
+    else shape<1024, 2>(f);
+}
+
 // The backward pass has about twice the registers a quad.  2^26 elements, us, float32 / bfloat16 (floor
 // 278 / 139): F = 256 (64, 1) 285 / 163, (32, 2) 305 / 165; F = 600 (64, 3) 339 / 240, (256, 1) 340 / 307;
 // F = 3,000 (256, 3) 335 / 229, (1024, 1) 418 / 330.
@@ -627,16 +705,25 @@ bool past_l2(int64_t elems) { return elems * 4 > int64_t{32} << 20; }
 int launch_norm_residual(const dualgcn_norm &p, const void *R, const void *B, void *Rn, void *Z, int32_t n,
                          int32_t F, hipStream_t s) {
     const ForwardArgs a{R, B, p.gate, Rn, Z, p.post_weight, p.post_bias, p.pre_weight, p.pre_bias, n, F,
-                        p.eps, p.scale, p.flags, past_l2(static_cast<int64_t>(n) * F)};
-    with_forward_shape(F, [&](auto tpr, auto quads) {
+                        p.eps, p.scale, p.flags, past_l2(static_cast<int64_t>(n) * F), 1.0 / F};
+    const bool exact = B && Z && (p.flags & DUALGCN_STREAM_BF16) && !(p.flags & DUALGCN_OUT_BF16);
+    const bool layer = p.flags & DUALGCN_NORM_LAYER, act = p.flags & DUALGCN_IN_BF16;
+    auto launch = [&](auto tpr, auto quads, auto exactly, auto l, auto b, auto st) {
         constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
         const int64_t need = (static_cast<int64_t>(n) + Shape<T, Q>::kGroups - 1) / Shape<T, Q>::kGroups;
         const dim3 grid(static_cast<unsigned>(std::min<int64_t>(need, kMaxForwardBlocks)));
-        with_flags([&](auto layer, auto act, auto stream) {
-            hipLaunchKernelGGL((norm_residual_kernel<T, Q, decltype(layer)::value, decltype(act)::value, decltype(stream)::value>),
-                               grid, dim3(Shape<T, Q>::kBlock), 0, s, a);
-        }, (p.flags & DUALGCN_NORM_LAYER) != 0, (p.flags & DUALGCN_IN_BF16) != 0, (p.flags & DUALGCN_STREAM_BF16) != 0);
-    });
+        hipLaunchKernelGGL((norm_residual_kernel<T, Q, decltype(l)::value, decltype(b)::value, decltype(st)::value, decltype(exactly)::value>),
+                           grid, dim3(Shape<T, Q>::kBlock), 0, s, a);
+    };
+    if (exact)
+        with_exact_shape(F, [&](auto tpr, auto quads) {
+            with_flags([&](auto l, auto b) { launch(tpr, quads, std::true_type(), l, b, std::true_type()); }, layer, act);
+        });
+    else
+        with_forward_shape(F, [&](auto tpr, auto quads) {
+            with_flags([&](auto l, auto b, auto st) { launch(tpr, quads, std::false_type(), l, b, st); }, layer, act,
+                       (p.flags & DUALGCN_STREAM_BF16) != 0);
+        });
     return hip_status(hipGetLastError());
 }
 

@@ -11,6 +11,7 @@ namespace dgc {
 
 typedef float row_f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 row_bf16x4 __attribute__((ext_vector_type(4)));
+typedef double row_f64x4 __attribute__((ext_vector_type(4)));
 // rows may start at any element: the loads and stores below need no more than its alignment
 typedef float row_f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned short row_u16x4 __attribute__((ext_vector_type(4)));
@@ -166,6 +167,14 @@ __device__ __forceinline__ void store_quad(void *base, int64_t at, int count, ro
 // The value of a float32 as it is when stored in bfloat16.
 __device__ __forceinline__ float through_bf16(float f) { return static_cast<float>(static_cast<__bf16>(f)); }
 
+// A float64 rounded to bfloat16's 8 significant bits, to nearest even, as a float32.  (By way of a float32 rounded
+// to nearest it could land on the middle between two bfloat16 numbers and go the wrong way.)  NaN stays NaN.
+__device__ __forceinline__ float round_to_bf16(double d) {
+    uint32_t hi = static_cast<uint32_t>(__double2hiint(d)) | (__double2loint(d) != 0 ? 1u : 0u);   // 7 of its 20 fraction bits stay
+    hi = hi + 0xFFFu + (hi >> 13 & 1u) & ~0x1FFFu;
+    return d != d ? __uint_as_float(0x7FC00000u) : static_cast<float>(__hiloint2double(static_cast<int>(hi), 0));
+}
+
 // A value that the optimiser takes for a new one: what was computed from it before is not kept in
 // registers for its next use.
 template <class T>
@@ -232,6 +241,46 @@ __device__ __forceinline__ void row_reduce(float (&v)[N], Op op, row_f32x4 *sh, 
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = lanes_reduce<kWaves>(one[i], op);
     }
+}
+
+// The sum of a float64 over the same threads, likewise.
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+    return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xF, 0xF, true),
+                            __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xF, 0xF, true));
+}
+template <int LANES>
+__device__ __forceinline__ double lanes_sum(double v) {
+    if constexpr (LANES >= 2) v += dpp<0xB1>(v);
+    if constexpr (LANES >= 4) v += dpp<0x4E>(v);
+    if constexpr (LANES >= 8) v += dpp<0x141>(v);
+    if constexpr (LANES >= 16) v += dpp<0x140>(v);
+    if constexpr (LANES >= 32) {
+        const auto h = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+        const auto l = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+        v = __hiloint2double(h[0], l[0]) + __hiloint2double(h[1], l[1]);
+    }
+    if constexpr (LANES >= 64) {
+        const auto h = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
+        const auto l = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
+        v = __hiloint2double(h[0], l[0]) + __hiloint2double(h[1], l[1]);
+    }
+    return v;
+}
+template <int THREADS>
+__device__ __forceinline__ double row_sum(double v, row_f32x4 *sh, int &turn) {
+    v = lanes_sum<(THREADS < 64 ? THREADS : 64)>(v);
+    if constexpr (THREADS > 64) {
+        constexpr int kWaves = THREADS / 64;
+        row_f32x4 *b = sh + (turn & 1) * kWaves;
+        ++turn;
+        if ((threadIdx.x & 63) == 0)
+            b[threadIdx.x >> 6] = row_f32x4{__int_as_float(__double2hiint(v)), __int_as_float(__double2loint(v)), 0.f, 0.f};
+        __syncthreads();
+        const row_f32x4 one = b[threadIdx.x & (kWaves - 1)];
+        v = lanes_sum<kWaves>(__hiloint2double(__float_as_int(one[0]), __float_as_int(one[1])));
+    }
+    return v;
 }
 
 template <int THREADS>
