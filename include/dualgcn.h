@@ -595,7 +595,8 @@ int dualgcn_quantize_weight_fp8(const float *W, int32_t F_in, int32_t F_out, int
  * X (device, e4m3 n x F_in row-major) with sx (float32[n][ceil(F_in / 128)]); W (device, e4m3
  * F_out x F_in row-major: W transposed) with sw (float32[ceil(F_out / 128)][ceil(F_in / 128)], one
  * for each 128 x 128 block); T (device, n x F_out row-major, float32, or bfloat16 with
- * DUALGCN_OUT_BF16).  The scales may be any float32 numbers.  Products of a block (of the e4m3
+ * DUALGCN_OUT_BF16).  The scales may be any float32 numbers, and their product may lie outside
+ * float32's range (rows with a scale outside [2^-50, 2^50] are slower).  Products of a block (of the e4m3
  * numbers widened to bfloat16, which is exact) are summed by the matrix cores in float32,
  * multiplied by the two scales and added in float32, block after block, in an order that depends
  * on the shape only.  The gradient G W^T is the same call on a quantised G and W not transposed.

@@ -221,6 +221,28 @@ struct Fragment {
     }
 };
 
+// The product x w of two scales as f g, g a power of two and f a normal number.  x w itself may be no float32 (it
+// overflows, or falls among the subnormal numbers and loses bits) though its product with a block's sum, 0 or between
+// 2^-18 and 2^25, is one: the sum is multiplied by g first, which is exact.  Where x w is between 2^-100 and 2^100, g is 1.
+struct Scales {
+    float f, g;
+    __device__ __forceinline__ Scales(float x, float w) {
+        f = x * w;
+        g = 1.f;
+        const float a = fabsf(f);
+        if (!(a >= 0x1p-100f && a <= 0x1p100f) && x != 0.f && w != 0.f) {
+            const int e = __builtin_amdgcn_frexp_expf(x) + __builtin_amdgcn_frexp_expf(w);      // 0 of infinity and NaN
+            const int eg = e - min(max(e, -100), 100);
+            f = __builtin_amdgcn_ldexpf(__builtin_amdgcn_frexp_mantf(x) * __builtin_amdgcn_frexp_mantf(w), e - eg);
+            g = __builtin_amdgcn_ldexpf(1.f, min(max(eg, -126), 127));           // past these the result is 0 or infinite
+        }
+    }
+};
+// Is a scale outside [2^-50, 2^50]?  (Two inside have a product that may be used as it is; zeros, infinities and NaN may too.)
+__device__ __forceinline__ bool far_scale(float x) {
+    return static_cast<uint32_t>(__builtin_amdgcn_frexp_expf(x) + 49) > 99u;
+}
+
 __device__ __forceinline__ void store_tile(const ProductArgs &a, int64_t row, int col, int last, f32x4 v) {
     const int count = last - col;
     if (row >= a.n || count <= 0) return;
@@ -251,8 +273,41 @@ __host__ __device__ __forceinline__ int lds_tile(int blocks) { return blocks * k
 // tiles are too few to give each XCD its share.
 constexpr int kXcds = 8;
 constexpr int kMostBlocks = 8;                       // F_in up to 1,024
+// The 32 rows of a wavefront from row0 on once more, a tile of 16 x 16 at a time, with scales of any size; `w`: W in
+// LDS.  Apart from the main loop, so that it takes few of its registers: tests for such scales alone cost
+// (us with and without) 2^22 rows 32 -> 16 101, 92, 2^20 128 -> 64 64, 60, 200,003 528 -> 200 82, 79, nothing where rows are wider.
+// With a second way beside the main loop's products, whose registers then bound the kernel, 528 -> 200 took 91.
+template <int CT>
+__device__ __forceinline__ void product_of_far_scales(const ProductArgs &a, const __bf16 *w, int64_t row0, int c0, int turn,
+                                                      const float (&column_scales)[2][kMostBlocks]) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, last = min(a.N, c0 + 16 * CT);
+#pragma unroll 1
+    for (int tile = 0; tile < kRowTiles * CT; ++tile) {
+        const int c = tile % CT;
+        const int64_t row = row0 + tile / CT * 16 + r, xr = min(row, static_cast<int64_t>(a.n) - 1);
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int b = 0; b < a.blocks; ++b) {
+            Fragment x;
+            x.load(a.X, xr, a.K, b, g);
+            bf16x8 xs[kSteps];
+            x.get(a.K, b, g, xs);
+            const __bf16 *p = w + c * lds_tile(a.blocks) + b * kSteps * 512 + lane * 8;
+            f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8 *>(p + 512 * k), xs[k], s, 0, 0, 0);
+            const Scales f(a.sx[xr * a.blocks + b], column_scales[c < turn ? 0 : 1][b]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] = fmaf(f.f, s[i] * f.g, acc[i]);
+        }
+        store_tile(a, row, c0 + 16 * c + 4 * g, last, acc);
+    }
+}
+
+// (the second bound: two workgroups a CU, three for one tile)
 template <int CT, bool ALONE>
-__global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_t slices, int32_t side) {
+__global__ __launch_bounds__(kThreads, ALONE ? 2 : CT == 1 ? 6 : CT <= 4 ? 4 : 2) void product_kernel(ProductArgs a, int32_t slices, int32_t side) {
     extern __shared__ uint4 lds[];
     __bf16 *w = reinterpret_cast<__bf16 *>(lds);
     const int tile_elems = lds_tile(a.blocks);
@@ -316,18 +371,22 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_
         for (int t = 0; t < kRowTiles; ++t)
 #pragma unroll
             for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        bool far = false;
         for (int b = 0; b < a.blocks; ++b) {
             bf16x8 x[kRowTiles][kSteps];
 #pragma unroll
             for (int t = 0; t < kRowTiles; ++t) {
                 in[t].get(a.K, b, g, x[t]);
                 sc[t] = sn[t];
+                far |= far_scale(sc[t]);
             }
             // the next block of this tile, or the first of the next tile (past the last: zeros), into the
             // registers that the widened ones have left
             const bool more = b + 1 < a.blocks;
             request(more ? tile : tile + stride, more ? b + 1 : 0);
             const float sw0 = column_scales[0][b], sw1 = column_scales[1][b];
+            far |= far_scale(sw0);
+            far |= far_scale(sw1);
             auto multiply = [&](auto steps) {
 #pragma unroll
                 for (int c = 0; c < CT; ++c) {
@@ -355,6 +414,10 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs a, int32_
             else multiply(std::integral_constant<int, kSteps>());
         }
         const int64_t row0 = tile * kRowsPerBlock;
+        if (__ballot(far)) {                         // scales whose products may not be used as they are: not from acc
+            product_of_far_scales<CT>(a, w, row0 + wave * kRows, c0, turn, column_scales);
+            continue;
+        }
         const int64_t elems = min(static_cast<int64_t>(kRowsPerBlock), a.n - row0) * a.N;
         const int own = anew(4 * g);                 // the places are worked out here, not kept over the tiles
 #pragma unroll
@@ -389,7 +452,7 @@ __global__ __launch_bounds__(kThreads) void product_few_kernel(ProductArgs a) {
         Fragment x, w;
         x.load(a.X, xr, a.K, b, g);
         w.load(a.W, wr, a.K, b, g);
-        const float f = a.sx[xr * a.blocks + b] * sw[b];
+        const Scales f(a.sx[xr * a.blocks + b], sw[b]);
         bf16x8 xs[kSteps], ws[kSteps];
         x.get(a.K, b, g, xs);
         w.get(a.K, b, g, ws);
@@ -397,7 +460,7 @@ __global__ __launch_bounds__(kThreads) void product_few_kernel(ProductArgs a) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[k], xs[k], s, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, s[i], acc[i]);
+        for (int i = 0; i < 4; ++i) acc[i] = fmaf(f.f, s[i] * f.g, acc[i]);
     }
     part[wave][lane] = acc;
     __syncthreads();

@@ -16,7 +16,7 @@
 //
 // Z norms the stream as it is stored.  Where the stream is bfloat16 and Z float32, the last bits of a sum that lies
 // beside the middle of two bfloat16 numbers decide over half a percent of an element of Z (of float32 sums, one
-// element in 6,000 was not the formula's): there the sum is formed in float64 and rounded once.
+// element in 20,000 was not the formula's): there the sum is formed in float64 and rounded once.
 //
 // Both passes are bound by memory (about one flop a byte): a row stays in the registers of
 // its threads from the load to the store, so every operand is read and every output written
