@@ -251,11 +251,11 @@ int check_update(const void *X, const float *W, const void *T, int32_t F_in, int
     return DUALGCN_OK;
 }
 
-// A range of device memory; `same` is the one operand that an output may be in place of.
+// A range of device memory; `same` is the number of the one operand that an output may be in place of, -1 for none.
 struct Span {
     const void *p;
     size_t bytes;
-    const void *same = nullptr;
+    int same = -1;
 };
 
 // No output shares a byte with an operand (but for the one it may replace whole) or with
@@ -265,7 +265,7 @@ bool apart(const Span (&in)[I], const Span (&out)[O]) {
     for (size_t o = 0; o < O; ++o) {
         if (!out[o].p) continue;
         for (size_t i = 0; i < I; ++i)
-            if (in[i].p && !(out[o].same && in[i].p == out[o].same && out[o].p == out[o].same) &&
+            if (in[i].p && !(out[o].same == static_cast<int>(i) && out[o].p == in[i].p) &&
                 overlaps(out[o].p, out[o].bytes, in[i].p, in[i].bytes))
                 return false;
         for (size_t k = 0; k < o; ++k)
@@ -582,7 +582,7 @@ int dualgcn_norm_residual(const dualgcn_norm *norm, const void *R, const void *B
     const Span in[] = {{R, rb}, {B, elems * (norm->flags & DUALGCN_IN_BF16 ? 2 : 4)}, {norm->gate, gate_bytes(*norm, n, F)},
                        {norm->post_weight, vector_bytes(F)}, {norm->post_bias, vector_bytes(F)},
                        {norm->pre_weight, vector_bytes(F)}, {norm->pre_bias, vector_bytes(F)}};
-    const Span out[] = {{Rn, rb, R}, {Z, elems * (norm->flags & DUALGCN_OUT_BF16 ? 2 : 4)}};
+    const Span out[] = {{Rn, rb, 0}, {Z, elems * (norm->flags & DUALGCN_OUT_BF16 ? 2 : 4)}};
     if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
     if ((st = dgc::device_status())) return st;
     return dgc::launch_norm_residual(*norm, R, B, Rn, Z, n, F, static_cast<hipStream_t>(stream));
@@ -623,7 +623,7 @@ int dualgcn_norm_residual_backward(const dualgcn_norm *norm, const void *Rn, con
     const size_t rb = elems * (sbf ? 2 : 4), gb = elems * (gbf ? 2 : 4);
     const Span in[] = {{Rn, rb}, {B, elems * (abf ? 2 : 4)}, {dZ, gb}, {dRn, rb}, {norm->gate, gate_bytes(*norm, n, F)},
                        {norm->post_weight, vb}, {norm->post_bias, vb}, {norm->pre_weight, vb}, {norm->pre_bias, vb}};
-    const Span out[] = {{dR, rb, dRn}, {dB, gb}, {g.post_weight, vb}, {g.post_bias, vb}, {g.pre_weight, vb},
+    const Span out[] = {{dR, rb, 3}, {dB, gb}, {g.post_weight, vb}, {g.post_bias, vb}, {g.pre_weight, vb},
                         {g.pre_bias, vb}, {g.gate, f & DUALGCN_GATE_FULL ? gb : gate_bytes(*norm, n, F)}, {workspace, ws}};
     if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
     if ((st = dgc::device_status())) return st;
