@@ -602,7 +602,7 @@ def _norm(R, B, post_norm, post_weight, post_bias, gate, gate_sigmoid, scale, pr
         if gate.dim() == 1:
             _shaped(gate, torch.float32, width, "gate")
             flags |= GATE_FEATURE
-        elif gate.dim() == 2 and gate.shape[1] == 1 and F != 1:
+        elif gate.dim() == 2 and gate.shape[1] == 1 and (F != 1 or gate.dtype is not B.dtype):
             _shaped(gate, torch.float32, (n, 1), "gate")
             flags |= GATE_NODE
         else:
