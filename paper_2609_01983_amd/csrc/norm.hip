@@ -31,6 +31,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxBlocks = 1024;                     // workgroups, hence partial column sums, of a backward pass
+template <int TPR>
+constexpr int kMostBlocks = TPR > 256 ? kMaxBlocks / 2 : kMaxBlocks;     // (at most one a CU where they are so large)
+// Rows that a group of threads adds to a column sum in float32, one after another.  The error of such a chain grows
+// with its length (67M rows of 4 in chains of 4,096 terms of 0.1: 4e-5 of the sum), so longer passes are done in parts,
+// whose sums are added in float64 (us whole and in parts: 2^21 x 128 1,325, 1,215; 2^17 x 4,096 bfloat16 1,675, 1,690).
+constexpr int kChain = 256;
 constexpr int64_t kMaxForwardBlocks = int64_t{1} << 21;
 
 // ------------------------------------------------------------------ shared by both directions
@@ -563,7 +569,8 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_backward_kernel(
 }
 
 // out[slot][c] = the sum over workgroups of the partial sums of column c: 32 threads sum
-// consecutive parts in order, in float64, and the parts are added in order.  Measured: 512 partial sums
+// consecutive parts in order, in float64, and the parts are added in order.  A pass in parts keeps the sum of those
+// before in `before` (float64, [slots][F]; not read by the first, not written by the last).  Measured: 512 partial sums
 // of 3 x 128 columns 4.6 us, 256 of 2 x 4,096 6.2 us, bound by the loads' latency: 16 are in flight.
 constexpr int kSumSegs = 32;
 constexpr int kSumCols = kThreads / kSumSegs;
@@ -571,7 +578,8 @@ struct SumOut {
     float *to[kSlots];               // the wanted slots, in order
 };
 __global__ __launch_bounds__(kThreads) void norm_columns_kernel(const float *__restrict__ partial, int32_t count,
-                                                                int32_t wanted, int32_t F, SumOut out) {
+                                                                int32_t wanted, int32_t F, double *before, bool first,
+                                                                bool last, SumOut out) {
     __shared__ double sh[kSumSegs][kSumCols];
     const int el = threadIdx.x % kSumCols, seg = threadIdx.x / kSumCols;
     const int c = blockIdx.x * kSumCols + el, slot = blockIdx.y;
@@ -597,7 +605,10 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(const float *__r
         double t = 0.0;
 #pragma unroll
         for (int k = 0; k < kSumSegs; ++k) t += sh[k][el];
-        out.to[slot][c] = static_cast<float>(t);
+        double *const b = before + static_cast<int64_t>(slot) * F + c;
+        if (!first) t += *b;
+        if (last) out.to[slot][c] = static_cast<float>(t);
+        else *b = t;
     }
 }
 
@@ -684,15 +695,15 @@ void with_flags(Fn f, bool b, More... more) {
 // Workgroups of a backward pass, each with a partial sum of every column.  Its wavefronts have two
 // rows in flight each, so two workgroups a CU fill the memory's queues with float32 operands
 // (F = 128, us at 2, 3, 4 a CU: 287 / 299 / 316), and four where every operand is bfloat16 (226 / 179 / 159).
-int backward_blocks(int32_t n, int32_t F, bool all_bf16) {
-    int groups = 1, per_cu = 1;
+int backward_blocks(int64_t n, int32_t F, bool all_bf16, int &groups) {
+    int per_cu = 1, most = 1;
     with_backward_shape(F, [&](auto tpr, auto quads) {
         constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
         groups = Shape<T, Q>::kGroups;
         per_cu = T > 256 ? 1 : T == 128 ? 4 : all_bf16 ? 5 - Q : 2;
+        most = kMostBlocks<T>;
     });
-    const int64_t need = (static_cast<int64_t>(n) + groups - 1) / groups;
-    return static_cast<int>(std::min<int64_t>(need, std::min(kMaxBlocks, per_cu * device_cus())));
+    return static_cast<int>(std::min<int64_t>((n + groups - 1) / groups, std::min(most, per_cu * device_cus())));
 }
 
 // Outputs the L2s (8 x 4 MiB) would not keep for the next launch are stored past them (us so and without the
@@ -728,17 +739,22 @@ int launch_norm_residual(const dualgcn_norm &p, const void *R, const void *B, vo
 }
 
 size_t norm_backward_workspace_bytes(int32_t n, int32_t F) {
-    int groups = 1;
-    with_backward_shape(F, [&](auto tpr, auto quads) { groups = Shape<decltype(tpr)::value, decltype(quads)::value>::kGroups; });
+    int groups = 1, most = 1;
+    with_backward_shape(F, [&](auto tpr, auto quads) {
+        groups = Shape<decltype(tpr)::value, decltype(quads)::value>::kGroups;
+        most = kMostBlocks<decltype(tpr)::value>;
+    });
     const int64_t need = (static_cast<int64_t>(n) + groups - 1) / groups;
-    return static_cast<size_t>(std::min<int64_t>(need, kMaxBlocks)) * kSlots * F * sizeof(float);
+    // the sums of the parts before, then the partial sums
+    return kSlots * static_cast<size_t>(F) * (sizeof(double) + static_cast<size_t>(std::min<int64_t>(need, most)) * sizeof(float));
 }
 
 int launch_norm_backward(const dualgcn_norm &p, const void *Rn, const void *B, const void *dZ, const void *dRn,
                          void *dR, void *dB, const dualgcn_norm_grads &g, int32_t n, int32_t F, void *workspace,
                          hipStream_t s) {
+    double *const before = static_cast<double *>(workspace);
     BackwardArgs a{Rn, B, p.gate, dZ, dRn, dR, dB, g.gate, p.post_weight, p.post_bias, p.pre_weight,
-                   static_cast<float *>(workspace), n, F, p.eps, p.scale, p.flags, 0u,
+                   reinterpret_cast<float *>(before + kSlots * static_cast<size_t>(F)), n, F, p.eps, p.scale, p.flags, 0u,
                    past_l2(static_cast<int64_t>(n) * F)};
     SumOut out{};
     int wanted = 0;
@@ -749,28 +765,56 @@ int launch_norm_backward(const dualgcn_norm &p, const void *Rn, const void *B, c
             a.want |= 1u << k;
             out.to[wanted++] = to[k];
         }
-    const int blocks = backward_blocks(
-        n, F, (~p.flags & (DUALGCN_IN_BF16 | DUALGCN_STREAM_BF16 | DUALGCN_GRAD_BF16)) == 0);
+    const bool act = p.flags & DUALGCN_IN_BF16, str = p.flags & DUALGCN_STREAM_BF16, grd = p.flags & DUALGCN_GRAD_BF16;
+    int groups = 1;
+    const int most = backward_blocks(n, F, act && str && grd, groups);
+    // parts of equal numbers of rows, whole steps of all workgroups
+    const int64_t step = static_cast<int64_t>(most) * groups, steps = (n + step - 1) / step;
+    const int64_t parts = wanted ? (steps + kChain - 1) / kChain : 1, rows = (steps + parts - 1) / parts * step;
+    // a pointer moved by `count` elements of four or (bf16) two bytes
+    auto moved = [](auto *x, int64_t count, bool bf16) {
+        using P = decltype(x);
+        return x ? (P)((char *)x + count * (bf16 ? 2 : 4)) : x;
+    };
     int st = DUALGCN_OK;
-    with_backward_shape(F, [&](auto tpr, auto quads) {
-        constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
-        const size_t lds = Q > 1 ? sizeof(row_f32x4) * Q * Shape<T, Q>::kBlock * __builtin_popcount(a.want & 15u) : 0;
-        with_flags([&](auto layer, auto act, auto stream, auto grad) {
-            const auto kernel = &norm_backward_kernel<T, Q, decltype(layer)::value, decltype(act)::value,
-                                                      decltype(stream)::value, decltype(grad)::value>;
-            if (lds > 48 * 1024 && (st = hip_status(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                                                         hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                                         static_cast<int>(lds)))))
-                return;
-            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(Shape<T, Q>::kBlock), lds, s, a);
-        }, (p.flags & DUALGCN_NORM_LAYER) != 0, (p.flags & DUALGCN_IN_BF16) != 0, (p.flags & DUALGCN_STREAM_BF16) != 0,
-           (p.flags & DUALGCN_GRAD_BF16) != 0);
-    });
-    if (!st) st = hip_status(hipGetLastError());
-    if (st || !wanted) return st;
-    hipLaunchKernelGGL(norm_columns_kernel, dim3((F + kSumCols - 1) / kSumCols, wanted), dim3(kThreads), 0, s,
-                       a.partial, blocks, wanted, F, out);
-    return hip_status(hipGetLastError());
+    for (int64_t row = 0; row < n && !st; row += rows) {
+        const int64_t at = row * F;
+        BackwardArgs part = a;
+        part.n = static_cast<int32_t>(std::min(rows, n - row));
+        part.Rn = moved(Rn, at, str);
+        part.B = moved(B, at, act);
+        part.dZ = moved(dZ, at, grd);
+        part.dRn = moved(dRn, at, str);
+        part.dR = moved(dR, at, str);
+        part.dB = moved(dB, at, grd);
+        if (p.flags & DUALGCN_GATE_FULL) {
+            part.gate = moved(p.gate, at, act);
+            part.dgate = moved(g.gate, at, grd);
+        } else if (p.flags & DUALGCN_GATE_NODE) {
+            part.gate = moved(p.gate, row, false);
+            part.dgate = moved(g.gate, row, false);
+        }
+        const int blocks = static_cast<int>(std::min<int64_t>((part.n + groups - 1) / groups, most));
+        with_backward_shape(F, [&](auto tpr, auto quads) {
+            constexpr int T = decltype(tpr)::value, Q = decltype(quads)::value;
+            const size_t lds = Q > 1 ? sizeof(row_f32x4) * Q * Shape<T, Q>::kBlock * __builtin_popcount(a.want & 15u) : 0;
+            with_flags([&](auto layer, auto bf, auto stream, auto grad) {
+                const auto kernel = &norm_backward_kernel<T, Q, decltype(layer)::value, decltype(bf)::value,
+                                                          decltype(stream)::value, decltype(grad)::value>;
+                if (lds > 48 * 1024 && (st = hip_status(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                                             hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                                             static_cast<int>(lds)))))
+                    return;
+                hipLaunchKernelGGL(kernel, dim3(blocks), dim3(Shape<T, Q>::kBlock), lds, s, part);
+            }, (p.flags & DUALGCN_NORM_LAYER) != 0, act, str, grd);
+        });
+        if (!st) st = hip_status(hipGetLastError());
+        if (st || !wanted) continue;
+        hipLaunchKernelGGL(norm_columns_kernel, dim3((F + kSumCols - 1) / kSumCols, wanted), dim3(kThreads), 0, s,
+                           a.partial, blocks, wanted, F, before, row == 0, row + rows >= n, out);
+        st = hip_status(hipGetLastError());
+    }
+    return st;
 }
 
 }  // namespace dgc
