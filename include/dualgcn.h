@@ -549,6 +549,9 @@ int dualgcn_distill_workspace(int32_t n, int32_t C, int32_t K, size_t *bytes);
  * is infinite if the teacher or the label takes it).  A row with a NaN, a +infinity or nothing
  * above -infinity among the logits it needs gives NaN, in its own row of G and in the loss.
  * float32 arithmetic, the loss joined in float64 in a fixed order; G does not depend on timing.
+ * A row's part of soft is off by up to about 1e-6 soft_scale temperature^2 up to a temperature of 8;
+ * above, soft is formed in float64 (in a launch of its own).  Q and P of G are float32 at any
+ * temperature: an element is off by up to about 1e-5 soft_scale temperature Q, whatever Q - P is.
  * n >= 1, 1 <= C < 2^20, 1 <= K <= 4096 (larger: DUALGCN_ERR_UNSUPPORTED), temperature in
  * [2^-14, 2^14], finite scales; outputs overlap nothing.  `workspace` (device, 256-byte aligned)
  * holds at least dualgcn_distill_workspace bytes; calls that may run at the same time need one

@@ -728,8 +728,9 @@ def distill_xent(Y, ids, teacher, labels=None, temperature=1.0, soft_scale=None,
     labels: int32 [n] or None.  Returns (G, loss): G = dloss[0]/dY ([n, C] float32, or bfloat16
     with grad_bf16) and the float32 device tensor loss = [soft + hard, soft, hard], soft =
     soft_scale T^2 sum KL(teacher || softmax(Y / T)), hard = hard_scale sum of the labels'
-    cross-entropy.  The scales default to 1 / (rows with an entry) and 1 / (labeled rows),
-    counted on the host only when not given."""
+    cross-entropy.  Past a temperature of 8 soft is formed in float64, by a second pass over Y.
+    The scales default to 1 / (rows with an entry) and 1 / (labeled rows), counted on the host only
+    when not given."""
     flags = IN_BF16 if _rows(Y, "Y") else 0
     n, C = shape = Y.shape
     if not isinstance(ids, torch.Tensor) or ids.dim() != 2:

@@ -715,11 +715,73 @@ __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {
                           a.partial + 2 * (static_cast<int64_t>(blockIdx.y) * splits + blockIdx.x));
 }
 
-// loss = {soft + hard, soft, hard} from the workgroups' sums, by a fixed tree.
+// ------------------------------------------------------------------ high temperatures
+//
+// Where the teacher keeps most classes, the divergence of a row falls as 1 / T^2, while its terms in float32 (the logarithms of
+// the sums above all) keep an error of about 5e-7, which T^2 enlarges: of a loss of 4 a row 3e-5 at T = 8, but 1e-3 at
+// T = 100 and more than itself at T = 10,000.  Past kHotTemperature the soft loss is formed in float64, in a
+// launch of its own: with z = (y - m) / T of both sides,
+//   sum p_k (log p_k - log Q[id_k]) = sum e_k (z_k - z_y[id_k]) / sum e_k + log sum_j exp(z_y[j]) - log sum e_k.
+// Bound by float64 exponentials, one a logit, and by the latency of few and long rows; us of a call below and past 8: 2^22 x 64
+// (16 entries, many twice) 1,045, 2,110; 65,536 x 2,000 bfloat16 165, 375; 4,095 x 131,072 bfloat16 519, 1,387; 30,007 x 47 13, 23;
+// 1 x 1,000,000 16, 285.
+constexpr float kHotTemperature = 8.f;
+
+template <int TPR, bool YBF, bool TBF>
+__global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_hot_kernel(Args a, double inv_t, double *out) {
+    constexpr int kBlock = TPR > 64 ? TPR : kThreads, kGroups = kBlock / TPR;
+    __shared__ row_f32x4 sh[row_reduce_quads<TPR>()];
+    int turn = 0;
+    const int l = threadIdx.x % TPR, g = threadIdx.x / TPR;
+    auto logit = [](const void *p, int64_t at) {
+        if constexpr (YBF) return bf16_to_float(static_cast<const unsigned short *>(p)[at]);
+        else return static_cast<const float *>(p)[at];
+    };
+    double soft = 0.0;
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kGroups; row0 < a.n;
+         row0 += static_cast<int64_t>(gridDim.x) * kGroups) {
+        const int64_t row = row0 + g;
+        const int C = row < a.n ? a.C : 0;               // a row behind the last has no classes and no entries
+        const int K = row < a.n ? a.K : 0;
+        // f of the classes and logits of the entries that count
+        auto entries = [&](auto f) {
+            for (int k = l; k < K; k += TPR) {
+                const int i = a.ids[row * a.K + k];
+                const float x = teacher_at<TBF>(a.teacher, row * a.K + k);
+                if (i >= 0 && i < C && !(x == -INFINITY)) f(i, x);
+            }
+        };
+        float top[3] = {-INFINITY, 0.f, -FLT_MAX};       // the entries' largest, is there one, the row's largest
+        entries([&](int, float x) {
+            top[0] = fmaxf(top[0], x);
+            top[1] = 1.f;
+        });
+#pragma unroll 4
+        for (int c = l; c < C; c += TPR) top[2] = fmaxf(top[2], logit(a.Y, row * a.C + c));
+        row_reduce<TPR>(top, MaxOp(), sh, turn);
+        const double mt = top[0], my = top[2];
+        double st = 0.0, cross = 0.0, sy = 0.0;
+        entries([&](int i, float x) {
+            const double z = (x - mt) * inv_t, e = exp(z);
+            st += e;
+            if (e != 0.0) cross += e * (z - (logit(a.Y, row * a.C + i) - my) * inv_t);     // no 0 * infinity
+        });
+#pragma unroll 4
+        for (int c = l; c < C; c += TPR) sy += exp((logit(a.Y, row * a.C + c) - my) * inv_t);
+        st = row_sum<TPR>(st, sh, turn);
+        cross = row_sum<TPR>(cross, sh, turn);
+        sy = row_sum<TPR>(sy, sh, turn);
+        if (l == 0 && top[1] > 0.f) soft += cross / st + log(sy) - log(st);
+    }
+    write_partial<kBlock>(soft / kLn2, 0.0, out + 2 * static_cast<int64_t>(blockIdx.x));    // as the other sums: in powers of 2
+}
+
+// loss = {soft + hard, soft, hard} from the workgroups' sums, by a fixed tree.  `hot`: the soft ones, if they are apart.
 // 16 bytes a load, eight in flight a thread (8,192 workgroups: 13 us with one load at a time).
 constexpr int kLossThreads = 1024;
 typedef double f64x2 __attribute__((ext_vector_type(2)));
 __global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(const double *__restrict__ partial, int32_t count,
+                                                                    const double *__restrict__ hot, int32_t hot_count,
                                                                     double soft, double hard, float *__restrict__ loss) {
     __shared__ f64x2 sh[kLossThreads];
     const int t = threadIdx.x;
@@ -730,6 +792,12 @@ __global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(const double
         const int i = t + j * kLossThreads;
         v[j] = i < count ? reinterpret_cast<const f64x2 *>(partial)[i] : f64x2{0.0, 0.0};
     }
+    if (hot)
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int i = t + j * kLossThreads;
+            v[j][0] = i < hot_count ? hot[2 * i] : 0.0;
+        }
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) sum += v[j];
     sh[t] = sum;
@@ -808,6 +876,21 @@ int launch_long(const Args &a, bool tbf, hipStream_t s) {
     return static_cast<int>(grid.x * grid.y);
 }
 
+template <int TPR>
+int launch_hot(const Args &a, bool ybf, bool tbf, float T, double *out, hipStream_t s) {
+    constexpr int kBlock = TPR > 64 ? TPR : kThreads;
+    const int blocks = row_blocks(a.n, kBlock / TPR);
+    auto launch = [&](auto y, auto t) {
+        hipLaunchKernelGGL((distill_hot_kernel<TPR, decltype(y)::value, decltype(t)::value>), dim3(blocks), dim3(kBlock), 0, s, a,
+                           1.0 / T, out);
+    };
+    if (ybf && tbf) launch(std::true_type(), std::true_type());
+    else if (ybf) launch(std::true_type(), std::false_type());
+    else if (tbf) launch(std::false_type(), std::true_type());
+    else launch(std::false_type(), std::false_type());
+    return blocks;
+}
+
 // Few lanes a row with several quads each share a wavefront's instructions between more rows
 // (2^27 elements, us, float32 / bfloat16: C = 128 (16, 2) 238 / 203, (32, 1) 309 / 295; C = 256 (16, 4) 217 / 169, (64, 1)
 // 317 / 306).
@@ -831,8 +914,9 @@ int launch_any(const Args &a, bool tbf, hipStream_t s) {
 }  // namespace
 
 size_t distill_workspace_bytes(int32_t n, int32_t C) {
-    // partial sums of the loss, then the statistics of split rows (rows that are split are few)
-    size_t bytes = 2 * sizeof(double) * kMaxBlocks;
+    // partial sums of the loss, those of the soft loss at high temperatures, then the statistics of split rows (rows
+    // that are split are few)
+    size_t bytes = 4 * sizeof(double) * kMaxBlocks;
     if (splits_of(n, C) > 1) bytes += sizeof(float) * 3 * static_cast<size_t>(n) * splits_of(n, C);
     return (bytes + 255) / 256 * 256;
 }
@@ -842,12 +926,22 @@ int launch_distill(const void *Y, bool y_bf16, const int32_t *ids, const void *t
                    bool g_bf16, float *loss, void *workspace, hipStream_t s) {
     double *partial = static_cast<double *>(workspace);
     const int64_t elems = static_cast<int64_t>(n) * C;
-    const Args a{Y, teacher, ids, labels, G, partial, reinterpret_cast<float *>(partial + 2 * kMaxBlocks), n, C, K,
+    const Args a{Y, teacher, ids, labels, G, partial, reinterpret_cast<float *>(partial + 4 * kMaxBlocks), n, C, K,
                  T == 1.f ? kLog2e : kLog2e / T, soft * T, hard, g_bf16, elems * (g_bf16 ? 2 : 4) > (int64_t{32} << 20)};
     const int blocks = y_bf16 ? launch_any<true>(a, t_bf16, s) : launch_any<false>(a, t_bf16, s);
-    const int st = hip_status(hipGetLastError());
+    int st = hip_status(hipGetLastError());
     if (st) return st;
-    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kLossThreads), 0, s, partial, blocks,
+    double *hot = nullptr;
+    int hot_blocks = 0;
+    if (T > kHotTemperature) {
+        hot = partial + 2 * kMaxBlocks;
+        hot_blocks = C <= 128 ? launch_hot<16>(a, y_bf16, t_bf16, T, hot, s)
+                   : C <= 2048 ? launch_hot<64>(a, y_bf16, t_bf16, T, hot, s)
+                   : C <= 16384 ? launch_hot<256>(a, y_bf16, t_bf16, T, hot, s)
+                               : launch_hot<1024>(a, y_bf16, t_bf16, T, hot, s);
+        if ((st = hip_status(hipGetLastError()))) return st;
+    }
+    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kLossThreads), 0, s, partial, blocks, hot, hot_blocks,
                        static_cast<double>(soft) * T * T, static_cast<double>(hard), loss);
     return hip_status(hipGetLastError());
 }
