@@ -453,14 +453,15 @@ int dualgcn_backward_data(const void *G, const float *W, const void *M, float *d
 /*
  * The norms of a residual block.  The vectors are float32[F] (device); a NULL weight is all
  * ones, a NULL bias all zeros; only layer norms take biases.  gate goes by the flags (at most
- * one of the three kinds; NULL without any).  eps is at least 2^-126 and scale finite.
+ * one of the three kinds; NULL without any).  eps is at least 2^-126 and scale finite, both in
+ * float32 too: where arithmetic is float32, they are rounded to it.
  */
 typedef struct dualgcn_norm {
     const float *post_weight, *post_bias;   /* the norm after the block (DUALGCN_NORM_POST) */
     const float *pre_weight, *pre_bias;     /* the norm before the next block */
     const void *gate;
-    float eps;
-    float scale;                            /* of the block in the residual stream */
+    double eps;
+    double scale;                           /* of the block in the residual stream */
     uint32_t flags;
 } dualgcn_norm;
 
@@ -481,7 +482,7 @@ typedef struct dualgcn_norm {
  *   Z NULL   the last block, or a block whose next one takes the stream as it is.
  * Rn may be R (the stream is updated in place); no other output may overlap an operand or
  * another output (DUALGCN_ERR_INVALID_ARG).  float32 arithmetic, but that a bfloat16 Rn beside a
- * float32 Z is formed in float64 and rounded once (formed in float32, a sum next to the middle of two
+ * float32 Z is formed in float64, eps and scale as they are, rounded to float32 and stored (formed in float32, a sum next to the middle of two
  * bfloat16 numbers may be stored as either).  Every output element is written by one thread, and the order of every sum is fixed.  n >= 1, 1 <= F <= 8192 (larger F:
  * DUALGCN_ERR_UNSUPPORTED); rows may start at any element.  No workspace.  Asynchronous.
  */

@@ -77,7 +77,7 @@ class PlanInfo(ctypes.Structure):
 class Norm(ctypes.Structure):
     _fields_ = [("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
                 ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p),
-                ("gate", ctypes.c_void_p), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
+                ("gate", ctypes.c_void_p), ("eps", ctypes.c_double), ("scale", ctypes.c_double),
                 ("flags", ctypes.c_uint32)]
 
 
@@ -625,7 +625,7 @@ def norm_residual(R, B=None, *, post_norm=True, post_weight=None, post_bias=None
     makes no Z.  gate: None, float32 [F] (one for each feature), float32 [n, 1] (one for each
     node), or [n, F] in B's type; with gate_sigmoid it holds logits.  Z is float32, or bfloat16
     with norm_bf16 (what `update` takes).  Z norms Rn as it is stored; a bfloat16 Rn beside a float32 Z
-    is summed in float64 and rounded once.  Rn may be R (in place).  Returns (Rn, Z)."""
+    is summed in float64, rounded to float32 and stored.  Rn may be R (in place).  Returns (Rn, Z)."""
     _rows(R, "R")
     n, F = shape = R.shape
     if B is None:

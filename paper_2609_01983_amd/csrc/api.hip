@@ -307,7 +307,7 @@ int check_norm(const dualgcn_norm *p, const void *B, int32_t n, int32_t F, uint3
         !elem_aligned(p->gate, (p->flags & DUALGCN_GATE_FULL) && (p->flags & DUALGCN_IN_BF16)))
         return DUALGCN_ERR_INVALID_ARG;
     // eps is a normal number: the reciprocal root is the hardware's
-    if (!(p->eps >= 0x1p-126f) || !(p->eps < 0x1p127f) || !finite(p->scale)) return DUALGCN_ERR_INVALID_ARG;
+    if (!(p->eps >= 0x1p-126) || !(p->eps < 0x1p127) || !finite(static_cast<float>(p->scale))) return DUALGCN_ERR_INVALID_ARG;
     if (F > dgc::kMaxNormWidth) return DUALGCN_ERR_UNSUPPORTED;
     return DUALGCN_OK;
 }

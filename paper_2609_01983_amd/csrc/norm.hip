@@ -16,7 +16,9 @@
 //
 // Z norms the stream as it is stored.  Where the stream is bfloat16 and Z float32, the last bits of a sum that lies
 // beside the middle of two bfloat16 numbers decide over half a percent of an element of Z (of float32 sums, one
-// element in 20,000 was not the formula's): there the sum is formed in float64 and rounded once.
+// element in 20,000 was not the formula's): there the sum is formed in float64, with eps and scale as the caller has
+// them, rounded to float32 and stored as any float32 sum.  (So a sum that is the middle but for the last bits of a
+// float64, as 0.7 B often makes it, goes to the even number.)
 //
 // Both passes are bound by memory (about one flop a byte): a row stays in the registers of
 // its threads from the load to the store, so every operand is read and every output written
@@ -172,7 +174,7 @@ struct ForwardArgs {
     float eps, scale;
     uint32_t flags;
     bool streaming;                  // outputs past the L2s: stored with a non-temporal hint
-    double inv_f;                    // 1 / F
+    double inv_f, eps64, scale64;    // for float64 sums: 1 / F, and eps and scale as the caller has them
 };
 
 // LAYER: layer norms; A: B and a full gate are bfloat16; S: the stream is; EXACT (S, B there, a float32 Z): the stream's
@@ -231,7 +233,7 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(
             if (post) {
                 Vector(a.w1, F, 1.f).load<Q, TINY>(at, odd, w);
                 if constexpr (LAYER) Vector(a.b1, F, 0.f).load<Q, TINY>(at, odd, c);
-                if constexpr (EXACT) normalise<TPR, Q, LAYER>(v, at, ragged, a.inv_f, static_cast<double>(a.eps), sh, turn);
+                if constexpr (EXACT) normalise<TPR, Q, LAYER>(v, at, ragged, a.inv_f, a.eps64, sh, turn);
                 else normalise<TPR, Q, LAYER>(v, at, ragged, inv_f, a.eps, sh, turn);
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {
@@ -258,20 +260,19 @@ __global__ __launch_bounds__((Shape<TPR, Q>::kBlock)) void norm_residual_kernel(
                     v[q] *= gate;
                 }
             }
-            const Sum node = gn;
-            const Sum scale = a.scale * (sig && (a.flags & DUALGCN_GATE_NODE) ? sigmoid(node) : node);
+            Sum node = gn;
+            if (sig && (a.flags & DUALGCN_GATE_NODE)) node = sigmoid(node);
+            const Sum scale = EXACT ? node : a.scale * node;
             const __amdgpu_buffer_rsrc_t wn = row_window<S>(a.Rn, first, elems);
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     // the next norm (and the backward pass) take the stream as it is stored
-                    if constexpr (EXACT) {
-                        x[q][i] = round_to_bf16(fma(scale, v[q][i], static_cast<double>(x[q][i])));
-                    } else {
-                        x[q][i] = fmaf(scale, v[q][i], x[q][i]);
-                        if constexpr (S) x[q][i] = through_bf16(x[q][i]);
-                    }
+                    // (anew: the compiler would join the two roundings to one)
+                    if constexpr (EXACT) x[q][i] = anew(static_cast<float>(fma(a.scale64, scale * v[q][i], static_cast<double>(x[q][i]))));
+                    else x[q][i] = fmaf(scale, v[q][i], x[q][i]);
+                    if constexpr (S) x[q][i] = through_bf16(x[q][i]);
                 }
                 store_row_quad<S, TINY>(wn, at[q], x[q], odd, a.streaming);
             }
@@ -645,8 +646,8 @@ void with_forward_shape(int32_t F, Fn f) {
 }
 
 // Float64 sums, bound by the vector unit (conversions, and a row's statistics): the widths by powers of two, so that
-// fewer instances do.  2^27 elements, bfloat16 in, float32 Z, RMS and a gate a feature, us: F = 64 289, 128 290, 256 290, 1,024
-// 306, 4,096 339; 192 385, 700 416 (float32 sums of all widths, whose stream was not the formula's: 226 to 293).
+// fewer instances do.  2^27 elements, bfloat16 in, float32 Z, RMS and a gate a feature, us: F = 64 272, 128 269, 256 270, 1,024
+// 292, 4,096 345; 192 358, 700 398 (float32 sums of all widths, whose stream was not the formula's: 226 to 293).
 template <class Fn>
 void with_exact_shape(int32_t F, Fn f) {
     if (F < 4) shape<1, 1>(f);
@@ -716,7 +717,8 @@ bool past_l2(int64_t elems) { return elems * 4 > int64_t{32} << 20; }
 int launch_norm_residual(const dualgcn_norm &p, const void *R, const void *B, void *Rn, void *Z, int32_t n,
                          int32_t F, hipStream_t s) {
     const ForwardArgs a{R, B, p.gate, Rn, Z, p.post_weight, p.post_bias, p.pre_weight, p.pre_bias, n, F,
-                        p.eps, p.scale, p.flags, past_l2(static_cast<int64_t>(n) * F), 1.0 / F};
+                        static_cast<float>(p.eps), static_cast<float>(p.scale), p.flags, past_l2(static_cast<int64_t>(n) * F),
+                        1.0 / F, p.eps, p.scale};
     const bool exact = B && Z && (p.flags & DUALGCN_STREAM_BF16) && !(p.flags & DUALGCN_OUT_BF16);
     const bool layer = p.flags & DUALGCN_NORM_LAYER, act = p.flags & DUALGCN_IN_BF16;
     auto launch = [&](auto tpr, auto quads, auto exactly, auto l, auto b, auto st) {
@@ -754,7 +756,8 @@ int launch_norm_backward(const dualgcn_norm &p, const void *Rn, const void *B, c
                          hipStream_t s) {
     double *const before = static_cast<double *>(workspace);
     BackwardArgs a{Rn, B, p.gate, dZ, dRn, dR, dB, g.gate, p.post_weight, p.post_bias, p.pre_weight,
-                   reinterpret_cast<float *>(before + kSlots * static_cast<size_t>(F)), n, F, p.eps, p.scale, p.flags, 0u,
+                   reinterpret_cast<float *>(before + kSlots * static_cast<size_t>(F)), n, F, static_cast<float>(p.eps),
+                   static_cast<float>(p.scale), p.flags, 0u,
                    past_l2(static_cast<int64_t>(n) * F)};
     SumOut out{};
     int wanted = 0;

@@ -167,14 +167,6 @@ __device__ __forceinline__ void store_quad(void *base, int64_t at, int count, ro
 // The value of a float32 as it is when stored in bfloat16.
 __device__ __forceinline__ float through_bf16(float f) { return static_cast<float>(static_cast<__bf16>(f)); }
 
-// A float64 rounded to bfloat16's 8 significant bits, to nearest even, as a float32.  (By way of a float32 rounded
-// to nearest it could land on the middle between two bfloat16 numbers and go the wrong way.)  NaN stays NaN.
-__device__ __forceinline__ float round_to_bf16(double d) {
-    uint32_t hi = static_cast<uint32_t>(__double2hiint(d)) | (__double2loint(d) != 0 ? 1u : 0u);   // 7 of its 20 fraction bits stay
-    hi = hi + 0xFFFu + (hi >> 13 & 1u) & ~0x1FFFu;
-    return d != d ? __uint_as_float(0x7FC00000u) : static_cast<float>(__hiloint2double(static_cast<int>(hi), 0));
-}
-
 // A value that the optimiser takes for a new one: what was computed from it before is not kept in
 // registers for its next use.
 template <class T>
