@@ -550,9 +550,10 @@ int dualgcn_distill_workspace(int32_t n, int32_t C, int32_t K, size_t *bytes);
  * is infinite if the teacher or the label takes it).  A row with a NaN, a +infinity or nothing
  * above -infinity among the logits it needs gives NaN, in its own row of G and in the loss.
  * float32 arithmetic, the loss joined in float64 in a fixed order; G does not depend on timing.
- * A row's part of soft is off by up to about 1e-6 soft_scale temperature^2 up to a temperature of 8;
+ * A row's part of soft is off by a few 1e-6 of soft_scale temperature^2 up to a temperature of 8;
  * above, soft is formed in float64 (in a launch of its own).  Q and P of G are float32 at any
- * temperature: an element is off by up to about 1e-5 soft_scale temperature Q, whatever Q - P is.
+ * temperature: an element is off by about 2^-16 soft_scale temperature (Q + P) at most, whatever
+ * Q - P is.
  * n >= 1, 1 <= C < 2^20, 1 <= K <= 4096 (larger: DUALGCN_ERR_UNSUPPORTED), temperature in
  * [2^-14, 2^14], finite scales; outputs overlap nothing.  `workspace` (device, 256-byte aligned)
  * holds at least dualgcn_distill_workspace bytes; calls that may run at the same time need one
@@ -600,7 +601,8 @@ int dualgcn_quantize_weight_fp8(const float *W, int32_t F_in, int32_t F_out, int
  * F_out x F_in row-major: W transposed) with sw (float32[ceil(F_out / 128)][ceil(F_in / 128)], one
  * for each 128 x 128 block); T (device, n x F_out row-major, float32, or bfloat16 with
  * DUALGCN_OUT_BF16).  The scales may be any float32 numbers, and their product may lie outside
- * float32's range (rows with a scale outside [2^-50, 2^50] are slower).  Products of a block (of the e4m3
+ * float32's range (rows with a scale outside [2^-85, 2^85], and any with a scale of W outside
+ * [2^-40, 2^40], are slower).  Products of a block (of the e4m3
  * numbers widened to bfloat16, which is exact) are summed by the matrix cores in float32,
  * multiplied by the two scales and added in float32, block after block, in an order that depends
  * on the shape only.  The gradient G W^T is the same call on a quantised G and W not transposed.

@@ -238,9 +238,12 @@ struct Scales {
         }
     }
 };
-// Is a scale outside [2^-50, 2^50]?  (Two inside have a product that may be used as it is; zeros, infinities and NaN may too.)
+// Is a scale of X outside [2^-85, 2^85], one of W outside [2^-40, 2^40]?  Two inside have a product that may be used as it is:
+// a normal number.  (Zeros, infinities and NaN may too.)  X has the wider range: gradients are small, weights are not.
+constexpr int kFarX = 85, kFarW = 40;
+template <int E>
 __device__ __forceinline__ bool far_scale(float x) {
-    return static_cast<uint32_t>(__builtin_amdgcn_frexp_expf(x) + 49) > 99u;
+    return static_cast<uint32_t>(__builtin_amdgcn_frexp_expf(x) + E - 1) > 2u * E - 1u;
 }
 
 __device__ __forceinline__ void store_tile(const ProductArgs &a, int64_t row, int col, int last, f32x4 v) {
@@ -275,7 +278,8 @@ constexpr int kXcds = 8;
 constexpr int kMostBlocks = 8;                       // F_in up to 1,024
 // The 32 rows of a wavefront from row0 on once more, a tile of 16 x 16 at a time, with scales of any size; `w`: W in
 // LDS.  Apart from the main loop, so that it takes few of its registers: tests for such scales alone cost
-// (us with and without) 2^22 rows 32 -> 16 101, 92, 2^20 128 -> 64 64, 60, 200,003 528 -> 200 82, 79, nothing where rows are wider.
+// (us with and without) 2^22 rows 32 -> 16 100, 93, 2^20 128 -> 64 64, 60, 200,003 528 -> 200 82, 80, nothing where rows are wider.
+// Rows that need it take 1.3 to 4.4 times as long (all of 2^22 256 -> 128 1,530, 645; of 2^19 1,024 -> 1,024 6,800, 1,545).
 // With a second way beside the main loop's products, whose registers then bound the kernel, 528 -> 200 took 91.
 template <int CT>
 __device__ __forceinline__ void product_of_far_scales(const ProductArgs &a, const __bf16 *w, int64_t row0, int c0, int turn,
@@ -378,15 +382,15 @@ __global__ __launch_bounds__(kThreads, ALONE ? 2 : CT == 1 ? 6 : CT <= 4 ? 4 : 2
             for (int t = 0; t < kRowTiles; ++t) {
                 in[t].get(a.K, b, g, x[t]);
                 sc[t] = sn[t];
-                far |= far_scale(sc[t]);
+                far |= far_scale<kFarX>(sc[t]);
             }
             // the next block of this tile, or the first of the next tile (past the last: zeros), into the
             // registers that the widened ones have left
             const bool more = b + 1 < a.blocks;
             request(more ? tile : tile + stride, more ? b + 1 : 0);
             const float sw0 = column_scales[0][b], sw1 = column_scales[1][b];
-            far |= far_scale(sw0);
-            far |= far_scale(sw1);
+            far |= far_scale<kFarW>(sw0);
+            far |= far_scale<kFarW>(sw1);
             auto multiply = [&](auto steps) {
 #pragma unroll
                 for (int c = 0; c < CT; ++c) {

@@ -695,7 +695,8 @@ void with_flags(Fn f, bool b, More... more) {
 
 // Workgroups of a backward pass, each with a partial sum of every column.  Its wavefronts have two
 // rows in flight each, so two workgroups a CU fill the memory's queues with float32 operands
-// (F = 128, us at 2, 3, 4 a CU: 287 / 299 / 316), and four where every operand is bfloat16 (226 / 179 / 159).
+// (us at 2, 3, 4 a CU: 20,001 x 99 20.7, 20.4, 20.6; 50,000 x 64 20.4, 21.7, 20.4; 30,000 x 256 36.7, 38.6, 36.7; 100,000 x 256 112,
+// 121, 123; 60,000 x 512 139, 143, 157; 2^20 x 128 606, 592, 672), and four where every operand is bfloat16 (226, 179, 159).
 int backward_blocks(int64_t n, int32_t F, bool all_bf16, int &groups) {
     int per_cu = 1, most = 1;
     with_backward_shape(F, [&](auto tpr, auto quads) {
