@@ -255,10 +255,12 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int64_t row, in
 
 // Workgroups of eight wavefronts, 32 rows each, with W of CT tiles of 16 columns in LDS.  Measured:
 // 2^22 rows 256 -> 128 float32 640 us, 3.25 GB, 5.0 TB/s, bound by memory; 2^19 rows 1,024 -> 1,024 1.59 ms, 690 TFLOP/s,
-// and 200,003 rows 528 -> 200 82 us, 515 TFLOP/s: the matrix unit and LDS (which have equal shares: 1 KB of W
-// for two products) are each busy about a third of the time, and the wavefronts wait for each other's
-// turns.  Requests of X two to four blocks ahead, or W's reads ordered a tile ahead of its products, made
-// wide products 2% faster and narrow ones 3 to 15% slower.
+// and 200,003 rows 528 -> 200 84 us, 500 TFLOP/s: there the matrix unit is busy 31 and 33% of the time, the vector unit
+// 34 and 43% (widening X, scaling sums), LDS 16 and 18%, by their counters, and the wavefronts wait for each
+// other's turns.  Taking all registers where W leaves room for one workgroup a CU, for W's fragments ahead of their products,
+// was 1 to 3% faster for 528 -> 200, 512 -> 200 and 400 -> 400 and 1 to 2% slower for 512 -> 512, 672 -> 128 and 1,024 -> 256.
+// Requests of X two to four blocks ahead, or W's reads ordered a tile ahead of its products, made wide products 2%
+// faster and narrow ones 3 to 15% slower.
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kRowTiles = 2;
@@ -310,8 +312,8 @@ __device__ __forceinline__ void product_of_far_scales(const ProductArgs &a, cons
 }
 
 // (the second bound: two workgroups a CU, three for one tile)
-template <int CT, bool ALONE>
-__global__ __launch_bounds__(kThreads, ALONE ? 2 : CT == 1 ? 6 : CT <= 4 ? 4 : 2) void product_kernel(ProductArgs a, int32_t slices, int32_t side) {
+template <int CT>
+__global__ __launch_bounds__(kThreads, CT == 1 ? 6 : CT <= 4 ? 4 : 2) void product_kernel(ProductArgs a, int32_t slices, int32_t side) {
     extern __shared__ uint4 lds[];
     __bf16 *w = reinterpret_cast<__bf16 *>(lds);
     const int tile_elems = lds_tile(a.blocks);
@@ -391,31 +393,26 @@ __global__ __launch_bounds__(kThreads, ALONE ? 2 : CT == 1 ? 6 : CT <= 4 ? 4 : 2
             const float sw0 = column_scales[0][b], sw1 = column_scales[1][b];
             far |= far_scale<kFarW>(sw0);
             far |= far_scale<kFarW>(sw1);
-            auto multiply = [&](auto steps) {
 #pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    const __bf16 *p = w + c * tile_elems + b * kSteps * 512 + lane * 8;
-                    f32x4 s[kRowTiles];
+            for (int c = 0; c < CT; ++c) {
+                const __bf16 *p = w + c * tile_elems + b * kSteps * 512 + lane * 8;
+                f32x4 s[kRowTiles];
 #pragma unroll
-                    for (int t = 0; t < kRowTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < kRowTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int k = 0; k < decltype(steps)::value; ++k) {
-                        const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(p + 512 * k);
+                for (int k = 0; k < kSteps; ++k) {
+                    const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(p + 512 * k);
 #pragma unroll
-                        for (int t = 0; t < kRowTiles; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[t][k], s[t], 0, 0, 0);
-                    }
-                    const float swc = c < turn ? sw0 : sw1;
-#pragma unroll
-                    for (int t = 0; t < kRowTiles; ++t) {
-                        const float f = sc[t] * swc;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[t][c][i] = fmaf(f, s[t][i], acc[t][c][i]);
-                    }
+                    for (int t = 0; t < kRowTiles; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[t][k], s[t], 0, 0, 0);
                 }
-            };
-            // a last block of up to 64 elements has them all in its first two steps
-            if (ALONE && a.K - b * kBlock <= 64) multiply(std::integral_constant<int, kSteps / 2>());
-            else multiply(std::integral_constant<int, kSteps>());
+                const float swc = c < turn ? sw0 : sw1;
+#pragma unroll
+                for (int t = 0; t < kRowTiles; ++t) {
+                    const float f = sc[t] * swc;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[t][c][i] = fmaf(f, s[t][i], acc[t][c][i]);
+                }
+            }
         }
         const int64_t row0 = tile * kRowsPerBlock;
         if (__ballot(far)) {                         // scales whose products may not be used as they are: not from acc
@@ -493,10 +490,10 @@ inline int64_t over(size_t lds) { return lds <= 64 * 1024 ? 16 : 2; }
 // past that the shared L2 wins).
 constexpr int64_t kSideTiles = 64;
 
-template <int CT, bool ALONE>
+template <int CT>
 int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
     const size_t lds = static_cast<size_t>(CT) * lds_tile(a.blocks) * sizeof(uint16_t);
-    const int st = allow_lds(reinterpret_cast<const void *>(&product_kernel<CT, ALONE>), lds);
+    const int st = allow_lds(reinterpret_cast<const void *>(&product_kernel<CT>), lds);
     if (st) return st;
     const int64_t tiles = (static_cast<int64_t>(a.n) + kRowsPerBlock - 1) / kRowsPerBlock;
     // registers: up to 128 a thread for four tiles of columns, hence two workgroups a CU
@@ -504,20 +501,8 @@ int launch_product(const ProductArgs &a, int slices, hipStream_t s) {
     // row tiles at a time, a whole number for each XCD
     const int side = tiles >= kSideTiles ? kXcds : 1;
     const int64_t per = std::max<int64_t>(1, (std::min<int64_t>(tiles, over(lds) * resident / slices) + side - 1) / side) * side;
-    hipLaunchKernelGGL((product_kernel<CT, ALONE>), dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices, side);
+    hipLaunchKernelGGL((product_kernel<CT>), dim3(static_cast<unsigned>(per * slices)), dim3(kThreads), lds, s, a, slices, side);
     return hip_status(hipGetLastError());
-}
-
-// ALONE: W leaves no room for a second workgroup on a CU, so the kernel may take all registers, which the
-// compiler fills with W's fragments ahead of their products, and a short last block is skipped by half (us
-// ALONE and not: 200,003 rows 528 -> 200 92, 98; 512 -> 200 73, 78; 2^20 1,024 -> 256 804, 820, 512 -> 512 830, 822; with
-// room for two 2^22 256 -> 128 669, 649; 2^20 128 -> 64 86, 80).
-template <int CT>
-int launch_tiles(const ProductArgs &a, int slices, hipStream_t s) {
-    [[maybe_unused]] const bool alone = 2 * static_cast<size_t>(CT) * lds_tile(a.blocks) * sizeof(uint16_t) > kLds;
-    if constexpr (CT > 2)                            // (two tiles of 1,024 leave room)
-        if (alone) return launch_product<CT, true>(a, slices, s);
-    return launch_product<CT, false>(a, slices, s);
 }
 
 // Slices of equal width: as few as fit, then as narrow as those need.
@@ -526,14 +511,14 @@ int launch_slices(const ProductArgs &a, int most, hipStream_t s) {
     while (most > 1 && static_cast<size_t>(most) * lds_tile(a.blocks) * sizeof(uint16_t) > kLds) --most;
     const int slices = (cols + most - 1) / most;
     switch ((cols + slices - 1) / slices) {
-        case 1: return launch_tiles<1>(a, slices, s);
-        case 2: return launch_tiles<2>(a, slices, s);
-        case 3: return launch_tiles<3>(a, slices, s);
-        case 4: return launch_tiles<4>(a, slices, s);
-        case 5: return launch_tiles<5>(a, slices, s);
-        case 6: return launch_tiles<6>(a, slices, s);
-        case 7: return launch_tiles<7>(a, slices, s);
-        default: return launch_tiles<8>(a, slices, s);
+        case 1: return launch_product<1>(a, slices, s);
+        case 2: return launch_product<2>(a, slices, s);
+        case 3: return launch_product<3>(a, slices, s);
+        case 4: return launch_product<4>(a, slices, s);
+        case 5: return launch_product<5>(a, slices, s);
+        case 6: return launch_product<6>(a, slices, s);
+        case 7: return launch_product<7>(a, slices, s);
+        default: return launch_product<8>(a, slices, s);
     }
 }
 
