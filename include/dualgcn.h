@@ -511,7 +511,7 @@ int dualgcn_norm_residual_backward_workspace(int32_t n, int32_t F, size_t *bytes
  *   grads the parameters' gradients; NULL = none.  post_* needs DUALGCN_NORM_POST, pre_* needs
  *         dZ, gate a gate.
  * The rows' statistics are computed again from Rn and B.  Sums over the rows are formed in
- * float32 over at most 288 of them and joined in float64 in a fixed order (in `workspace`, device,
+ * float32 over at most 160 of them and joined in float64 in a fixed order (in `workspace`, device,
  * 256-byte aligned, at least dualgcn_norm_residual_backward_workspace bytes), so results do not
  * depend on timing.  Calls that may run at the same time need a workspace each.  Outputs overlap
  * nothing but as said for dR.  Limits as for

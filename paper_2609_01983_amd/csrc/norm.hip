@@ -37,8 +37,9 @@ template <int TPR>
 constexpr int kMostBlocks = TPR > 256 ? kMaxBlocks / 2 : kMaxBlocks;     // (at most one a CU where they are so large)
 // Rows that a group of threads adds to a column sum in float32, one after another.  The error of such a chain grows
 // with its length (67M rows of 4 in chains of 4,096 terms of 0.1: 4e-5 of the sum), so longer passes are done in parts,
-// whose sums are added in float64 (us whole and in parts: 2^21 x 128 1,325, 1,215; 2^17 x 4,096 bfloat16 1,675, 1,690).
-constexpr int kChain = 256;
+// whose sums are added in float64 (us whole, in parts of 256, 128, 64 steps: 2^20 x 128 605, 605, 591, 602; 2^21 x 128 1,295, 1,200,
+// 1,169, 1,186; 2^17 x 1,024 595, 596, 607, 633; 2^17 x 4,096 bfloat16 1,654, 1,670, 1,709, 1,784).
+constexpr int kChain = 128;
 constexpr int64_t kMaxForwardBlocks = int64_t{1} << 21;
 
 // ------------------------------------------------------------------ shared by both directions

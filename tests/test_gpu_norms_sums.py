@@ -1,9 +1,9 @@
 """The norms around a block over many rows: column sums of passes so long that they are done in parts,
 rows over several steps of every shape, and outputs past 32 MiB with a block and every pair of types.
 
-A column sum adds at most 256 rows in float32 one after another (a group of threads), then at most 31 groups, all else
-in float64: 288 roundings, each of at most u = 2^-24 of the sum so far, which for terms of one sign
-grows to the whole sum evenly: 144 u of the terms' magnitudes, and K_BACK u (normref.py) for the terms themselves."""
+A column sum adds at most 128 rows in float32 one after another (a group of threads), then at most 31 groups, all else
+in float64: 160 roundings, each of at most u = 2^-24 of the sum so far, which for terms of one sign
+grows to the whole sum evenly: 80 u of the terms' magnitudes, and K_BACK u (normref.py) for the terms themselves."""
 import numpy as np
 import pytest
 import torch
@@ -13,7 +13,7 @@ from test_gpu_norms import _case, _check_backward, _check_forward
 
 pytestmark = pytest.mark.gpu
 
-SUM = ref.U * (144 + ref.K_BACK)
+SUM = ref.U * (80 + ref.K_BACK)
 
 
 @pytest.fixture(scope="module")
