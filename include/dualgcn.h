@@ -482,9 +482,11 @@ typedef struct dualgcn_norm {
  *   Z NULL   the last block, or a block whose next one takes the stream as it is.
  * Rn may be R (the stream is updated in place); no other output may overlap an operand or
  * another output (DUALGCN_ERR_INVALID_ARG).  float32 arithmetic, but that a bfloat16 Rn beside a
- * float32 Z is formed in float64, eps and scale as they are, rounded to float32 and stored (formed in float32, a sum next to the middle of two
- * bfloat16 numbers may be stored as either).  Every output element is written by one thread, and the order of every sum is fixed.  n >= 1, 1 <= F <= 8192 (larger F:
- * DUALGCN_ERR_UNSUPPORTED); rows may start at any element.  No workspace.  Asynchronous.
+ * float32 Z is formed in float64, with eps and scale as they are, rounded to float32 and stored
+ * (formed in float32, a sum next to the middle of two bfloat16 numbers may be stored as either).
+ * Every output element is written by one thread, and the order of every sum is fixed.  n >= 1,
+ * 1 <= F <= 8192 (larger F: DUALGCN_ERR_UNSUPPORTED); rows may start at any element.  No
+ * workspace.  Asynchronous.
  */
 int dualgcn_norm_residual(const dualgcn_norm *norm, const void *R, const void *B, void *Rn, void *Z,
                           int32_t n, int32_t F, void *stream);

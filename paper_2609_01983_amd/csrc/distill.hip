@@ -226,8 +226,8 @@ __device__ __forceinline__ void write_partial(double soft, double hard, double *
 }
 
 // Rows whose logits stay in the registers of their TPR threads, Q quads each.  YBF, TBF: the
-// logits, the teacher's are bfloat16.  Measured: 2^22 x 64 with 16 entries a row, T = 4 and labels, 2.7 GB in 527 us,
-// 5.1 TB/s; 30,007 x 47 with 8 entries 13 MB in 7.4 us.  Short rows are bound by the vector unit as much
+// logits, the teacher's are bfloat16.  Measured: 2^22 x 64 with 16 entries a row, T = 4 and labels, 2.7 GB in 526 us a call
+// (536 to 556 in a trace), 5.1 TB/s; 30,007 x 47 with 8 entries 13 MB in 7.4 us.  Short rows are bound by the vector unit as much
 // as by memory: two exponentials a logit, three reductions a row and the entries' own work.
 template <int TPR, int Q, bool YBF, bool TBF>
 __global__ __launch_bounds__((TPR > 64 ? TPR : kThreads)) void distill_rows_kernel(Args a) {
@@ -459,7 +459,8 @@ __device__ __forceinline__ void put_zeros(const Args &a, int64_t row, int c0, in
 
 // A row that QUADS quads of THREADS threads hold.  The second bound keeps a CU's registers full.
 // Measured, 16 entries a row, T = 2, labels, float32 / bfloat16: 16,384 x 8,192 192 / 130 us (5.6 / 4.1 TB/s), 8,192 x 16,384
-// 218 / 124 us, 65,536 x 2,000 223 / 158 us; bfloat16 is bound by its four exponentials a logit.
+// 218 / 124 us, 65,536 x 2,000 223 / 158 us; with bfloat16 the vector unit is busy all the time by its counter (four exponentials a
+// logit), with float32 77%.
 template <bool YBF, bool TBF, bool ODD, int THREADS, int QUADS>
 __global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(Args a) {
     __shared__ row_f32x4 sh[row_reduce_quads<THREADS>()];
@@ -630,7 +631,7 @@ __global__ __launch_bounds__(kSweep) void distill_stats_kernel(Args a) {
 }
 
 // The gradient of rows of any length.  With one split the workgroup sweeps its rows' statistics
-// itself; else they come from `stats`.  Measured: 4,095 x 131,072 bfloat16, T = 1, 64 entries: 2.15 GB in 479 us,
+// itself; else they come from `stats`.  Measured: 4,095 x 131,072 bfloat16, T = 1, 64 entries: 2.15 GB in 479 us a call,
 // 4.5 TB/s, and a second reading of Y, 1.07 GB, from beyond the L2 and for the most part not from HBM.
 template <bool YBF, bool TBF, bool ODD>
 __global__ __launch_bounds__(kSweep, 4) void distill_sweep_kernel(Args a) {

@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t to_e4m3(row_f32x4 v) {
 
 // A workgroup takes 16 rows, 16 lanes each, and up to eight blocks of them (blockIdx.y); a lane has
 // the elements from 4 l and 64 + 4 l on of a block, and two blocks' loads are in flight.  Bound by
-// memory: 2^21 x 256 464 us from float32, 280 from bfloat16 (5.8 TB/s); 200,003 x 528 bfloat16 68 us (4.6 TB/s: rows
+// memory: 2^21 x 256 464 us from float32, 280 from bfloat16 (5.8 TB/s); 200,003 x 528 bfloat16 69 to 73 us (4.3 to 4.6 TB/s: rows
 // of 528 bytes end inside lines, which are written twice, 128 MB for 106).
 constexpr int kQuantThreads = 256;
 constexpr int kQuantLanes = 16;
@@ -254,7 +254,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int64_t row, in
 }
 
 // Workgroups of eight wavefronts, 32 rows each, with W of CT tiles of 16 columns in LDS.  Measured:
-// 2^22 rows 256 -> 128 float32 640 us, 3.25 GB, 5.0 TB/s, bound by memory; 2^19 rows 1,024 -> 1,024 1.59 ms, 690 TFLOP/s,
+// 2^22 rows 256 -> 128 float32 652 us a call, 3.25 GB, 5.0 TB/s, bound by memory; 2^19 rows 1,024 -> 1,024 1.55 ms, 710 TFLOP/s,
 // and 200,003 rows 528 -> 200 84 us, 500 TFLOP/s: there the matrix unit is busy 31 and 33% of the time, the vector unit
 // 34 and 43% (widening X, scaling sums), LDS 16 and 18%, by their counters, and the wavefronts wait for each
 // other's turns.  Taking all registers where W leaves room for one workgroup a CU, for W's fragments ahead of their products,

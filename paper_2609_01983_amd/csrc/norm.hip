@@ -351,8 +351,8 @@ struct RowIn {
 // LAYER: layer norms; A: B and a full gate are bfloat16; S: the stream and its gradients are; G: dZ,
 // dB and a full gate's gradient are.  The workgroups are few and keep their column sums over all their
 // rows, so that the partial sums are small beside the rows.
-// Measured: 2^20 x 128 float32, RMS norms and a gate a feature, 3.2 GB in 562 to 595 us, 5.4 to 5.7 TB/s; 8,191 x 4,096 bfloat16
-// 403 MB in 103 us, 3.9 TB/s, bound by the two reductions of each row of which a workgroup of 1,024 threads
+// Measured: 2^20 x 128 float32, RMS norms and a gate a feature, 3.2 GB in two parts of 289 to 300 us, 5.4 to 5.6 TB/s; 8,191 x
+// 4,096 bfloat16 403 MB in 106 to 109 us, 3.8 TB/s, bound by the two reductions of each row of which a workgroup of 1,024 threads
 // has one at work and one on its way; 20,001 x 99 with layer norms and a sigmoid gate 55 MB in 23 us: five rounds of
 // latency, and the columns' sums joined at the end.
 template <int TPR, int Q, bool LAYER, bool A, bool S, bool G>
