@@ -9,8 +9,10 @@
  * layer before it; for training, the loss gradient and
  * the backward products of a layer; the values of other aggregators on the same
  * structure; and plans saved and loaded across runs.  For deep GCNs: the norms, gate and
- * residual scale between two blocks and their gradients, the loss of a student
- * against its teacher's top logits, and the update phase from 8-bit operands.
+ * residual scale between two blocks and their gradients, group norms with an activation over
+ * the graphs of a batch and their gradients, the loss of a student
+ * against its teacher's top logits, the gradients' norm with clipping and the clipped step,
+ * and the update phase from 8-bit and from 4-bit operands.
  *
  * Conventions for every entry point
  *   - Pointers named *_h are host memory; every other array pointer is device
@@ -614,6 +616,155 @@ int dualgcn_quantize_weight_fp8(const float *W, int32_t F_in, int32_t F_out, int
  */
 int dualgcn_update_fp8(const void *X, const float *sx, const void *W, const float *sw, void *T, int32_t n,
                        int32_t F_in, int32_t F_out, uint32_t flags, void *stream);
+
+/* ------------------------------------------------------------------ batches of graphs */
+
+/* Flags of the group norms (with DUALGCN_RELU, DUALGCN_IN_BF16, DUALGCN_OUT_BF16 and DUALGCN_GRAD_BF16). */
+#define DUALGCN_SILU 4096u       /* act(p) = p / (1 + exp(-p)) */
+#define DUALGCN_ZERO_REST 8192u  /* rows of no graph receive zeros; else they are left as they were */
+
+/*
+ * A group norm over the graphs of a batch (Sec. 2.1: rows are nodes).  ptr (device, int32[graphs + 1], not
+ * decreasing, within [0, n]): graph b has the rows [ptr[b], ptr[b + 1]), none if they are equal.  NULL: one graph
+ * of all n rows (graphs is ignored).  The offsets are read on the device; where they are out of order or of range
+ * the results are undefined, but nothing outside the operands is read or written.
+ * groups divides F: group g has the features [g F / groups, (g + 1) F / groups).  weight and bias are
+ * float32[F] (device); NULL is all ones and all zeros.  eps is at least 2^-126.  act is the identity, or by
+ * the flags ReLU or SiLU.
+ */
+typedef struct dualgcn_group_norm {
+    const int32_t *ptr;
+    const float *weight, *bias;
+    double eps;
+    int32_t graphs;
+    int32_t F, groups;
+    uint32_t flags;
+} dualgcn_group_norm;
+
+/* Bytes of the workspace dualgcn_group_norm_act needs (host only). */
+int dualgcn_group_norm_act_workspace(const dualgcn_group_norm *norm, int32_t n, size_t *bytes);
+
+/*
+ * dualgcn_group_norm_act -- for every graph and group, with m and v the mean and variance (divided by the number)
+ * of the graph's features in the group, over its nodes and the group's features:
+ *   u = (X - m) / sqrt(v + eps),  Y = act(weight * u + bias)
+ *
+ * X (device, n x F row-major, float32, or bfloat16 with DUALGCN_IN_BF16); Y (device, n x F, float32, or
+ * bfloat16 with DUALGCN_OUT_BF16), which may be X if the types are the same; stats (device,
+ * float64[graphs][groups][2], 16-byte aligned) receives m and 1 / sqrt(v + eps), which the backward pass reads (0
+ * and 1 / sqrt(eps) for a graph without nodes).  Rows of no graph are left as they were in Y, or
+ * with DUALGCN_ZERO_REST filled with zeros.  A group with an infinity or a NaN is NaN throughout.
+ * Sums are float64, in a fixed order; u is formed from float32 differences with m as two float32 numbers.
+ * n from 1 to 2^31 - 2^22, 1 <= F <= 8192, up to 2^30 graphs (larger: DUALGCN_ERR_UNSUPPORTED); rows may start at
+ * any element.
+ * `workspace` (device, 256-byte aligned) holds at least dualgcn_group_norm_act_workspace bytes; calls that may run
+ * at the same time need one each.  Outputs overlap nothing but as said for Y.  Asynchronous.
+ */
+int dualgcn_group_norm_act(const dualgcn_group_norm *norm, const void *X, void *Y, double *stats, int32_t n,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of the workspace dualgcn_group_norm_act_backward needs (host only). */
+int dualgcn_group_norm_act_backward_workspace(const dualgcn_group_norm *norm, int32_t n, size_t *bytes);
+
+/*
+ * dualgcn_group_norm_act_backward -- the gradients of dualgcn_group_norm_act.
+ *
+ * norm, X and stats as in (and from) the forward call; dY (device, n x F, float32, or bfloat16 with
+ * DUALGCN_GRAD_BF16) the gradient of Y; dX (in dY's type; may be dY) the gradient of X, on rows of no graph as
+ * said for Y; dweight and dbias (device, float32[F]) those of the vectors, over the rows of all graphs; each NULL if it
+ * is not wanted.  The sign of weight * u + bias decides what a ReLU passes, as float64 arithmetic gives
+ * it.  Sums are float64 (of float32 terms), in a fixed order.  DUALGCN_OUT_BF16 has no meaning here
+ * and is ignored.  Limits, workspace and overlaps as for dualgcn_group_norm_act.  Asynchronous.
+ */
+int dualgcn_group_norm_act_backward(const dualgcn_group_norm *norm, const void *X, const void *dY, const double *stats,
+                                    void *dX, float *dweight, float *dbias, int32_t n, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------ clipped gradients */
+
+/* One tensor of a call on many: `count` elements (0 or more) of a gradient, float32, or bfloat16 with
+ * flags = DUALGCN_GRAD_BF16 (else 0), at any element's address. */
+typedef struct dualgcn_grad {
+    const void *grad;
+    const float *weight;         /* dualgcn_clipped_sgd: the weights; else NULL */
+    void *out;                   /* where the result goes (dualgcn_grad_norm: NULL) */
+    int64_t count;
+    uint32_t flags;
+} dualgcn_grad;
+
+/* Bytes of the workspace that the three calls below need for so many tensors (host only). */
+int dualgcn_grad_norm_workspace(int32_t tensors, size_t *bytes);
+
+/*
+ * Training with clipped gradients (dualgcn_weight_grad's own step is applied before the other layers' gradients are
+ * known).  grads_h (host; read before the call returns) lists 1 to 2^20 tensors of up to 2^40 elements.  With
+ *   norm = sqrt(the sum of all elements' squares)   (device, float32[1])
+ *   f    = 1 if norm + eps <= max_norm, else max_norm / (norm + eps)
+ * dualgcn_grad_norm     norm
+ * dualgcn_clip_grads    norm, and out = f grad in grad's type; out may be grad
+ * dualgcn_clipped_sgd   norm, and out = weight - lr f grad, float32; out may be weight
+ * The squares are summed in float64 in a fixed order, and the results formed in float64 and rounded once (to
+ * bfloat16: to float32 first); f goes by the float64 norm, also where that is past float32's range.  A gradient listed
+ * twice counts twice.  An infinite element gives f = 0 (and NaN at
+ * that element), a NaN gives NaN everywhere; max_norm (0 or more) may be infinite: then f is 1.  eps is 0 or more
+ * and finite, lr finite.  `workspace` (device, 256-byte aligned) holds at least dualgcn_grad_norm_workspace bytes; calls
+ * that may run at the same time need one each.  No output overlaps an operand (but as said for out) or
+ * another output.  Asynchronous.
+ */
+int dualgcn_grad_norm(const dualgcn_grad *grads_h, int32_t tensors, float *norm, void *workspace, size_t workspace_bytes,
+                      void *stream);
+int dualgcn_clip_grads(const dualgcn_grad *grads_h, int32_t tensors, double max_norm, double eps, float *norm,
+                       void *workspace, size_t workspace_bytes, void *stream);
+int dualgcn_clipped_sgd(const dualgcn_grad *grads_h, int32_t tensors, double max_norm, double eps, double lr, float *norm,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------ 4-bit operands */
+
+/* Elements that share a scale in the 4-bit operands. */
+#define DUALGCN_MX_BLOCK 32
+
+/*
+ * The update phase from 4-bit operands in the microscaled form: elements in e2m1 (sign, 2 exponent bits of bias
+ * 1, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two a byte, the first in the lower four bits, and for each 32
+ * consecutive elements of a row a scale in e8m0 (one byte s: 2^(s - 127); 255 is NaN).  A row of F elements has
+ * blocks = ceil(F / 32) scales and 16 blocks bytes; the places behind its end hold 0.
+ *
+ * dualgcn_quantize_mxfp4 -- X (device, n x F row-major, float32, or bfloat16 with DUALGCN_IN_BF16) into Q (device,
+ * n x 16 blocks bytes) and scales (device, n x blocks bytes).  A scale is the least power of two, 2^-127 or more,
+ * that brings the block's largest magnitude to 7 or below (1 for zeros); elements are divided by it and
+ * rounded once, to nearest even, and what is then above 6 to 6: no element is off by more than half a
+ * step.  A block with an infinity or a NaN has the scale NaN.  1 <= F < 2^20; n ceil(F / 32) < 2^32 - 256 (larger:
+ * DUALGCN_ERR_UNSUPPORTED).  Q 16-byte aligned.  Asynchronous.
+ *
+ * dualgcn_quantize_weight_mxfp4 -- W (device, float32 F_in x F_out row-major) as dualgcn_update_mxfp4 reads it: with
+ * `transpose` not 0, Q is F_out rows of F_in elements (for X W); with 0, F_in rows of F_out elements (for G W^T,
+ * the gradient's product; the blocks then run along F_out, and the numbers differ from the others').
+ * 1 <= F_in, F_out <= 65536 (larger: DUALGCN_ERR_UNSUPPORTED).  Asynchronous.
+ *
+ * dualgcn_dequantize_mxfp4 -- the values of Q and scales as X (device, n x F, float32, or bfloat16 with
+ * DUALGCN_OUT_BF16), what dualgcn_spmm gathers: exact, but that values from 2^128 on are infinite.  Limits as for
+ * dualgcn_quantize_mxfp4.  Asynchronous.
+ */
+int dualgcn_quantize_mxfp4(const void *X, int32_t n, int32_t F, uint32_t flags, void *Q, void *scales, void *stream);
+int dualgcn_quantize_weight_mxfp4(const float *W, int32_t F_in, int32_t F_out, int32_t transpose, void *Q, void *scales,
+                                  void *stream);
+int dualgcn_dequantize_mxfp4(const void *Q, const void *scales, int32_t n, int32_t F, uint32_t flags, void *X, void *stream);
+
+/*
+ * dualgcn_update_mxfp4 -- T = X W from 4-bit operands on the matrix cores (dualgcn_update_fp8's companion: an
+ * eighth of float32 features' bytes).
+ *
+ * X (device, n rows of F_in elements) with sx, W (device, F_out rows of F_in elements: W transposed) with sw, in
+ * the form above; T (device, n x F_out row-major, float32, or bfloat16 with DUALGCN_OUT_BF16).  The places
+ * behind F_in in a row's last block are multiplied too: one of the operands holds 0 there (both do, as the
+ * quantisers write them).  Products and sums are formed by the matrix cores in float32, in an order that depends on
+ * the shape only; a partial sum past float32's range leaves an infinity or a NaN.  A NaN scale of X makes its
+ * row of T NaN, one of W its column.  The gradient G W^T is the same call on a quantised G and W not transposed.
+ * n >= 1; 1 <= F_in, F_out <= 65536 (else DUALGCN_ERR_UNSUPPORTED); X and W 16-byte aligned; T overlaps no
+ * operand.  No workspace.  Asynchronous.
+ */
+int dualgcn_update_mxfp4(const void *X, const void *sx, const void *W, const void *sw, void *T, int32_t n, int32_t F_in,
+                         int32_t F_out, uint32_t flags, void *stream);
 
 /* ------------------------------------------------------------------ measurement */
 

@@ -15,6 +15,12 @@ Between the blocks of a deep GCN, in training from a teacher, and in serving fro
     R, Z = norm_residual(R, B, gate=gate)       # R + gate * norm(B), and its norm
     G, loss = distill_xent(Y, ids, teacher)     # against the teacher's top logits, and dloss/dY
     T = update_fp8(*quantize_fp8(Z), *W8)       # T = Z W, e4m3 with a scale for each 128
+    T = update_mxfp4(*quantize_mxfp4(Z), *W4)   # T = Z W, e2m1 with a scale for each 32
+
+Over the graphs of a batch, and for all weights at once:
+
+    Y, stats = group_norm(X, ptr, groups=8, act="silu")    # and group_norm_backward
+    norm = clipped_sgd(weights, grads, lr, max_norm=1.0)   # W -= lr * clipped gradient
 """
 import collections
 import ctypes
@@ -31,8 +37,9 @@ FORCE_AUTO, FORCE_SPARSE, FORCE_DENSE = 0, 1, 2
 RELU, OUT_BF16, IN_BF16, GRAD_BF16 = 1, 2, 4, 8
 STREAM_BF16, NORM_LAYER, NORM_POST = 16, 32, 64
 GATE_FEATURE, GATE_NODE, GATE_FULL, GATE_SIGMOID = 128, 256, 512, 1024
-TEACHER_BF16 = 2048
+TEACHER_BF16, SILU, ZERO_REST = 2048, 4096, 8192
 FP8_BLOCK = 128                  # elements that share a scale in the 8-bit operands
+MX_BLOCK = 32                    # and in the 4-bit ones
 LOSS_SLOTS = 1025                # float64 entries of the loss buffer of softmax_xent
 ALPHA_ADAPTIVE = 0xFFFFFFFF      # alpha = (ALPHA_ADAPTIVE, q): adaptive weight in steps of 1/q
 ALPHA_BALANCED = 0xFFFFFFFE      # alpha = (ALPHA_BALANCED, q): weight balancing the spreads of N and D
@@ -87,6 +94,17 @@ class NormGradPointers(ctypes.Structure):
                 ("gate", ctypes.c_void_p)]
 
 
+class GroupNorm(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("eps", ctypes.c_double), ("graphs", ctypes.c_int32), ("F", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("count", ctypes.c_int64), ("flags", ctypes.c_uint32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python paper_2609_01983_amd/build.py`")
@@ -130,6 +148,20 @@ def _load():
         "dualgcn_quantize_fp8": ([P, I32, I32, U32, P, P, P], ctypes.c_int),
         "dualgcn_quantize_weight_fp8": ([P, I32, I32, I32, P, P, P], ctypes.c_int),
         "dualgcn_update_fp8": ([P, P, P, P, P, I32, I32, I32, U32, P], ctypes.c_int),
+        "dualgcn_group_norm_act_workspace": ([ctypes.POINTER(GroupNorm), I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "dualgcn_group_norm_act": ([ctypes.POINTER(GroupNorm), P, P, P, I32, P, SZ, P], ctypes.c_int),
+        "dualgcn_group_norm_act_backward_workspace": ([ctypes.POINTER(GroupNorm), I32, ctypes.POINTER(SZ)],
+                                                      ctypes.c_int),
+        "dualgcn_group_norm_act_backward": ([ctypes.POINTER(GroupNorm), P, P, P, P, P, P, I32, P, SZ, P], ctypes.c_int),
+        "dualgcn_grad_norm_workspace": ([I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "dualgcn_grad_norm": ([ctypes.POINTER(Grad), I32, P, P, SZ, P], ctypes.c_int),
+        "dualgcn_clip_grads": ([ctypes.POINTER(Grad), I32, ctypes.c_double, ctypes.c_double, P, P, SZ, P], ctypes.c_int),
+        "dualgcn_clipped_sgd": ([ctypes.POINTER(Grad), I32, ctypes.c_double, ctypes.c_double, ctypes.c_double, P, P, SZ,
+                                 P], ctypes.c_int),
+        "dualgcn_quantize_mxfp4": ([P, I32, I32, U32, P, P, P], ctypes.c_int),
+        "dualgcn_quantize_weight_mxfp4": ([P, I32, I32, I32, P, P, P], ctypes.c_int),
+        "dualgcn_dequantize_mxfp4": ([P, P, I32, I32, U32, P, P], ctypes.c_int),
+        "dualgcn_update_mxfp4": ([P, P, P, P, P, I32, I32, I32, U32, P], ctypes.c_int),
         "dualgcn_bandwidth_probe": ([I32, P, P, SZ, P], ctypes.c_int),
         "dualgcn_bandwidth_probe_out_floats": ([], I32),
     }
@@ -834,6 +866,279 @@ def update_fp8(X, sx, W, sw, T=None, out_bf16=False, stream=None):
     return T
 
 
+# ------------------------------------------------------------------ batches of graphs
+
+_ACTS = {None: 0, "relu": RELU, "silu": SILU}
+
+
+def _group(X, ptr, groups, weight, bias, act, eps):
+    """The checked parameters of a group norm, as the library takes them."""
+    flags = IN_BF16 if _rows(X, "X") else 0
+    if act not in _ACTS:
+        raise ValueError('act must be None, "relu" or "silu"')
+    F = X.shape[1]
+    if groups < 1 or F % groups:
+        raise ValueError(f"groups must divide the {F} features, got {groups}")
+    width = (F,)
+    if weight is not None:
+        _shaped(weight, torch.float32, width, "weight")
+    if bias is not None:
+        _shaped(bias, torch.float32, width, "bias")
+    graphs = 1
+    if ptr is not None:
+        if not isinstance(ptr, torch.Tensor) or ptr.dim() != 1 or ptr.numel() < 2:
+            raise ValueError("ptr must be an int32 tensor of one offset more than there are graphs")
+        graphs = ptr.numel() - 1
+        if graphs > 0x7FFFFFFF:
+            raise ValueError("more than 2^31 - 1 graphs")
+        _shaped(ptr, torch.int32, (graphs + 1,), "ptr")
+    return GroupNorm(_ptr(ptr), _ptr(weight), _ptr(bias), eps, graphs, F, groups, flags | _ACTS[act])
+
+
+def _workspace(query, what, p, n, like, workspace, stream):
+    if workspace is not None:
+        return _dev(workspace, torch.uint8, "workspace")
+    nbytes = ctypes.c_size_t()
+    _check(query(p, n, ctypes.byref(nbytes)), what)
+    return _empty((nbytes.value,), torch.uint8, like, stream)
+
+
+def group_norm_workspace_bytes(n, F, groups, graphs=1, backward=False):
+    """Bytes of the workspace of group_norm (or of its backward pass) for n rows of F features in `graphs` graphs."""
+    p = GroupNorm(1 << 30, None, None, 1e-5, graphs, F, groups, 0)
+    nbytes = ctypes.c_size_t()
+    name = "dualgcn_group_norm_act_backward_workspace" if backward else "dualgcn_group_norm_act_workspace"
+    _check(getattr(_lib, name)(p, n, ctypes.byref(nbytes)), name)
+    return nbytes.value
+
+
+def group_norm(X, ptr=None, *, groups, weight=None, bias=None, act=None, eps=1e-5, out_bf16=False, Y=None, stats=None,
+               workspace=None, stream=None):
+    """(Y, stats): a group norm with an activation over the nodes of each graph of a batch.
+
+    X: [n, F] float32 or bfloat16, a row for each node; ptr: int32 [graphs + 1] on the device, graph b has the rows
+    ptr[b] .. ptr[b + 1] - 1 (None: all rows are one graph).  The mean and variance go over a graph's nodes and the F / groups
+    features of a group; weight and bias: float32 [F] or None; act: None, "relu" or "silu".  Y is [n, F]
+    float32, or bfloat16 with out_bf16; it may be X (in place) if the types are the same.  Rows of no graph (padding) are 0 in
+    a Y made here, and left as they were in one that is given.  stats: float64 [graphs, groups, 2], the mean and
+    1 / sqrt(variance + eps), which group_norm_backward takes."""
+    p = _group(X, ptr, groups, weight, bias, act, eps)
+    n, F = shape = X.shape
+    s = _queue(stream, X, ptr, weight, bias, Y, stats, workspace)
+    ydt = torch.float32
+    if out_bf16:
+        ydt = torch.bfloat16
+        p.flags |= OUT_BF16
+    if Y is None:
+        Y = _empty(shape, ydt, X, stream)
+        p.flags |= ZERO_REST
+    else:
+        _shaped(Y, ydt, shape, "Y")
+    if stats is None:
+        stats = _empty((p.graphs, groups, 2), torch.float64, X, stream)
+    else:
+        _shaped(stats, torch.float64, (p.graphs, groups, 2), "stats")
+    workspace = _workspace(_lib.dualgcn_group_norm_act_workspace, "dualgcn_group_norm_act_workspace", p, n, X, workspace,
+                           stream)
+    _check(_lib.dualgcn_group_norm_act(p, X.data_ptr(), Y.data_ptr(), stats.data_ptr(), n, workspace.data_ptr(),
+                                       workspace.numel(), s), "dualgcn_group_norm_act")
+    return Y, stats
+
+
+class GroupNormGrads(collections.namedtuple("GroupNormGrads", "X weight bias")):
+    """Gradients of group_norm's operands; None where there is no such operand."""
+    __slots__ = ()
+
+
+def group_norm_backward(X, dY, stats, ptr=None, *, groups, weight=None, bias=None, act=None, dX=None, workspace=None,
+                        stream=None):
+    """GroupNormGrads of group_norm: X, ptr and the parameters are its own, stats what it returned, dY ([n, F] float32
+    or bfloat16) the gradient of Y.  The gradient of X is in dY's type (dX may be dY; rows of no graph as for Y), those of
+    the vectors float32 [F], None for a vector that is None."""
+    p = _group(X, ptr, groups, weight, bias, act, 1e-5)
+    n, F = shape = X.shape
+    if _rows(dY, "dY"):
+        p.flags |= GRAD_BF16
+    _shaped(dY, dY.dtype, shape, "dY")
+    _shaped(stats, torch.float64, (p.graphs, groups, 2), "stats")
+    s = _queue(stream, X, dY, stats, ptr, weight, bias, dX, workspace)
+    if dX is None:
+        dX = _empty(shape, dY.dtype, X, stream)
+        p.flags |= ZERO_REST
+    else:
+        _shaped(dX, dY.dtype, shape, "dX")
+    dw = None if weight is None else _empty((F,), torch.float32, X, stream)
+    db = None if bias is None else _empty((F,), torch.float32, X, stream)
+    workspace = _workspace(_lib.dualgcn_group_norm_act_backward_workspace, "dualgcn_group_norm_act_backward_workspace", p,
+                           n, X, workspace, stream)
+    _check(_lib.dualgcn_group_norm_act_backward(p, X.data_ptr(), dY.data_ptr(), stats.data_ptr(), dX.data_ptr(), _ptr(dw),
+                                                _ptr(db), n, workspace.data_ptr(), workspace.numel(), s),
+           "dualgcn_group_norm_act_backward")
+    return GroupNormGrads(dX, dw, db)
+
+
+# ------------------------------------------------------------------ clipped gradients
+
+def grad_norm_workspace_bytes(tensors):
+    nbytes = ctypes.c_size_t()
+    _check(_lib.dualgcn_grad_norm_workspace(tensors, ctypes.byref(nbytes)), "dualgcn_grad_norm_workspace")
+    return nbytes.value
+
+
+def _flat(t, name):
+    """A float32 or bfloat16 tensor of any shape: is it bfloat16?"""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and
+            (t.dtype is torch.float32 or t.dtype is torch.bfloat16)):
+        _float_or_bf16(t, name)
+    return t.dtype is torch.bfloat16
+
+
+def _grads(grads, weights, out, norm, workspace, stream):
+    """The list of a call on many gradients as the library takes it, and what the call needs beside it."""
+    if not grads:
+        raise ValueError("no gradients")
+    rows = (Grad * len(grads))()
+    for i, g in enumerate(grads):
+        rows[i].flags = GRAD_BF16 if _flat(g, "a gradient") else 0
+        rows[i].grad, rows[i].count = g.data_ptr(), g.numel()
+    s = _queue(stream, *grads, *(weights or ()), *(out or ()), norm, workspace)
+    if weights is not None:
+        if len(weights) != len(grads):
+            raise ValueError("as many weights as gradients")
+        for i, (w, g) in enumerate(zip(weights, grads)):
+            rows[i].weight = _shaped(w, torch.float32, g.shape, "a weight").data_ptr()
+    if out is not None:
+        if len(out) != len(grads):
+            raise ValueError("as many outputs as gradients")
+        for i, (o, g) in enumerate(zip(out, grads)):
+            rows[i].out = _shaped(o, g.dtype if weights is None else torch.float32, g.shape, "an output").data_ptr()
+    norm = _empty((1,), torch.float32, grads[0], stream) if norm is None else _shaped(norm, torch.float32, (1,), "norm")
+    if workspace is None:
+        workspace = _empty((grad_norm_workspace_bytes(len(grads)),), torch.uint8, grads[0], stream)
+    else:
+        _dev(workspace, torch.uint8, "workspace")
+    return rows, norm, workspace, s
+
+
+def grad_norm(grads, norm=None, workspace=None, stream=None):
+    """The norm of all gradients together (a list of float32 and bfloat16 tensors of any shapes), float32 [1]."""
+    rows, norm, workspace, s = _grads(grads, None, None, norm, workspace, stream)
+    _check(_lib.dualgcn_grad_norm(rows, len(rows), norm.data_ptr(), workspace.data_ptr(), workspace.numel(), s),
+           "dualgcn_grad_norm")
+    return norm
+
+
+def clip_grads(grads, max_norm, out=None, eps=1e-6, norm=None, workspace=None, stream=None):
+    """(out, norm): the gradients scaled by min(1, max_norm / (norm + eps)), norm that of all of them together (float32
+    [1], on the device: nothing is waited for).  out: tensors like the gradients; None or `grads` itself: in place."""
+    if out is None:
+        out = grads
+    rows, norm, workspace, s = _grads(grads, None, out, norm, workspace, stream)
+    _check(_lib.dualgcn_clip_grads(rows, len(rows), max_norm, eps, norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                   s), "dualgcn_clip_grads")
+    return out, norm
+
+
+def clipped_sgd(weights, grads, lr, max_norm, out=None, eps=1e-6, norm=None, workspace=None, stream=None):
+    """(out, norm): weights - lr * clipped gradients (as clip_grads has them), float32; the gradients stay as they are.
+    out: tensors like the weights; None or `weights` itself: in place."""
+    if out is None:
+        out = weights
+    rows, norm, workspace, s = _grads(grads, weights, out, norm, workspace, stream)
+    _check(_lib.dualgcn_clipped_sgd(rows, len(rows), max_norm, eps, lr, norm.data_ptr(), workspace.data_ptr(),
+                                    workspace.numel(), s), "dualgcn_clipped_sgd")
+    return out, norm
+
+
+# ------------------------------------------------------------------ 4-bit operands
+
+def _mx_blocks(F):
+    return (F + MX_BLOCK - 1) // MX_BLOCK
+
+
+def _mx_out(like, n, F, Q, scales, stream):
+    b = _mx_blocks(F)
+    Q = _empty((n, 16 * b), torch.uint8, like, stream) if Q is None else _shaped(Q, torch.uint8, (n, 16 * b), "Q")
+    if scales is None:
+        return Q, _empty((n, b), torch.uint8, like, stream)
+    return Q, _shaped(scales, torch.uint8, (n, b), "scales")
+
+
+def _mx(Q, scales, name, its):
+    """A matrix in 4 bits: its rows and blocks."""
+    if not isinstance(Q, torch.Tensor) or Q.dim() != 2 or Q.shape[1] % 16:
+        raise ValueError(f"{name} must be a uint8 tensor [rows, 16 * blocks]")
+    n, b = Q.shape[0], Q.shape[1] // 16
+    if n > 0x7FFFFFFF or 32 * b > 0x7FFFFFFF:
+        raise ValueError(f"{name} has more than 2^31 - 1 rows or columns")
+    _shaped(Q, torch.uint8, (n, 16 * b), name)
+    _shaped(scales, torch.uint8, (n, b), its)
+    return n, b
+
+
+def quantize_mxfp4(X, Q=None, scales=None, stream=None):
+    """(Q, scales): X ([n, F] float32 or bfloat16) in 4 bits (e2m1, two a byte, the first in the lower four bits) as uint8
+    [n, 16 * ceil(F / 32)], with a scale 2^(s - 127) for each 32 consecutive features of a row, uint8
+    [n, ceil(F / 32)] (255: NaN)."""
+    flags = IN_BF16 if _rows(X, "X") else 0
+    n, F = X.shape
+    s = _queue(stream, X, Q, scales)
+    Q, scales = _mx_out(X, n, F, Q, scales, stream)
+    _check(_lib.dualgcn_quantize_mxfp4(X.data_ptr(), n, F, flags, Q.data_ptr(), scales.data_ptr(), s),
+           "dualgcn_quantize_mxfp4")
+    return Q, scales
+
+
+def quantize_weight_mxfp4(W, transpose=True, Q=None, scales=None, stream=None):
+    """(Q, scales): W ([F_in, F_out] float32) in 4 bits as update_mxfp4 reads it: F_out rows of F_in elements for X W, or
+    with transpose=False F_in rows of F_out elements for the gradient's product G W^T (its blocks run along
+    F_out: other numbers than the transposed form's)."""
+    _dev(W, torch.float32, "W")
+    if W.dim() != 2:
+        raise ValueError("W must be [F_in, F_out]")
+    F_in, F_out = W.shape
+    if max(F_in, F_out) > 0x7FFFFFFF:
+        raise ValueError("more than 2^31 - 1 rows or columns")
+    s = _queue(stream, W, Q, scales)
+    rows, F = (F_out, F_in) if transpose else (F_in, F_out)
+    Q, scales = _mx_out(W, rows, F, Q, scales, stream)
+    _check(_lib.dualgcn_quantize_weight_mxfp4(W.data_ptr(), F_in, F_out, 1 if transpose else 0, Q.data_ptr(),
+                                              scales.data_ptr(), s), "dualgcn_quantize_weight_mxfp4")
+    return Q, scales
+
+
+def dequantize_mxfp4(Q, scales, F=None, X=None, out_bf16=False, stream=None):
+    """The values of quantize_mxfp4's (Q, scales) as float32 [n, F], or bfloat16 with out_bf16 (both hold every one).
+    F: the features of a row, where the last block is not full."""
+    n, b = _mx(Q, scales, "Q", "scales")
+    if F is None:
+        F = 32 * b
+    if _mx_blocks(F) != b or F < 1:
+        raise ValueError(f"rows of {F} elements have {_mx_blocks(F)} blocks, not {b}")
+    s = _queue(stream, Q, scales, X)
+    xdt = torch.bfloat16 if out_bf16 else torch.float32
+    X = _empty((n, F), xdt, Q, stream) if X is None else _shaped(X, xdt, (n, F), "X")
+    _check(_lib.dualgcn_dequantize_mxfp4(Q.data_ptr(), scales.data_ptr(), n, F, OUT_BF16 if out_bf16 else 0, X.data_ptr(),
+                                         s), "dualgcn_dequantize_mxfp4")
+    return X
+
+
+def update_mxfp4(X, sx, W, sw, T=None, out_bf16=False, stream=None):
+    """T = X W from 4-bit operands on the matrix cores, both as quantize_mxfp4 and quantize_weight_mxfp4 make them: X uint8
+    [n, 16 * blocks] with its scales sx [n, blocks], W uint8 [F_out, 16 * blocks] (transposed) with sw [F_out, blocks].
+    T is float32 [n, F_out], or bfloat16 with out_bf16."""
+    n, b = _mx(X, sx, "X", "sx")
+    F_out, wb = _mx(W, sw, "W", "sw")
+    if wb != b:
+        raise ValueError(f"X has {b} blocks a row, W {wb}")
+    s = _queue(stream, X, sx, W, sw, T)
+    tdt = torch.bfloat16 if out_bf16 else torch.float32
+    T = _empty((n, F_out), tdt, X, stream) if T is None else _shaped(T, tdt, (n, F_out), "T")
+    _check(_lib.dualgcn_update_mxfp4(X.data_ptr(), sx.data_ptr(), W.data_ptr(), sw.data_ptr(), T.data_ptr(), n, 32 * b,
+                                     F_out, OUT_BF16 if out_bf16 else 0, s), "dualgcn_update_mxfp4")
+    return T
+
+
 PROBE_COPY, PROBE_READ = 0, 1
 
 
@@ -873,4 +1178,7 @@ __all__ = ["Plan", "spmm", "spmm_update", "update", "gcn_layer", "gcn_layer_work
            "norm_residual_backward_workspace_bytes", "Norm", "NormGradPointers", "STREAM_BF16", "NORM_LAYER",
            "NORM_POST", "GATE_FEATURE", "GATE_NODE", "GATE_FULL", "GATE_SIGMOID",
            "distill_xent", "distill_workspace_bytes", "TEACHER_BF16",
-           "quantize_fp8", "quantize_weight_fp8", "update_fp8", "FP8_BLOCK"]
+           "quantize_fp8", "quantize_weight_fp8", "update_fp8", "FP8_BLOCK",
+           "group_norm", "group_norm_backward", "GroupNormGrads", "group_norm_workspace_bytes", "GroupNorm", "SILU",
+           "ZERO_REST", "grad_norm", "clip_grads", "clipped_sgd", "grad_norm_workspace_bytes", "Grad",
+           "quantize_mxfp4", "quantize_weight_mxfp4", "dequantize_mxfp4", "update_mxfp4", "MX_BLOCK"]

@@ -1,5 +1,6 @@
 // C ABI of libdualgcn: argument checks, status codes and dispatch to the kernels.
 // Every check that needs no device runs before the device is touched.
+#include <algorithm>
 #include <atomic>
 #include <cstdlib>
 #include <cstring>
@@ -311,6 +312,81 @@ int check_norm(const dualgcn_norm *p, const void *B, int32_t n, int32_t F, uint3
     if (F > dgc::kMaxNormWidth) return DUALGCN_ERR_UNSUPPORTED;
     return DUALGCN_OK;
 }
+
+// A group norm's parameters; `more` are the flags a call takes beside its own.
+constexpr int32_t kMostGroupRows = 0x7FFFFFFF - (1 << 22) + 1;
+int check_group(const dualgcn_group_norm *p, int32_t n, uint32_t more) {
+    if (!p || n < 1 || p->F < 1 || p->groups < 1 || p->F % p->groups || (p->ptr && p->graphs < 1)) return DUALGCN_ERR_INVALID_ARG;
+    const uint32_t act = DUALGCN_RELU | DUALGCN_SILU;
+    if (p->flags & ~(act | DUALGCN_IN_BF16 | DUALGCN_ZERO_REST | more) || (p->flags & act) == act) return DUALGCN_ERR_INVALID_ARG;
+    if (!(p->eps >= 0x1p-126) || !(p->eps < 0x1p127)) return DUALGCN_ERR_INVALID_ARG;
+    if (!elem_aligned(p->ptr, false) || !elem_aligned(p->weight, false) || !elem_aligned(p->bias, false)) return DUALGCN_ERR_INVALID_ARG;
+    if (p->F > dgc::kMaxNormWidth || n > kMostGroupRows || (p->ptr && p->graphs > (1 << 30))) return DUALGCN_ERR_UNSUPPORTED;
+    return DUALGCN_OK;
+}
+size_t group_stats_bytes(const dualgcn_group_norm &p) { return 2 * sizeof(double) * (p.ptr ? static_cast<size_t>(p.graphs) : 1) * p.groups; }
+size_t group_ptr_bytes(const dualgcn_group_norm &p) { return p.ptr ? sizeof(int32_t) * (static_cast<size_t>(p.graphs) + 1) : 0; }
+
+// The tensors of a call on many gradients: `kind` 0 has the norm alone, 1 scales them, 2 steps the weights.
+int check_grads(const dualgcn_grad *g, int32_t tensors, int kind, const float *norm, const void *workspace, size_t workspace_bytes) {
+    if (!g || tensors < 1 || !norm || !workspace || !elem_aligned(norm, false)) return DUALGCN_ERR_INVALID_ARG;
+    if (tensors > (1 << 20)) return DUALGCN_ERR_UNSUPPORTED;
+    const size_t ws = dgc::clip_workspace_bytes(tensors);
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < ws) return DUALGCN_ERR_INVALID_ARG;
+    struct Range {
+        uintptr_t from, to;
+        bool out;
+    };
+    try {
+        std::vector<Range> all;
+        all.reserve(3 * static_cast<size_t>(tensors) + 2);
+        auto add = [&](const void *p, size_t bytes, bool out) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            if (bytes) all.push_back({at, at + bytes, out});
+        };
+        add(norm, sizeof(float), true);
+        add(workspace, ws, true);
+        for (int32_t i = 0; i < tensors; ++i) {
+            if (g[i].count < 0 || (g[i].flags & ~DUALGCN_GRAD_BF16)) return DUALGCN_ERR_INVALID_ARG;
+            if (g[i].count > (int64_t{1} << 40)) return DUALGCN_ERR_UNSUPPORTED;
+            if ((!kind && g[i].out) || (kind != 2 && g[i].weight)) return DUALGCN_ERR_INVALID_ARG;
+            if (g[i].count && (!g[i].grad || (kind && !g[i].out) || (kind == 2 && !g[i].weight))) return DUALGCN_ERR_INVALID_ARG;
+            const bool bf = g[i].flags & DUALGCN_GRAD_BF16;
+            if (!elem_aligned(g[i].grad, bf) || !elem_aligned(g[i].weight, false) ||
+                !elem_aligned(g[i].out, bf && kind == 1))
+                return DUALGCN_ERR_INVALID_ARG;
+            const size_t gb = static_cast<size_t>(g[i].count) * (bf ? 2 : 4), wb = static_cast<size_t>(g[i].count) * 4;
+            if (!(kind == 1 && g[i].out == g[i].grad)) add(g[i].grad, gb, false);
+            if (kind == 2 && g[i].out != g[i].weight) add(g[i].weight, wb, false);
+            if (kind) add(g[i].out, kind == 1 ? gb : wb, true);
+        }
+        // in order of their starts, an output begins behind every end so far and an operand behind the outputs'
+        std::sort(all.begin(), all.end(), [](const Range &a, const Range &b) { return a.from < b.from; });
+        uintptr_t any = 0, out = 0;
+        for (const Range &r : all) {
+            if (r.from < (r.out ? any : out)) return DUALGCN_ERR_INVALID_ARG;
+            any = std::max(any, r.to);
+            if (r.out) out = std::max(out, r.to);
+        }
+    } catch (...) {
+        return DUALGCN_ERR_OOM;
+    }
+    return DUALGCN_OK;
+}
+
+int clip(const dualgcn_grad *g, int32_t tensors, int kind, double max_norm, double eps, double lr, float *norm, void *workspace,
+         size_t workspace_bytes, void *stream) {
+    int st = check_grads(g, tensors, kind, norm, workspace, workspace_bytes);
+    if (st) return st;
+    if (!(max_norm >= 0.0) || !(eps >= 0.0) || eps - eps != 0.0 || lr - lr != 0.0) return DUALGCN_ERR_INVALID_ARG;
+    if ((st = dgc::device_status())) return st;
+    return dgc::launch_clip(g, tensors, kind != 0, max_norm, eps, lr, norm, workspace, static_cast<hipStream_t>(stream));
+}
+
+// Sizes of the 4-bit form of n rows of F elements.
+size_t mx_blocks(int32_t n, int32_t F) { return static_cast<size_t>(n) * ((static_cast<size_t>(F) + DUALGCN_MX_BLOCK - 1) / DUALGCN_MX_BLOCK); }
+constexpr size_t kMxBytes = DUALGCN_MX_BLOCK / 2;
+constexpr size_t kMostMxBlocks = (size_t{1} << 32) - 256;
 
 }  // namespace
 
@@ -714,6 +790,152 @@ int dualgcn_update_fp8(const void *X, const float *sx, const void *W, const floa
     const int st = dgc::device_status();
     if (st) return st;
     return dgc::launch_update_fp8(X, sx, W, sw, T, bf, n, F_in, F_out, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_group_norm_act_workspace(const dualgcn_group_norm *norm, int32_t n, size_t *bytes) {
+    const int st = check_group(norm, n, DUALGCN_OUT_BF16 | DUALGCN_GRAD_BF16);
+    if (st) return st;
+    if (!bytes) return DUALGCN_ERR_INVALID_ARG;
+    *bytes = dgc::group_norm_workspace_bytes(*norm, n);
+    return DUALGCN_OK;
+}
+
+int dualgcn_group_norm_act(const dualgcn_group_norm *norm, const void *X, void *Y, double *stats, int32_t n, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    dgc::TraceRange trace("dualgcn_group_norm_act");
+    int st = check_group(norm, n, DUALGCN_OUT_BF16);
+    if (st) return st;
+    const bool xbf = norm->flags & DUALGCN_IN_BF16, ybf = norm->flags & DUALGCN_OUT_BF16;
+    if (!X || !Y || !stats || !workspace || !elem_aligned(X, xbf) || !elem_aligned(Y, ybf) ||
+        reinterpret_cast<uintptr_t>(stats) % 16 || reinterpret_cast<uintptr_t>(workspace) % 256)
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t ws = dgc::group_norm_workspace_bytes(*norm, n), elems = static_cast<size_t>(n) * norm->F, vb = vector_bytes(norm->F);
+    if (workspace_bytes < ws) return DUALGCN_ERR_INVALID_ARG;
+    const Span in[] = {{X, elems * (xbf ? 2 : 4)}, {norm->ptr, group_ptr_bytes(*norm)}, {norm->weight, vb}, {norm->bias, vb}};
+    const Span out[] = {{Y, elems * (ybf ? 2 : 4), xbf == ybf ? 0 : -1}, {stats, group_stats_bytes(*norm)}, {workspace, ws}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    if ((st = dgc::device_status())) return st;
+    return dgc::launch_group_norm(*norm, X, Y, stats, n, workspace, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_group_norm_act_backward_workspace(const dualgcn_group_norm *norm, int32_t n, size_t *bytes) {
+    const int st = check_group(norm, n, DUALGCN_OUT_BF16 | DUALGCN_GRAD_BF16);
+    if (st) return st;
+    if (!bytes) return DUALGCN_ERR_INVALID_ARG;
+    *bytes = dgc::group_norm_backward_workspace_bytes(*norm, n);
+    return DUALGCN_OK;
+}
+
+int dualgcn_group_norm_act_backward(const dualgcn_group_norm *norm, const void *X, const void *dY, const double *stats, void *dX,
+                                    float *dweight, float *dbias, int32_t n, void *workspace, size_t workspace_bytes,
+                                    void *stream) {
+    dgc::TraceRange trace("dualgcn_group_norm_act_backward");
+    int st = check_group(norm, n, DUALGCN_OUT_BF16 | DUALGCN_GRAD_BF16);
+    if (st) return st;
+    const bool xbf = norm->flags & DUALGCN_IN_BF16, gbf = norm->flags & DUALGCN_GRAD_BF16;
+    if (!X || !dY || !stats || !workspace || !elem_aligned(X, xbf) || !elem_aligned(dY, gbf) || !elem_aligned(dX, gbf) ||
+        !elem_aligned(dweight, false) || !elem_aligned(dbias, false) || reinterpret_cast<uintptr_t>(stats) % 16 ||
+        reinterpret_cast<uintptr_t>(workspace) % 256)
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t ws = dgc::group_norm_backward_workspace_bytes(*norm, n), elems = static_cast<size_t>(n) * norm->F;
+    if (workspace_bytes < ws) return DUALGCN_ERR_INVALID_ARG;
+    const size_t vb = vector_bytes(norm->F), gb = elems * (gbf ? 2 : 4);
+    const Span in[] = {{dY, gb}, {X, elems * (xbf ? 2 : 4)}, {stats, group_stats_bytes(*norm)}, {norm->ptr, group_ptr_bytes(*norm)},
+                       {norm->weight, vb}, {norm->bias, vb}};
+    const Span out[] = {{dX, gb, 0}, {dweight, vb}, {dbias, vb}, {workspace, ws}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    if ((st = dgc::device_status())) return st;
+    return dgc::launch_group_norm_backward(*norm, X, dY, stats, dX, dweight, dbias, n, workspace, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_grad_norm_workspace(int32_t tensors, size_t *bytes) {
+    if (!bytes || tensors < 1) return DUALGCN_ERR_INVALID_ARG;
+    if (tensors > (1 << 20)) return DUALGCN_ERR_UNSUPPORTED;
+    *bytes = dgc::clip_workspace_bytes(tensors);
+    return DUALGCN_OK;
+}
+
+int dualgcn_grad_norm(const dualgcn_grad *grads_h, int32_t tensors, float *norm, void *workspace, size_t workspace_bytes,
+                      void *stream) {
+    dgc::TraceRange trace("dualgcn_grad_norm");
+    return clip(grads_h, tensors, 0, 0.0, 0.0, 0.0, norm, workspace, workspace_bytes, stream);
+}
+
+int dualgcn_clip_grads(const dualgcn_grad *grads_h, int32_t tensors, double max_norm, double eps, float *norm, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+    dgc::TraceRange trace("dualgcn_clip_grads");
+    return clip(grads_h, tensors, 1, max_norm, eps, 0.0, norm, workspace, workspace_bytes, stream);
+}
+
+int dualgcn_clipped_sgd(const dualgcn_grad *grads_h, int32_t tensors, double max_norm, double eps, double lr, float *norm,
+                        void *workspace, size_t workspace_bytes, void *stream) {
+    dgc::TraceRange trace("dualgcn_clipped_sgd");
+    return clip(grads_h, tensors, 2, max_norm, eps, lr, norm, workspace, workspace_bytes, stream);
+}
+
+int dualgcn_quantize_mxfp4(const void *X, int32_t n, int32_t F, uint32_t flags, void *Q, void *scales, void *stream) {
+    dgc::TraceRange trace("dualgcn_quantize_mxfp4");
+    if (!X || !Q || !scales || n < 1 || F < 1 || (flags & ~DUALGCN_IN_BF16)) return DUALGCN_ERR_INVALID_ARG;
+    const bool bf = flags & DUALGCN_IN_BF16;
+    const size_t blocks = mx_blocks(n, F);
+    if (F >= (1 << 20) || blocks >= kMostMxBlocks) return DUALGCN_ERR_UNSUPPORTED;
+    if (!elem_aligned(X, bf) || reinterpret_cast<uintptr_t>(Q) % 16) return DUALGCN_ERR_INVALID_ARG;
+    const Span in[] = {{X, static_cast<size_t>(n) * F * (bf ? 2 : 4)}};
+    const Span out[] = {{Q, blocks * kMxBytes}, {scales, blocks}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    return dgc::launch_quantize_mxfp4(X, bf, n, F, Q, scales, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_quantize_weight_mxfp4(const float *W, int32_t F_in, int32_t F_out, int32_t transpose, void *Q, void *scales,
+                                  void *stream) {
+    dgc::TraceRange trace("dualgcn_quantize_weight_mxfp4");
+    if (!W || !Q || !scales || F_in < 1 || F_out < 1) return DUALGCN_ERR_INVALID_ARG;
+    if (F_in > (1 << 16) || F_out > (1 << 16)) return DUALGCN_ERR_UNSUPPORTED;
+    if (!elem_aligned(W, false) || reinterpret_cast<uintptr_t>(Q) % 16) return DUALGCN_ERR_INVALID_ARG;
+    const size_t blocks = transpose ? mx_blocks(F_out, F_in) : mx_blocks(F_in, F_out);
+    const Span in[] = {{W, static_cast<size_t>(F_in) * F_out * sizeof(float)}};
+    const Span out[] = {{Q, blocks * kMxBytes}, {scales, blocks}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return transpose ? dgc::launch_quantize_weight_mxfp4(W, F_in, F_out, Q, scales, s)
+                     : dgc::launch_quantize_mxfp4(W, false, F_in, F_out, Q, scales, s);
+}
+
+int dualgcn_dequantize_mxfp4(const void *Q, const void *scales, int32_t n, int32_t F, uint32_t flags, void *X, void *stream) {
+    dgc::TraceRange trace("dualgcn_dequantize_mxfp4");
+    if (!X || !Q || !scales || n < 1 || F < 1 || (flags & ~DUALGCN_OUT_BF16)) return DUALGCN_ERR_INVALID_ARG;
+    const bool bf = flags & DUALGCN_OUT_BF16;
+    const size_t blocks = mx_blocks(n, F);
+    if (F >= (1 << 20) || blocks >= kMostMxBlocks) return DUALGCN_ERR_UNSUPPORTED;
+    if (!elem_aligned(X, bf) || reinterpret_cast<uintptr_t>(Q) % 16) return DUALGCN_ERR_INVALID_ARG;
+    const Span in[] = {{Q, blocks * kMxBytes}, {scales, blocks}};
+    const Span out[] = {{X, static_cast<size_t>(n) * F * (bf ? 2 : 4)}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    return dgc::launch_dequantize_mxfp4(Q, scales, n, F, X, bf, static_cast<hipStream_t>(stream));
+}
+
+int dualgcn_update_mxfp4(const void *X, const void *sx, const void *W, const void *sw, void *T, int32_t n, int32_t F_in,
+                         int32_t F_out, uint32_t flags, void *stream) {
+    dgc::TraceRange trace("dualgcn_update_mxfp4");
+    if (!X || !sx || !W || !sw || !T || n < 1 || F_in < 1 || F_out < 1 || (flags & ~DUALGCN_OUT_BF16))
+        return DUALGCN_ERR_INVALID_ARG;
+    if (F_in > (1 << 16) || F_out > (1 << 16)) return DUALGCN_ERR_UNSUPPORTED;
+    const bool bf = flags & DUALGCN_OUT_BF16;
+    if (reinterpret_cast<uintptr_t>(X) % 16 || reinterpret_cast<uintptr_t>(W) % 16 || !elem_aligned(T, bf))
+        return DUALGCN_ERR_INVALID_ARG;
+    const size_t xb = mx_blocks(n, F_in), wb = mx_blocks(F_out, F_in);
+    const Span in[] = {{X, xb * kMxBytes}, {sx, xb}, {W, wb * kMxBytes}, {sw, wb}};
+    const Span out[] = {{T, static_cast<size_t>(n) * F_out * (bf ? 2 : 4)}};
+    if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;
+    const int st = dgc::device_status();
+    if (st) return st;
+    return dgc::launch_update_mxfp4(X, sx, W, sw, T, bf, n, F_in, F_out, static_cast<hipStream_t>(stream));
 }
 
 int dualgcn_plan_query(const dualgcn_plan *plan, dualgcn_plan_info *out) {

@@ -29,4 +29,25 @@ int launch_quantize_weight(const float *W, int32_t rows, int32_t cols, bool tran
 int launch_update_fp8(const void *X, const float *sx, const void *W, const float *sw, void *T, bool out_bf16,
                       int32_t n, int32_t F_in, int32_t F_out, hipStream_t stream);
 
+// ---- group norms over the graphs of a batch (group.hip): arguments as the entry points take them, checked
+size_t group_norm_workspace_bytes(const dualgcn_group_norm &p, int32_t n);
+size_t group_norm_backward_workspace_bytes(const dualgcn_group_norm &p, int32_t n);
+int launch_group_norm(const dualgcn_group_norm &p, const void *X, void *Y, double *stats, int32_t n, void *workspace,
+                      hipStream_t stream);
+int launch_group_norm_backward(const dualgcn_group_norm &p, const void *X, const void *dY, const double *stats, void *dX,
+                               float *dweight, float *dbias, int32_t n, void *workspace, hipStream_t stream);
+
+// ---- the gradients' norm, clipping, the clipped step (clip.hip): arguments checked; without `apply` the norm alone
+constexpr int kClipPartials = 2048;                  // of a launch over up to a table's tensors
+size_t clip_workspace_bytes(int32_t tensors);
+int launch_clip(const dualgcn_grad *grads, int32_t tensors, bool apply, double max_norm, double eps, double lr, float *norm,
+                void *workspace, hipStream_t stream);
+
+// ---- the update phase in 4 bits (mxfp4.hip): arguments as the entry points take them, checked
+int launch_quantize_mxfp4(const void *X, bool bf16, int32_t n, int32_t F, void *Q, void *scales, hipStream_t stream);
+int launch_quantize_weight_mxfp4(const float *W, int32_t rows, int32_t cols, void *Q, void *scales, hipStream_t stream);
+int launch_dequantize_mxfp4(const void *Q, const void *scales, int32_t n, int32_t F, void *X, bool bf16, hipStream_t stream);
+int launch_update_mxfp4(const void *X, const void *sx, const void *W, const void *sw, void *T, bool out_bf16, int32_t n,
+                        int32_t F_in, int32_t F_out, hipStream_t stream);
+
 }  // namespace dgc

@@ -1,4 +1,4 @@
-// Device helpers of the row-wise operators (norm.hip, distill.hip, fp8.hip): four
+// Device helpers of the row-wise operators (norm.hip, distill.hip, fp8.hip, group.hip, clip.hip, mxfp4.hip): four
 // consecutive elements of a float32 or bfloat16 row at any alignment, and sums and maxima
 // over the 2^k lanes that share a row.
 #pragma once

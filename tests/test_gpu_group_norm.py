@@ -1,0 +1,336 @@
+"""Group norms with an activation over the graphs of a batch on the GPU, against float64 (bounds: groupref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import groupref
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module")
+def dg(device):
+    import paper_2609_01983_amd as dg
+    return dg
+
+
+def host(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def near(got, want, bound, what):
+    g = host(got)
+    bound = bound + (groupref.BF16 * (np.abs(want) + bound) if got.dtype == torch.bfloat16 else groupref.U * np.abs(want)) + 1e-44
+    bad = ~(np.abs(g - want) <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} outside, first at {np.argwhere(bad)[0]}: {g[bad][:3]} for {want[bad][:3]}"
+
+
+def offsets(rng, n, B, first=0, last=None):
+    """B graphs of random sizes in the rows [first, last); several without rows where B is large."""
+    last = n if last is None else last
+    return np.concatenate([[first], np.sort(rng.integers(first, last + 1, B - 1)), [last]]).astype(np.int32)
+
+
+def case(device, n, F, ptr, vectors=True, bf16=False, shift=0.5, seed=0):
+    rng = np.random.default_rng(seed + n + F)
+    X = torch.from_numpy((rng.standard_normal((n, F)) * np.exp(0.5 * rng.standard_normal(F)) + shift * rng.standard_normal(F)).astype(np.float32))
+    X = (X.to(torch.bfloat16) if bf16 else X).to(device)
+    w = torch.from_numpy((1 + 0.3 * rng.standard_normal(F)).astype(np.float32)).to(device) if vectors else None
+    b = torch.from_numpy((0.3 * rng.standard_normal(F)).astype(np.float32)).to(device) if vectors else None
+    dY = torch.from_numpy(rng.standard_normal((n, F)).astype(np.float32)).to(device)
+    return X, w, b, dY, None if ptr is None else torch.from_numpy(ptr).to(device)
+
+
+def check_stats(stats, want):
+    """Sums of x - s in float64: 2^-53 for each of at most 2^24 additions in chains of 2^12 (threads, lanes, tiles one
+    after another), of magnitudes that s keeps near the spread; 1e-11 leaves room."""
+    got = host(stats)
+    spread = 1.0 / want[..., 1]
+    assert (np.abs(got[..., 0] - want[..., 0]) <= 1e-11 * (spread + np.abs(want[..., 0]))).all()
+    assert (np.abs(got[..., 1] / want[..., 1] - 1) <= 1e-11).all()
+
+
+def check(dg, X, w, b, dY, ptr, G, act, out_bf16=False, grad_bf16=False):
+    hp = None if ptr is None else ptr.cpu().numpy()
+    Y, stats = dg.group_norm(X, ptr, groups=G, weight=w, bias=b, act=act, eps=EPS, out_bf16=out_bf16)
+    want, bound, st, rows = groupref.forward(host(X), hp, G, host(w), host(b), act, EPS)
+    check_stats(stats, st)
+    near(Y, want, bound, "Y")
+    if grad_bf16:
+        dY = dY.to(torch.bfloat16)
+    got = dg.group_norm_backward(X, dY, stats, ptr, groups=G, weight=w, bias=b, act=act)
+    wants = groupref.backward(host(X), host(dY), hp, G, host(w), host(b), act, EPS)
+    near(got.X, *wants[0], "dX")
+    assert got.X.dtype == dY.dtype and (got.weight is None) == (w is None) and (got.bias is None) == (b is None)
+    if w is not None:
+        near(got.weight, *wants[1], "dweight")
+        near(got.bias, *wants[2], "dbias")
+    return Y, stats, got
+
+
+@pytest.mark.parametrize("act", [None, "relu", "silu"])
+@pytest.mark.parametrize("F,G", [(1, 1), (2, 1), (3, 3), (4, 2), (5, 1), (8, 8), (33, 3), (64, 8), (99, 9), (128, 1), (130, 130),
+                                 (256, 32), (260, 2), (300, 3), (520, 4), (520, 2), (1032, 8), (2048, 1)])
+@pytest.mark.parametrize("n,B", [(1, 1), (2, 3), (37, 4), (200, 60), (5003, 7), (9001, 700)])
+def test_sizes(dg, device, n, B, F, G, act):
+    if n * F > 4_000_000:
+        n = 4_000_000 // F
+    rng = np.random.default_rng(n + B)
+    check(dg, *case(device, n, F, offsets(rng, n, B)), G, act)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("out_bf16", [False, True])
+@pytest.mark.parametrize("F,G", [(3, 1), (99, 9), (128, 16), (514, 1)])
+def test_types(dg, device, F, G, bf16, out_bf16):
+    rng = np.random.default_rng(F)
+    check(dg, *case(device, 3001, F, offsets(rng, 3001, 40), bf16=bf16), G, "silu", out_bf16, out_bf16)
+    check(dg, *case(device, 700, F, offsets(rng, 700, 40), bf16=bf16, vectors=False), G, "relu", out_bf16, not out_bf16)
+
+
+@pytest.mark.parametrize("n", [1, 7, 1000, 70001])
+def test_one_graph(dg, device, n):
+    check(dg, *case(device, n, 48, None), 6, "silu")
+
+
+def test_lengths_beside_the_tiles(dg, device):
+    """Graphs that end at, one row before and one row behind the ends of tiles of 32 to 256 rows, in every order."""
+    for F, G in ((128, 4), (16, 2), (256, 8)):
+        sizes = [31, 1, 32, 0, 33, 0, 0, 64, 63, 1, 1, 95, 128, 127, 2, 256, 255, 1, 257, 0, 511, 1025, 1, 0]
+        ptr = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+        check(dg, *case(device, int(ptr[-1]), F, ptr), G, "relu")
+
+
+def test_wide(dg, device):
+    for F, G in ((8192, 1), (8192, 2048), (8190, 90), (4100, 4)):
+        check(dg, *case(device, 70, F, np.array([0, 3, 3, 44, 70], np.int32)), G, "silu")
+
+
+@pytest.mark.parametrize("act", [None, "relu"])
+def test_rows_of_no_graph(dg, device, act):
+    """Rows before the first graph and behind the last: 0 in outputs made by the call, left as they were in given ones."""
+    for n, F, G in ((400, 24, 3), (90, 3, 1), (3000, 520, 2), (20, 64, 4)):
+        for first, last in ((n // 5, n - n // 4), (0, 1), (n - 1, n), (n, n), (n // 2, n // 2)):
+            rng = np.random.default_rng(n)
+            X, w, b, dY, ptr = case(device, n, F, offsets(rng, n, 5, first, last))
+            X[:first], dY[last:] = float("nan"), float("nan")
+            rest = np.r_[0:first, last:n]
+            hX, hd = host(X), host(dY)
+            hX[rest], hd[rest] = 0.0, 0.0
+            hp = ptr.cpu().numpy()
+            Y, stats = dg.group_norm(X, ptr, groups=G, weight=w, bias=b, act=act, eps=EPS)
+            want, bound, st, _ = groupref.forward(hX, hp, G, host(w), host(b), act, EPS)
+            near(Y, want, bound, "Y")
+            check_stats(stats, st)
+            g = dg.group_norm_backward(X, dY, stats, ptr, groups=G, weight=w, bias=b, act=act)
+            wants = groupref.backward(hX, hd, hp, G, host(w), host(b), act, EPS)
+            for x, y, what in zip(g, wants, ("dX", "dweight", "dbias")):
+                near(x, *y, what)
+            given = torch.full_like(X, 7.0)
+            dg.group_norm(X, ptr, groups=G, weight=w, bias=b, act=act, eps=EPS, Y=given)
+            assert (given[rest] == 7).all() and torch.equal(given[first:last], Y[first:last])
+            given = torch.full_like(X, 7.0)
+            dg.group_norm_backward(X, dY, stats, ptr, groups=G, weight=w, bias=b, act=act, dX=given)
+            assert (given[rest] == 7).all() and torch.equal(given[first:last], g.X[first:last])
+
+
+def test_in_place(dg, device):
+    for n, B in ((5000, 6), (5000, 900), (40, 1)):
+        rng = np.random.default_rng(B)
+        X, w, b, dY, ptr = case(device, n, 96, offsets(rng, n, B))
+        p = dict(groups=4, weight=w, bias=b, act="silu")
+        Y, stats = dg.group_norm(X, ptr, **p)
+        g = dg.group_norm_backward(X, dY, stats, ptr, **p)
+        Z = X.clone()
+        dg.group_norm(Z, ptr, Y=Z, **p)
+        assert torch.equal(Z, Y)
+        d = dY.clone()
+        again = dg.group_norm_backward(X, d, stats, ptr, dX=d, **p)
+        assert torch.equal(d, g.X) and torch.equal(again.weight, g.weight)
+
+
+def test_rows_at_odd_places(dg, device):
+    """Operands at elements that are 4 (bfloat16: 2) bytes from any alignment; nothing around the outputs is written."""
+    n, F, G = 3001, 70, 5
+    rng = np.random.default_rng(3)
+    X, w, b, dY, ptr = case(device, n, F, offsets(rng, n, 33))
+    for t in (torch.float32, torch.bfloat16):
+        Xt, dt = X.to(t), dY.to(t)
+        p = dict(groups=G, weight=w, bias=b, act="relu")
+        Y, stats = dg.group_norm(Xt, ptr, out_bf16=t == torch.bfloat16, **p)
+        g = dg.group_norm_backward(Xt, dt, stats, ptr, **p)
+
+        def at(k, v):
+            buf = torch.full((n * F + 9,), 5.0, device=device, dtype=t)
+            view = buf[k:k + n * F].view(n, F)
+            if v is not None:
+                view.copy_(v)
+            return buf, view
+
+        _, Xo = at(1, Xt)
+        _, do = at(3, dt)
+        buf, Yo = at(3, None)
+        dg.group_norm(Xo, ptr, out_bf16=t == torch.bfloat16, Y=Yo, **p)
+        assert torch.equal(Yo, Y) and (buf[:3] == 5).all() and (buf[3 + n * F:] == 5).all()
+        buf, dXo = at(5, None)
+        go = dg.group_norm_backward(Xo, do, stats, ptr, dX=dXo, **p)
+        assert torch.equal(dXo, g.X) and (buf[:5] == 5).all() and (buf[5 + n * F:] == 5).all()
+        assert torch.equal(go.weight, g.weight) and torch.equal(go.bias, g.bias)
+
+
+def test_large_means_and_equal_elements(dg, device):
+    """A mean 1e5 times the spread (features as float32 still tell apart), a group of one repeated value, single nodes with
+    one feature a group: variance 0."""
+    for n, B in ((4000, 3), (300, 80)):
+        rng = np.random.default_rng(n)
+        X, w, b, dY, ptr = case(device, n, 64, offsets(rng, n, B))
+        X += 1e5
+        check(dg, X, w, b, dY, ptr, 8, "relu")
+        X[:, 8:16] = 3e4 + 0.1
+        check(dg, X, w, b, dY, ptr, 8, "silu")
+    X, w, b, dY, _ = case(device, 50, 6, None)
+    check(dg, X, w, b, dY, torch.arange(51, dtype=torch.int32, device=device), 6, "silu")
+
+
+def test_what_is_not_finite_stays_in_its_group(dg, device):
+    n, F, G = 4000, 64, 4
+    rng = np.random.default_rng(1)
+    X, w, b, dY, ptr = case(device, n, F, offsets(rng, n, 5))
+    p = dict(groups=G, weight=w, bias=b)
+    for act in ("relu", "silu", None):
+        clean, cs = dg.group_norm(X, ptr, act=act, **p)
+        gclean = dg.group_norm_backward(X, dY, cs, ptr, act=act, **p)
+        lo, hi = int(ptr[2]), int(ptr[3])
+        assert hi > lo + 3
+        for row, v in ((lo, float("nan")), (lo + 2, float("inf")), (lo, float("-inf")), (hi - 1, float("nan"))):
+            bad = X.clone()
+            bad[row, 17] = v
+            Y, stats = dg.group_norm(bad, ptr, act=act, **p)
+            assert torch.isnan(Y[lo:hi, 16:32]).all() and torch.isnan(stats[2, 1]).any()
+            g = dg.group_norm_backward(bad, dY, stats, ptr, act=act, **p)
+            assert torch.isnan(g.X[lo:hi, 16:32]).all()
+            for got, want in ((Y, clean), (g.X, gclean.X)):
+                got[lo:hi, 16:32] = want[lo:hi, 16:32]
+                assert torch.equal(got, want)
+            keep = torch.ones(F, dtype=torch.bool, device=device)
+            keep[16:32] = False
+            assert torch.equal(g.weight[keep], gclean.weight[keep])
+
+
+def test_relu_decides_by_float64(dg, device):
+    """Elements whose normed value times the weight is the bias's negative but for 2^-30: float32 would not tell on which side
+    of 0 they lie."""
+    n, F = 2000, 8
+    rng = np.random.default_rng(9)
+    x = rng.standard_normal((n, F)).astype(np.float32)
+    st = groupref.statistics(x.astype(np.float64), None, 1, EPS)[0, 0]
+    w = np.full(F, 1.5, np.float32)
+    row = 1234
+    b = (-(x[row].astype(np.float64) - st[0]) * st[1] * w).astype(np.float32)       # p of that row is a float32's last place
+    p = (x.astype(np.float64) - st[0]) * st[1] * w + b
+    assert (np.abs(p[row]) < 2.0 ** -22).all() and (p[row] > 0).any() and (p[row] < 0).any()
+    to = lambda a: torch.from_numpy(a).to(device)  # noqa: E731
+    X, W, Bv = to(x), to(w), to(b)
+    _, stats = dg.group_norm(X, groups=1, weight=W, bias=Bv, act="relu", eps=EPS)
+    dY = torch.zeros(n, F, device=device)
+    dY[row] = 1.0
+    g = dg.group_norm_backward(X, dY, stats, groups=1, weight=W, bias=Bv, act="relu")
+    assert np.array_equal(host(g.bias), (p[row] > 0).astype(float))
+
+
+@pytest.mark.filterwarnings("ignore")
+def test_gradients_against_differences():
+    """The reference's own gradient formulas against central differences in float64."""
+    rng = np.random.default_rng(4)
+    n, F, G = 9, 6, 2
+    ptr = np.array([0, 4, 4, 5, 9])
+    X, w, b, dY = rng.standard_normal((n, F)), rng.standard_normal(F), rng.standard_normal(F), rng.standard_normal((n, F))
+    for kind in (None, "relu", "silu"):
+        loss = lambda X, w, b: (groupref.forward(X, ptr, G, w, b, kind, EPS)[0] * dY).sum()  # noqa: E731
+        grads = groupref.backward(X, dY, ptr, G, w, b, kind, EPS)
+        h = 1e-6
+        for k, (v, (g, _)) in enumerate(zip((X, w, b), grads)):
+            for at in np.ndindex(v.shape):
+                a, c = [t.copy() for t in (X, w, b)], [t.copy() for t in (X, w, b)]
+                a[k][at] += h
+                c[k][at] -= h
+                assert abs((loss(*a) - loss(*c)) / (2 * h) - g[at]) <= 1e-6 * (1 + abs(g[at]))
+
+
+def test_streams_and_graphs(dg, device):
+    """On a side stream, and captured: replays read new features and new offsets."""
+    for n, F in ((500, 40), (20000, 64)):
+        rng = np.random.default_rng(n)
+        X, w, b, dY, ptr = case(device, n, F, offsets(rng, n, 9))
+        p = dict(groups=4, weight=w, bias=b, act="silu")
+
+        def call(stream=None):
+            Y, stats = dg.group_norm(X, ptr, stream=stream, **p)
+            return (Y, stats, *dg.group_norm_backward(X, dY, stats, ptr, stream=stream, **p))
+
+        want = call()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = call(side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        torch.cuda.synchronize()
+        graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cap = call()
+        with torch.cuda.graph(other):
+            cap2 = call()
+        for k in range(3):
+            X.normal_()
+            ptr.copy_(torch.from_numpy(offsets(np.random.default_rng(k), n, 9, k, n - 2 * k)))
+            want = call()
+            graph.replay()
+            other.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(cap, want)) and all(torch.equal(x, y) for x, y in zip(cap2, want))
+
+
+def test_more_than_2_to_the_31_elements(dg, device):
+    n, F = (1 << 24) + 77, 136
+    X = torch.empty(n, F, device=device, dtype=torch.bfloat16).normal_()
+    ptr = torch.tensor([0, 1 << 23, n - 3000, n - 10, n], device=device, dtype=torch.int32)
+    w = torch.rand(F, device=device)
+    p = dict(groups=8, weight=w, act="relu")
+    Y, stats = dg.group_norm(X, ptr, out_bf16=True, **p)
+    dX = dg.group_norm_backward(X, Y, stats, ptr, **p).X
+    for k in (2, 3):                                     # the last graphs by themselves
+        lo, hi = int(ptr[k]), int(ptr[k + 1])
+        part = X[lo:hi].contiguous()
+        Yk, sk = dg.group_norm(part, out_bf16=True, **p)
+        assert torch.allclose(sk[0], stats[k], rtol=1e-12, atol=1e-12)
+        assert (Yk.float() - Y[lo:hi].float()).abs().max() <= 2.0 ** -8 * Yk.float().abs().max()
+        dk = dg.group_norm_backward(part, Yk, sk, **p).X
+        assert (dk.float() - dX[lo:hi].float()).abs().max() <= 2.0 ** -7 * dk.float().abs().max()
+
+
+def test_refusals(dg, device):
+    X, w, b, dY, ptr = case(device, 40, 24, np.array([0, 10, 40], np.int32))
+    Y, stats = dg.group_norm(X, ptr, groups=3)
+    for bad in (lambda: dg.group_norm(X.double(), groups=3), lambda: dg.group_norm(X.cpu(), groups=3),
+                lambda: dg.group_norm(X, ptr.long(), groups=3), lambda: dg.group_norm_backward(X, dY, stats.float(), ptr, groups=3),
+                lambda: dg.group_norm(X, groups=3, weight=w.double())):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: dg.group_norm(X, groups=5), lambda: dg.group_norm(X, groups=0), lambda: dg.group_norm(X, groups=3, act="tanh"),
+                lambda: dg.group_norm(X, groups=3, weight=w[:23]), lambda: dg.group_norm(X, ptr[:1], groups=3),
+                lambda: dg.group_norm(X.t(), groups=4), lambda: dg.group_norm(X, ptr, groups=3, Y=Y[:39]),
+                lambda: dg.group_norm(X, ptr, groups=3, stats=stats[:1]),
+                lambda: dg.group_norm_backward(X, dY[:39], stats, ptr, groups=3),
+                lambda: dg.group_norm_backward(X, dY, stats, groups=3)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: dg.group_norm(X, groups=3, eps=0.0), lambda: dg.group_norm(X, ptr, groups=3, Y=X[:, :].view(40, 24), out_bf16=False,
+                                                                                  workspace=torch.empty(64, dtype=torch.uint8, device=device))):
+        with pytest.raises(dg.DualGCNError) as e:
+            bad()
+        assert e.value.status == dg.ERR_INVALID_ARG
+    with pytest.raises(dg.DualGCNError) as e:
+        dg.group_norm(torch.zeros(2, 8193, device=device), groups=1)
+    assert e.value.status == dg.ERR_UNSUPPORTED
