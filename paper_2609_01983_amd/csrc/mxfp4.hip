@@ -20,6 +20,8 @@ namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -222,38 +224,317 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int64_t row, in
 // A workgroup makes 16 rows x 16 columns; its wavefronts take steps of four blocks in turn, operands straight
 // from memory, and join their sums in order through LDS.
 constexpr int kFewWaves = 8;
+constexpr int kFewAhead = 4;                         // steps whose operands are in flight
 __global__ __launch_bounds__(kFewWaves * 64) void product_few_kernel(ProductArgs a) {
     __shared__ f32x4 part[kFewWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = lane & 15, g = lane >> 4;
     const int cols = (a.N + 15) / 16, steps = (a.blocks + 3) / 4;
-    const int64_t tiles = (static_cast<int64_t>(a.n) + 15) / 16 * cols;
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int c0 = static_cast<int>(tile % cols) * 16;
-        const int64_t row0 = tile / cols * 16;
-        const int64_t xr = min(row0 + r, static_cast<int64_t>(a.n) - 1), wr = min(c0 + r, a.N - 1);
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int s = wave; s < steps; s += kFewWaves) {
-            const int b = 4 * s + g;
-            u32x4 x = {0, 0, 0, 0}, w = {0, 0, 0, 0};
-            uint32_t sx = kOne, sw = kOne;
-            if (b < a.blocks) {
-                const int64_t xb = xr * a.blocks + b, wb = wr * a.blocks + b;
-                x = *reinterpret_cast<const u32x4 *>(a.X + xb * kBytes);
-                w = *reinterpret_cast<const u32x4 *>(a.W + wb * kBytes);
-                sx = a.sx[xb];
-                sw = a.sw[wb];
-            }
-            acc = mfma16<0, 0>(w, sw, x, sx, acc);
+    const int c0 = static_cast<int>(blockIdx.x % cols) * 16;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x / cols) * 16;
+    const int64_t xr = min(row0 + r, static_cast<int64_t>(a.n) - 1), wr = min(c0 + r, a.N - 1);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = wave; s0 < steps; s0 += kFewWaves * kFewAhead) {
+        u32x4 x[kFewAhead], w[kFewAhead];
+        uint32_t sx[kFewAhead], sw[kFewAhead];
+#pragma unroll
+        for (int k = 0; k < kFewAhead; ++k) {
+            // (behind the last block its own once more, and 0 for one operand)
+            const int b = min(4 * (s0 + k * kFewWaves) + g, a.blocks - 1);
+            const int64_t xb = xr * a.blocks + b, wb = wr * a.blocks + b;
+            x[k] = *reinterpret_cast<const u32x4 *>(a.X + xb * kBytes);
+            w[k] = *reinterpret_cast<const u32x4 *>(a.W + wb * kBytes);
+            sx[k] = a.sx[xb];
+            sw[k] = a.sw[wb];
         }
-        part[wave][lane] = acc;
-        __syncthreads();
-        if (wave == 0) {
-            for (int k = 1; k < min(kFewWaves, steps); ++k) acc += part[k][lane];
-            store_tile(a, row0 + r, c0 + 4 * g, acc);
+#pragma unroll
+        for (int k = 0; k < kFewAhead; ++k) {
+            const bool there = 4 * (s0 + k * kFewWaves) + g < a.blocks;
+            const u32x4 zero = {0, 0, 0, 0};
+            acc = mfma16<0, 0>(w[k], there ? sw[k] : kOne, there ? x[k] : zero, there ? sx[k] : kOne, acc);
         }
-        __syncthreads();
     }
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0) {
+        for (int k = 1; k < min(kFewWaves, steps); ++k) acc += part[k][lane];
+        store_tile(a, row0 + r, c0 + 4 * g, acc);
+    }
+}
+
+constexpr int kXcds = 8;
+constexpr uint32_t kFar = 0xFFFFFF00u;               // a byte offset past every window
+
+// Many rows: a workgroup of WR x WC wavefronts makes a tile of T, each wavefront 32 R rows of 32 C columns of it.  X and W go
+// through LDS, eight blocks (128 bytes a row) a stage, straight from memory, two stages in turn.  A row's eight blocks
+// stand in an order that depends on the row, so that the lanes' reads of a block of 16 rows fall on all banks.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+constexpr int kStageBlocks = 8;
+constexpr int kStageBytes = kStageBlocks * kBytes;   // of a row
+constexpr int kScaleStages = 4;                           // stages whose scales are read together
+
+// Row i of a matrix instruction is column wide_column(i) of the 32, so that a lane's 16 results are consecutive columns.
+__device__ __forceinline__ int wide_column(int i) { return (i >> 2 & 1) * 16 + (i >> 3) * 4 + (i & 3); }
+__device__ __forceinline__ int wide_row_of(int column) { return (column >> 2 & 3) * 8 + (column >> 4 & 1) * 4 + (column & 3); }
+
+template <int S>
+__device__ __forceinline__ f32x16 mfma32(u32x4 w, uint32_t sw, u32x4 x, uint32_t sx, f32x16 acc) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(w), operand(x), acc, 4, 4, S, static_cast<int>(sw), S, static_cast<int>(sx));
+}
+
+template <int WR, int WC, int R, int C, bool BF>
+struct Tile {
+    static constexpr int kWaves = WR * WC, kBlockSize = 64 * kWaves, kRows = WR * R * 32, kCols = WC * C * 32;
+    static constexpr int kStage = (kRows + kCols) * kStageBytes, kScales = (kRows + kCols) * kStageBlocks * kScaleStages;     // bytes
+    static constexpr int kOut = 32 * (C * 32 * (BF ? 2 : 4) + 16);       // a wavefront's results on their way out
+    static_assert(kRows % (8 * kWaves) == 0 && kCols % (8 * kWaves) == 0 && kWaves % 4 == 0, "pieces of a wavefront");
+    static constexpr int kScaleRows = (kRows + kCols + kBlockSize - 1) / kBlockSize;       // of a thread
+    static constexpr size_t lds(int blocks) {
+        const size_t all = blocks <= kStageBlocks ? kStage + kScales / kScaleStages : 2 * kStage + (blocks > kScaleStages * kStageBlocks ? 2 : 1) * kScales;
+        return std::max<size_t>(all, kWaves * kOut);
+    }
+};
+
+template <int WR, int WC, int R, int C, bool BF>
+__global__ __launch_bounds__(64 * WR * WC, R * C <= 2 ? 4 : R * C <= 4 ? 3 : 2) void product_tiles_kernel(ProductArgs a, int32_t row_tiles, int32_t col_tiles) {
+    using K = Tile<WR, WC, R, C, BF>;
+    extern __shared__ uint4 lds[];
+    uint8_t *base = reinterpret_cast<uint8_t *>(lds);
+    // Workgroup w is on XCD w % 8: each XCD takes consecutive tiles, eight of rows beside each other for each of columns, so that
+    // those at work at a time share rows of X and columns of W.
+    const int all = row_tiles * col_tiles, per = (all + kXcds - 1) / kXcds;
+    const int tile = static_cast<int>(blockIdx.x % kXcds) * per + static_cast<int>(blockIdx.x / kXcds);
+    if (static_cast<int>(blockIdx.x / kXcds) >= per || tile >= all) return;
+    const int band = tile / (8 * col_tiles), high = min(8, row_tiles - 8 * band), in = tile - band * 8 * col_tiles;
+    const int64_t row0 = static_cast<int64_t>(8 * band + in % high) * K::kRows;
+    const int c0 = in / high * K::kCols;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 31, g = lane >> 5;
+    const int row_bytes = a.blocks * kBytes;
+    const int rows = static_cast<int>(min(static_cast<int64_t>(K::kRows), a.n - row0)), cols = min(K::kCols, a.N - c0);
+    const __amdgpu_buffer_rsrc_t wx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.X) + row0 * row_bytes, 0, rows * row_bytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ww = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.W) + static_cast<int64_t>(c0) * row_bytes, 0, cols * row_bytes, 0x00020000);
+    const uint8_t *sx = a.sx + row0 * a.blocks, *sw = a.sw + static_cast<int64_t>(c0) * a.blocks;
+
+    // eight rows of 128 bytes an instruction: lane l has row l / 8's place l % 8.  What lies behind the last row or block is 0.
+    const int line = wave * 8 + lane / 8;
+    const int bx = lane % 8 ^ (line >> 1 & 7), bw = lane % 8 ^ (wide_row_of(line & 31) >> 1 & 7);
+    const uint32_t from = static_cast<uint32_t>(line) * row_bytes;
+    auto request = [&](int stage, int b0) {
+        uint8_t *to = base + stage * K::kStage + wave * 8 * kStageBytes;
+        const uint32_t x_at = b0 + bx < a.blocks ? from + (b0 + bx) * kBytes : kFar;
+        const uint32_t w_at = b0 + bw < a.blocks ? from + (b0 + bw) * kBytes : kFar;
+        typedef __attribute__((address_space(3))) void *lds_ptr;
+#pragma unroll
+        for (int i = 0; i < K::kRows / 8 / K::kWaves; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wx, (lds_ptr)(to + i * K::kWaves * 8 * kStageBytes), 16,
+                                                     x_at == kFar ? kFar : x_at + static_cast<uint32_t>(i * K::kWaves * 8) * row_bytes, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < K::kCols / 8 / K::kWaves; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ww, (lds_ptr)(to + (K::kRows + i * K::kWaves * 8) * kStageBytes), 16,
+                                                     w_at == kFar ? kFar : w_at + static_cast<uint32_t>(i * K::kWaves * 8) * row_bytes, 0, 0, 0);
+    };
+    // The scales of four stages' blocks of the thread's rows, eight bytes a stage; 1 behind the last block, where both operands are
+    // 0.  (A stage's at a time cost as much as its operands: 64 rows are 64 lines, whatever is read of each.)
+    uint64_t held[K::kScaleRows][kScaleStages];
+    const uint32_t x_end = static_cast<uint32_t>(min((a.n - row0) * a.blocks, int64_t{1} << 31));      // of the operand
+    const uint32_t w_end = static_cast<uint32_t>(min(static_cast<int64_t>(a.N - c0) * a.blocks, int64_t{1} << 31));
+    uint8_t *const scales = base + (a.blocks > kStageBlocks ? 2 : 1) * K::kStage;
+    auto request_scales = [&](int b0) {
+        const int stages = min(kScaleStages, (a.blocks - b0 + kStageBlocks - 1) / kStageBlocks);
+#pragma unroll
+        for (int i = 0; i < K::kScaleRows; ++i) {
+            const int row = i * K::kBlockSize + static_cast<int>(threadIdx.x);
+            const bool of_x = row < K::kRows;
+            const int own = of_x ? min(row, rows - 1) : min(row - K::kRows, cols - 1);
+            const uint32_t at = own * static_cast<uint32_t>(a.blocks) + b0, end = of_x ? x_end : w_end;
+            const uint8_t *from = (of_x ? sx : sw) + at;
+#pragma unroll
+            for (int q = 0; q < kScaleStages; ++q) {
+                typedef uint64_t u64_at1 __attribute__((aligned(1)));
+                held[i][q] = 0;
+                if (q < stages) {                                        // uniform
+                    if (at + (q + 1) * kStageBlocks <= end) {            // the next rows' scales are read along
+                        held[i][q] = *reinterpret_cast<const u64_at1 *>(from + q * kStageBlocks);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kStageBlocks - 1; ++k)
+                            if (at + q * kStageBlocks + k < end) held[i][q] |= static_cast<uint64_t>(from[q * kStageBlocks + k]) << 8 * k;
+                    }
+                }
+            }
+        }
+    };
+    auto keep_scales = [&](int b0) {
+        uint8_t *to = scales + b0 / kStageBlocks / kScaleStages % 2 * K::kScales;
+#pragma unroll
+        for (int q = 0; q < kScaleStages; ++q) {
+            const int left = a.blocks - b0 - q * kStageBlocks;
+            if (left <= 0) break;                                        // uniform
+            const uint64_t kept = left >= kStageBlocks ? ~uint64_t{0} : (uint64_t{1} << 8 * left) - 1;
+#pragma unroll
+            for (int i = 0; i < K::kScaleRows; ++i) {
+                const int row = i * K::kBlockSize + static_cast<int>(threadIdx.x);
+                if (row < K::kRows + K::kCols)
+                    *reinterpret_cast<uint64_t *>(to + (q * (K::kRows + K::kCols) + row) * kStageBlocks) = (held[i][q] & kept) | (0x7F7F7F7F7F7F7F7Full & ~kept);
+            }
+        }
+    };
+
+    f32x16 acc[R][C];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < C; ++j) acc[i][j] = f32x16{};
+    const int x0 = wave / WC * R * 32, w0 = wave % WC * C * 32;          // the wavefront's rows and columns of the tile
+    // A turn multiplies two blocks of k; the next turn's operands are on their way from LDS meanwhile, also over the end of a
+    // stage: the barrier that hands the stages over stands before its last turn's products.
+    u32x4 x[2][R], w[2][C];
+    u32x2 fx[R], fw[C];
+    const int own_x = x0 + r, own_w = w0 + wide_column(r);
+    auto fetch = [&](int stage, int k) {
+        const uint8_t *xs = base + stage * K::kStage, *ws = xs + K::kRows * kStageBytes;
+        const int place = (2 * k + g ^ (r >> 1 & 7)) * kBytes;
+#pragma unroll
+        for (int i = 0; i < R; ++i) x[k % 2][i] = *reinterpret_cast<const u32x4 *>(xs + (own_x + 32 * i) * kStageBytes + place);
+#pragma unroll
+        for (int j = 0; j < C; ++j) w[k % 2][j] = *reinterpret_cast<const u32x4 *>(ws + (own_w + 32 * j) * kStageBytes + place);
+    };
+    auto fetch_scales = [&](int b0) {
+        const int q = b0 / kStageBlocks;
+        const uint8_t *sc = scales + q / kScaleStages % 2 * K::kScales + q % kScaleStages * (K::kRows + K::kCols) * kStageBlocks;
+#pragma unroll
+        for (int i = 0; i < R; ++i) fx[i] = *reinterpret_cast<const u32x2 *>(sc + (own_x + 32 * i) * kStageBlocks);
+#pragma unroll
+        for (int j = 0; j < C; ++j) fw[j] = *reinterpret_cast<const u32x2 *>(sc + (K::kRows + own_w + 32 * j) * kStageBlocks);
+    };
+    // loads into LDS are waited for by hand: a barrier alone need not
+    auto hand_over = [&]() {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    auto multiply = [&](int k, const uint32_t (&sx)[R], const uint32_t (&sw)[C]) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+                acc[i][j] = k % 2 ? mfma32<2>(w[k % 2][j], sw[j], x[k % 2][i], sx[i], acc[i][j])
+                                  : mfma32<0>(w[k % 2][j], sw[j], x[k % 2][i], sx[i], acc[i][j]);
+        // the turns stay in order: without this the compiler reads several turns' operands first and spills
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < C; ++j) asm volatile("" : "+v"(acc[i][j])::"memory");
+    };
+    constexpr int kStageTurns = kStageBlocks / 2, kGroupBlocks = kScaleStages * kStageBlocks;
+    request(0, 0);
+    request_scales(0);
+    keep_scales(0);
+    hand_over();
+    if (a.blocks > kStageBlocks) request(1, kStageBlocks);
+    if (a.blocks > kGroupBlocks) request_scales(kGroupBlocks);
+    fetch_scales(0);
+    fetch(0, 0);
+    uint32_t nx[R], nw[C];                           // a word of each for two turns
+    auto scales_of = [&](int k) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) nx[i] = fx[i][k / 2] >> 8 * g;
+#pragma unroll
+        for (int j = 0; j < C; ++j) nw[j] = fw[j][k / 2] >> 8 * g;
+    };
+    int stage = 0, b0 = 0;
+    for (; b0 + kStageBlocks < a.blocks; b0 += kStageBlocks, stage ^= 1) {
+#pragma unroll
+        for (int k = 0; k < kStageTurns; ++k) {
+            if (k % 2 == 0) scales_of(k);
+            if (k + 1 < kStageTurns) {
+                fetch(stage, k + 1);
+            } else {
+                const int next = b0 + kStageBlocks;
+                if (next % kGroupBlocks == 0) keep_scales(next);
+                hand_over();                         // the next stage is there, this one has been read
+                if (next + kStageBlocks < a.blocks) request(stage, next + kStageBlocks);
+                if (next % kGroupBlocks == 0 && next + kGroupBlocks < a.blocks) request_scales(next + kGroupBlocks);
+                fetch_scales(next);
+                fetch(stage ^ 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(k, nx, nw);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kStageTurns; ++k) {
+        if (k % 2 == 0) scales_of(k);
+        if (k + 1 < kStageTurns) fetch(stage, k + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(k, nx, nw);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // a lane's 16 results are columns 16 g .. 16 g + 15 of row r: 32 rows at a time go through the wavefront's own part of LDS,
+    // so that a row is written in whole lines
+    __syncthreads();
+    constexpr int kSize = BF ? 2 : 4, kPer = 16 / kSize, kLine = C * 32 * kSize, kPitch = kLine + 16, kLanes = kLine / 16;
+    uint8_t *own = base + wave * K::kOut;
+    const int last = a.N - c0 - w0;                                      // columns there are of the wavefront's
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; q += kPer) {
+                u32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (BF) {
+                        typedef float f32x2 __attribute__((ext_vector_type(2)));
+                        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                        v[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc[i][j][q + 2 * e], acc[i][j][q + 2 * e + 1]}), bf16x2));
+                    } else {
+                        v[e] = __float_as_uint(acc[i][j][q + e]);
+                    }
+                }
+                *reinterpret_cast<u32x4 *>(own + r * kPitch + (32 * j + 16 * g + q) * kSize) = v;
+            }
+        __builtin_amdgcn_wave_barrier();
+        const int64_t first = row0 + x0 + 32 * i;
+#pragma unroll
+        for (int k = 0; k < (32 * kLanes + 63) / 64; ++k) {
+            const int piece = 64 * k + lane, row = piece / kLanes, col = piece % kLanes * kPer;
+            if (row >= 32 || first + row >= a.n || col >= last) continue;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(own + row * kPitch + col * kSize);
+            char *to = static_cast<char *>(a.T) + ((first + row) * a.N + c0 + w0 + col) * kSize;
+            if (last - col >= kPer) {
+                *reinterpret_cast<typename std::conditional<BF, u32x4_at2, u32x4_at4>::type *>(to) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPer - 1; ++e)
+                    if (e < last - col) {
+                        if constexpr (BF) reinterpret_cast<unsigned short *>(to)[e] = static_cast<unsigned short>(v[e / 2] >> 16 * (e % 2));
+                        else reinterpret_cast<uint32_t *>(to)[e] = v[e];
+                    }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+int allow_lds(const void *kernel, size_t bytes) {
+    if (bytes <= 64 * 1024) return DUALGCN_OK;
+    return hip_status(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+}
+
+template <int WR, int WC, int R, int C, bool BF>
+int launch_tiles(const ProductArgs &a, hipStream_t s) {
+    using K = Tile<WR, WC, R, C, BF>;
+    const size_t lds = K::lds(a.blocks);
+    const int st = allow_lds(reinterpret_cast<const void *>(&product_tiles_kernel<WR, WC, R, C, BF>), lds);
+    if (st) return st;
+    const int64_t rows = (static_cast<int64_t>(a.n) + K::kRows - 1) / K::kRows, cols = (a.N + K::kCols - 1) / K::kCols;
+    hipLaunchKernelGGL((product_tiles_kernel<WR, WC, R, C, BF>), dim3(static_cast<unsigned>((rows * cols + kXcds - 1) / kXcds * kXcds)),
+                       dim3(K::kBlockSize), lds, s, a, static_cast<int32_t>(rows), static_cast<int32_t>(cols));
+    return hip_status(hipGetLastError());
 }
 
 }  // namespace
@@ -299,9 +580,23 @@ int launch_update_mxfp4(const void *X, const void *sx, const void *W, const void
                         int32_t F_in, int32_t F_out, hipStream_t s) {
     const ProductArgs a{static_cast<const uint8_t *>(X), static_cast<const uint8_t *>(sx), static_cast<const uint8_t *>(W),
                         static_cast<const uint8_t *>(sw), T, n, F_out, (F_in + kBlock - 1) / kBlock, out_bf16};
-    const int64_t tiles = (static_cast<int64_t>(n) + 15) / 16 * ((F_out + 15) / 16);
-    hipLaunchKernelGGL(product_few_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(tiles, 1 << 20))), dim3(kFewWaves * 64), 0, s, a);
-    return hip_status(hipGetLastError());
+    // Which kernel, us (f32 T; few, 256 x 256, 128 x 128, 128 x 64 tiles):
+    //   few rows or tiles: 1 row 8,192 -> 1,024 7.9, -, -, 19.0; 64 rows 9.4, -, -, 19.6; 64 rows 4,096 -> 4,096 16.4, 29.8, 14.9, 11.3
+    //   the largest, where they still fill the chip and several stages follow each other: 4,096^2 -> 4,096 -, 46.5, 54.3,
+    //     68.9; 2^19 1,024 -> 1,024 -, 612, 673, 778; 200,000 512 -> 512 -, 103, 129, 126, but 512 -> 256 -, 52.6, 48.3, 48.1
+    //   narrow tiles, where there are few columns or the others leave compute units idle: 10^6 rows 128 -> 16 -, 108, 50, 35;
+    //     1,000 rows 4,096 -> 4,096 -, 35.4, 18.9, 18.8, but 2,000 rows -, 37.3, 28.1, 35.2
+    auto tiles_of = [&](int64_t rows, int64_t cols) { return (n + rows - 1) / rows * ((F_out + cols - 1) / cols); };
+    const int64_t cus = device_cus();
+    if (n <= 32 || tiles_of(16, 16) <= cus) {
+        hipLaunchKernelGGL(product_few_kernel, dim3(static_cast<unsigned>(tiles_of(16, 16))), dim3(kFewWaves * 64), 0, s, a);
+        return hip_status(hipGetLastError());
+    }
+    if (a.blocks > kStageBlocks && (F_out > 256 || a.blocks > 2 * kStageBlocks) && 4 * tiles_of(256, 256) >= 3 * cus)
+        return out_bf16 ? launch_tiles<2, 4, 4, 2, true>(a, s) : launch_tiles<2, 4, 4, 2, false>(a, s);
+    if (F_out <= 64 || tiles_of(128, 128) < cus)
+        return out_bf16 ? launch_tiles<4, 1, 1, 2, true>(a, s) : launch_tiles<4, 1, 1, 2, false>(a, s);
+    return out_bf16 ? launch_tiles<2, 2, 2, 2, true>(a, s) : launch_tiles<2, 2, 2, 2, false>(a, s);
 }
 
 }  // namespace dgc
