@@ -51,6 +51,7 @@ struct GroupArgs {
     int32_t lanes;                                   // of a group of whole quads in a power of two of lanes, else 0
     int32_t act;                                     // 0, DUALGCN_RELU or DUALGCN_SILU
     bool fill;                                       // rows of no graph receive zeros
+    bool streaming;                                  // the output is more than the caches keep
     bool split;                                      // a workgroup has one group, in chunks of kSlice columns
 };
 
@@ -417,7 +418,7 @@ struct Forward {
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
                     if (row + k * c.kRows >= rows) break;                // uniform
-                    store_row_quad<Y_BF, TINY>(wy, at[k], activated(unit(in[k].get(c.at, c.odd)) * v.weight + v.bias, a.act), c.odd, false);
+                    store_row_quad<Y_BF, TINY>(wy, at[k], activated(unit(in[k].get(c.at, c.odd)) * v.weight + v.bias, a.act), c.odd, a.streaming);
                 }
             }
         }
@@ -534,9 +535,10 @@ struct Backward {
 
     // f(place, d, u) for rows [first, first + rows) of graph `number` in chunk `chunk`, where d = dY act'(p).  Next to 0 it is the
     // sign of p in float64 that decides what a ReLU passes.
-    template <class Fn>
+    // after() follows each kAheadBack of a thread's rows.
+    template <class Fn, class After>
     static __device__ __forceinline__ void rows_do(const GroupArgs &a, const Cols &c, const Unit &unit, row_f32x4 weight, row_f32x4 bias, int number,
-                                                   int first, int rows, Fn f) {
+                                                   int first, int rows, Fn f, After after) {
         const __amdgpu_buffer_rsrc_t wx = rows_of<X_BF>(a, a.X, first, rows), wg = rows_of<G_BF>(a, a.dY, first, rows);
         for (int row = 0; row < rows; row += c.kRows * kAheadBack) {
             RawRowQuad<X_BF, TINY> xs[kAheadBack];
@@ -579,6 +581,7 @@ struct Backward {
                 f(at[k], g, u);
                 __builtin_amdgcn_sched_barrier(0);       // a row after the other: four at once take twice the registers
             }
+            after();
         }
     }
     static __device__ __forceinline__ Unit unit_of(const GroupArgs &a, const Cols &c, int number) {
@@ -604,8 +607,8 @@ struct Backward {
                 m2[i] = static_cast<float>(v.y * one);
             }
             rows_do(a, c, unit, weight, bias, g.number, first, rows, [&](const QuadPlace &at, row_f32x4 d, row_f32x4 u) {
-                store_row_quad<G_BF, TINY>(to, at, unit.r * (d * weight - m1 - u * m2), c.odd, false);
-            });
+                store_row_quad<G_BF, TINY>(to, at, unit.r * (d * weight - m1 - u * m2), c.odd, a.streaming);
+            }, [] {});
         }
     }
 };
@@ -670,13 +673,19 @@ __global__ __launch_bounds__(kThreads, 3) void group_back_kernel(GroupArgs a) {
             const typename K::Cols c(a, chunk);
             const row_f32x4 weight = c.vector(a.weight, 1.f), bias = c.vector(a.bias, 0.f);
             double d1[4] = {0.0, 0.0, 0.0, 0.0}, d2[4] = {0.0, 0.0, 0.0, 0.0};
+            // float32 over kAheadBack rows, then float64
+            const row_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            row_f32x4 s1 = zero, s2 = zero;
             K::rows_do(a, c, K::unit_of(a, c, number), weight, bias, number, first, rows, [&](const QuadPlace &, row_f32x4 d, row_f32x4 u) {
-                const row_f32x4 du = d * u;
+                s1 += d;
+                s2 += d * u;
+            }, [&] {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    d1[i] += d[i];
-                    d2[i] += du[i];
+                    d1[i] += s1[i];
+                    d2[i] += s2[i];
                 }
+                s1 = s2 = zero;
             });
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -770,7 +779,7 @@ __global__ __launch_bounds__(kThreads) void group_back_apply_kernel(GroupArgs a)
 constexpr int kWaveTurns = 16;
 constexpr int kWaveGraphs = 2048;
 // A team's turns for a graph that is not long, forward and backward: about what the two more launches for long ones take.
-constexpr int kLimitTurns = 32, kLimitTurnsBack = 16;
+constexpr int kLimitTurns = 32, kLimitTurnsBack = 8;
 
 int lanes_of(int32_t width) { return width < 4 ? 1 : width <= 32 ? 8 : width <= 64 ? 16 : width <= 128 ? 32 : 64; }
 
@@ -788,7 +797,8 @@ struct Shape {
         const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMostTiles / sets, (int64_t{1} << 22) / F));
         team = !split && B >= kWaveGraphs && n / B * lanes <= 64 * kWaveTurns ? 1 : kWaves;
         const int64_t at_once = std::max<int64_t>(1, (back ? kLimitTurnsBack : kLimitTurns) * 64 * team / lanes / chunks);
-        int64_t rows = ((n + most - 1) / most + turn - 1) / turn * turn;
+        const int64_t least = back ? 2 * turn : turn;
+        int64_t rows = ((n + most - 1) / most + least - 1) / least * least;
         if (rows > at_once && n / at_once <= 4 * most) rows = at_once;       // rather more tiles than long turns
         rows = std::min(rows, std::max<int64_t>(1, (int64_t{1} << 26) / F / turn) * turn);       // 32-bit offsets
         tile_rows = static_cast<int32_t>(rows);
@@ -881,6 +891,7 @@ GroupArgs common(const dualgcn_group_norm &p, const void *X, int32_t n, const Sh
     a.split = s.split;
     a.act = static_cast<int32_t>(p.flags & (DUALGCN_RELU | DUALGCN_SILU));
     a.fill = p.flags & DUALGCN_ZERO_REST;
+    a.streaming = static_cast<int64_t>(n) * p.F >= int64_t{1} << 26;
     a.slots = static_cast<double2 *>(workspace);
     a.pieces = reinterpret_cast<int4 *>(static_cast<char *>(workspace) + up(sizeof(double2) * (static_cast<size_t>(s.tiles) + a.B) * a.G));
     return a;
