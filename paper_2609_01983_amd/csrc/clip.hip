@@ -56,23 +56,24 @@ __device__ __forceinline__ int tensor_of(const Table &t, uint32_t chunk) {
 }
 
 // The sum over a workgroup, the same in every thread.
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v) {
-    __shared__ row_f32x4 sh[row_reduce_quads<kThreads>()];
+    __shared__ row_f32x4 sh[row_reduce_quads<THREADS>()];
     int turn = 0;
-    return row_sum<kThreads>(v, sh, turn);
+    return row_sum<THREADS>(v, sh, turn);
 }
 
 template <bool BF>
-__device__ __forceinline__ double squares(const void *g, int64_t at, int64_t count) {
+__device__ __forceinline__ double squares(const void *g, int64_t at, int64_t count, int thread) {
     row_f32x4 v[kQuads];
     const int64_t left = count - at;
     if (left >= kChunk) {
 #pragma unroll
-        for (int k = 0; k < kQuads; ++k) v[k] = load_quad<BF>(g, at + 4 * (k * kThreads + static_cast<int>(threadIdx.x)), 4);
+        for (int k = 0; k < kQuads; ++k) v[k] = load_quad<BF>(g, at + 4 * (k * kThreads + thread), 4);
     } else {
 #pragma unroll
         for (int k = 0; k < kQuads; ++k) {
-            const int i = 4 * (k * kThreads + static_cast<int>(threadIdx.x));
+            const int i = 4 * (k * kThreads + thread);
             v[k] = load_quad<BF>(g, at + i, static_cast<int>(left) - i);
         }
     }
@@ -87,15 +88,20 @@ __device__ __forceinline__ double squares(const void *g, int64_t at, int64_t cou
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-__global__ __launch_bounds__(kThreads) void square_kernel(SumTable<kSumTensors> t, double *__restrict__ partial) {
+// Chunk c of a table: its elements' squares' sum, or the result.
+template <class Table>
+__device__ __forceinline__ double squares_of(const Table &t, uint32_t c, int thread) {
+    const int k = tensor_of(t, c);
+    const int64_t at = static_cast<int64_t>(c - t.first[k]) * kChunk, n = t.count[k];
+    return n < 0 ? squares<true>(t.grad[k], at, -n, thread) : squares<false>(t.grad[k], at, n, thread);
+}
+
+template <int N>
+__global__ __launch_bounds__(kThreads) void square_kernel(SumTable<N> t, double *__restrict__ partial) {
     double s = 0.0;
     const uint32_t chunks = t.first[t.tensors];
-    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int k = tensor_of(t, c);
-        const int64_t at = static_cast<int64_t>(c - t.first[k]) * kChunk, n = t.count[k];
-        s += n < 0 ? squares<true>(t.grad[k], at, -n) : squares<false>(t.grad[k], at, n);
-    }
-    s = block_sum(s);
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) s += squares_of(t, c, threadIdx.x);
+    s = block_sum<kThreads>(s);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
@@ -104,7 +110,7 @@ __device__ __forceinline__ double norm_of(const double *__restrict__ partial, in
     double s = 0.0;
 #pragma unroll 8
     for (int i = threadIdx.x; i < partials; i += kThreads) s += partial[i];
-    return sqrt(block_sum(s));
+    return sqrt(block_sum<kThreads>(s));
 }
 
 __global__ __launch_bounds__(kThreads) void norm_kernel(const double *__restrict__ partial, int32_t partials, float *norm) {
@@ -113,19 +119,19 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const double *__restrict
 }
 
 template <bool BF>
-__device__ __forceinline__ void scale_chunk(const void *g, const float *w, void *out, int64_t at, int64_t count, double f) {
+__device__ __forceinline__ void scale_chunk(const void *g, const float *w, void *out, int64_t at, int64_t count, double f, int thread) {
     row_f32x4 v[kQuads], x[kQuads];
     const int64_t left = count - at;
     const int most = left < kChunk ? static_cast<int>(left) : kChunk;
 #pragma unroll
     for (int k = 0; k < kQuads; ++k) {
-        const int i = 4 * (k * kThreads + static_cast<int>(threadIdx.x));
+        const int i = 4 * (k * kThreads + thread);
         v[k] = load_quad<BF>(g, at + i, most - i);
         if (w) x[k] = load_quad<false>(w, at + i, most - i);
     }
 #pragma unroll
     for (int k = 0; k < kQuads; ++k) {
-        const int i = 4 * (k * kThreads + static_cast<int>(threadIdx.x));
+        const int i = 4 * (k * kThreads + thread);
         row_f32x4 y;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -135,19 +141,39 @@ __device__ __forceinline__ void scale_chunk(const void *g, const float *w, void 
     }
 }
 
-__global__ __launch_bounds__(kThreads) void apply_kernel(ApplyTable<kApplyTensors> t, const double *__restrict__ partial,
-                                                         int32_t partials, double max_norm, double eps, double lr, float *norm) {
-    const double v = norm_of(partial, partials), with = v + eps;
+__device__ __forceinline__ double factor_of(double norm, double max_norm, double eps) {
+    return norm + eps <= max_norm ? 1.0 : max_norm / (norm + eps);       // (a NaN stays one)
+}
+template <class Table>
+__device__ __forceinline__ void scale_of(const Table &t, uint32_t c, double f, double lr, int thread) {
+    const int k = tensor_of(t, c);
+    const int64_t at = static_cast<int64_t>(c - t.first[k]) * kChunk, n = t.count[k];
+    const double by = t.weight[k] ? -lr * f : f;
+    if (n < 0) scale_chunk<true>(t.grad[k], t.weight[k], t.out[k], at, -n, by, thread);
+    else scale_chunk<false>(t.grad[k], t.weight[k], t.out[k], at, n, by, thread);
+}
+
+template <int N>
+__global__ __launch_bounds__(kThreads) void apply_kernel(ApplyTable<N> t, const double *__restrict__ partial, int32_t partials, double max_norm,
+                                                         double eps, double lr, float *norm) {
+    const double v = norm_of(partial, partials);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(v);
-    double f = with <= max_norm ? 1.0 : max_norm / with;         // (a NaN stays one)
+    const double f = factor_of(v, max_norm, eps);
     const uint32_t chunks = t.first[t.tensors];
-    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int k = tensor_of(t, c);
-        const int64_t at = static_cast<int64_t>(c - t.first[k]) * kChunk, n = t.count[k];
-        const double by = t.weight[k] ? -lr * f : f;
-        if (n < 0) scale_chunk<true>(t.grad[k], t.weight[k], t.out[k], at, -n, by);
-        else scale_chunk<false>(t.grad[k], t.weight[k], t.out[k], at, n, by);
-    }
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) scale_of(t, c, f, lr, threadIdx.x);
+}
+
+// Few small tensors: both passes by one workgroup, four chunks at a time.
+constexpr int kSmallThreads = 4 * kThreads, kSmallTensors = 8, kSmallChunks = 8;
+__global__ __launch_bounds__(kSmallThreads) void small_kernel(ApplyTable<kSmallTensors> t, bool apply, double max_norm, double eps, double lr, float *norm) {
+    const uint32_t chunks = t.first[t.tensors], first = threadIdx.x / kThreads;
+    const int thread = threadIdx.x % kThreads;
+    double s = 0.0;
+    for (uint32_t c = first; c < chunks; c += kSmallThreads / kThreads) s += squares_of(t, c, thread);
+    const double v = sqrt(block_sum<kSmallThreads>(s)), f = factor_of(v, max_norm, eps);
+    if (threadIdx.x == 0) *norm = static_cast<float>(v);
+    if (apply)
+        for (uint32_t c = first; c < chunks; c += kSmallThreads / kThreads) scale_of(t, c, f, lr, thread);
 }
 
 // Launches over the tensors, as many at a time as a table holds: fill(table, place, tensor) and
@@ -181,30 +207,53 @@ size_t clip_workspace_bytes(int32_t tensors) {
     return tables * kGrid * sizeof(double);
 }
 
-int launch_clip(const dualgcn_grad *g, int32_t tensors, bool apply, double max_norm, double eps, double lr, float *norm,
-                void *workspace, hipStream_t s) {
-    double *partial = static_cast<double *>(workspace);
+namespace {
+
+template <int S, int A>
+int launch_tables(const dualgcn_grad *g, int32_t tensors, bool apply, double max_norm, double eps, double lr, float *norm, double *partial,
+                  hipStream_t s) {
     int32_t partials = 0;
-    in_tables<SumTable<kSumTensors>, kSumTensors>(
-        g, tensors, [](SumTable<kSumTensors> &, int, const dualgcn_grad &) {},
-        [&](const SumTable<kSumTensors> &t) {
+    in_tables<SumTable<S>, S>(
+        g, tensors, [](SumTable<S> &, int, const dualgcn_grad &) {},
+        [&](const SumTable<S> &t) {
             const int32_t grid = static_cast<int32_t>(std::min<uint32_t>(t.first[t.tensors], kGrid));
-            hipLaunchKernelGGL(square_kernel, dim3(grid), dim3(kThreads), 0, s, t, partial + partials);
+            hipLaunchKernelGGL(square_kernel<S>, dim3(grid), dim3(kThreads), 0, s, t, partial + partials);
             partials += grid;
         });
     if (apply)
-        in_tables<ApplyTable<kApplyTensors>, kApplyTensors>(
+        in_tables<ApplyTable<A>, A>(
             g, tensors,
-            [](ApplyTable<kApplyTensors> &t, int at, const dualgcn_grad &one) {
+            [](ApplyTable<A> &t, int at, const dualgcn_grad &one) {
                 t.weight[at] = one.weight;
                 t.out[at] = one.out;
             },
-            [&](const ApplyTable<kApplyTensors> &t) {
+            [&](const ApplyTable<A> &t) {
                 const uint32_t grid = std::min<uint32_t>(t.first[t.tensors], kGrid);
-                hipLaunchKernelGGL(apply_kernel, dim3(grid), dim3(kThreads), 0, s, t, partial, partials, max_norm, eps, lr, norm);
+                hipLaunchKernelGGL(apply_kernel<A>, dim3(grid), dim3(kThreads), 0, s, t, partial, partials, max_norm, eps, lr, norm);
                 norm = nullptr;
             });
     if (norm) hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, s, partial, partials, norm);
+    return hip_status(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_clip(const dualgcn_grad *g, int32_t tensors, bool apply, double max_norm, double eps, double lr, float *norm,
+                void *workspace, hipStream_t s) {
+    double *partial = static_cast<double *>(workspace);
+    if (tensors > kSmallTensors)
+        return launch_tables<kSumTensors, kApplyTensors>(g, tensors, apply, max_norm, eps, lr, norm, partial, s);
+    int64_t chunks = 0;
+    for (int32_t i = 0; i < tensors; ++i) chunks += (g[i].count + kChunk - 1) / kChunk;
+    if (chunks == 0 || chunks > kSmallChunks)
+        return launch_tables<kSmallTensors, kSmallTensors>(g, tensors, apply, max_norm, eps, lr, norm, partial, s);
+    in_tables<ApplyTable<kSmallTensors>, kSmallTensors>(
+        g, tensors,
+        [](ApplyTable<kSmallTensors> &t, int at, const dualgcn_grad &one) {
+            t.weight[at] = one.weight;
+            t.out[at] = one.out;
+        },
+        [&](const ApplyTable<kSmallTensors> &t) { hipLaunchKernelGGL(small_kernel, dim3(1), dim3(kSmallThreads), 0, s, t, apply, max_norm, eps, lr, norm); });
     return hip_status(hipGetLastError());
 }
 
