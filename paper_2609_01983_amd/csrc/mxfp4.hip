@@ -576,27 +576,45 @@ int launch_dequantize_mxfp4(const void *Q, const void *scales, int32_t n, int32_
     return hip_status(hipGetLastError());
 }
 
-int launch_update_mxfp4(const void *X, const void *sx, const void *W, const void *sw, void *T, bool out_bf16, int32_t n,
-                        int32_t F_in, int32_t F_out, hipStream_t s) {
-    const ProductArgs a{static_cast<const uint8_t *>(X), static_cast<const uint8_t *>(sx), static_cast<const uint8_t *>(W),
-                        static_cast<const uint8_t *>(sw), T, n, F_out, (F_in + kBlock - 1) / kBlock, out_bf16};
+namespace {
+
+int launch_product(const ProductArgs &a, hipStream_t s) {
     // Which kernel, us (f32 T; few, 256 x 256, 128 x 128, 128 x 64 tiles):
     //   few rows or tiles: 1 row 8,192 -> 1,024 7.9, -, -, 19.0; 64 rows 9.4, -, -, 19.6; 64 rows 4,096 -> 4,096 16.4, 29.8, 14.9, 11.3
     //   the largest, where they still fill the chip and several stages follow each other: 4,096^2 -> 4,096 -, 46.5, 54.3,
     //     68.9; 2^19 1,024 -> 1,024 -, 612, 673, 778; 200,000 512 -> 512 -, 103, 129, 126, but 512 -> 256 -, 52.6, 48.3, 48.1
     //   narrow tiles, where there are few columns or the others leave compute units idle: 10^6 rows 128 -> 16 -, 108, 50, 35;
     //     1,000 rows 4,096 -> 4,096 -, 35.4, 18.9, 18.8, but 2,000 rows -, 37.3, 28.1, 35.2
-    auto tiles_of = [&](int64_t rows, int64_t cols) { return (n + rows - 1) / rows * ((F_out + cols - 1) / cols); };
+    auto tiles_of = [&](int64_t rows, int64_t cols) { return (a.n + rows - 1) / rows * ((a.N + cols - 1) / cols); };
     const int64_t cus = device_cus();
-    if (n <= 32 || tiles_of(16, 16) <= cus) {
+    if (a.n <= 32 || tiles_of(16, 16) <= cus) {
         hipLaunchKernelGGL(product_few_kernel, dim3(static_cast<unsigned>(tiles_of(16, 16))), dim3(kFewWaves * 64), 0, s, a);
         return hip_status(hipGetLastError());
     }
-    if (a.blocks > kStageBlocks && (F_out > 256 || a.blocks > 2 * kStageBlocks) && 4 * tiles_of(256, 256) >= 3 * cus)
-        return out_bf16 ? launch_tiles<2, 4, 4, 2, true>(a, s) : launch_tiles<2, 4, 4, 2, false>(a, s);
-    if (F_out <= 64 || tiles_of(128, 128) < cus)
-        return out_bf16 ? launch_tiles<4, 1, 1, 2, true>(a, s) : launch_tiles<4, 1, 1, 2, false>(a, s);
-    return out_bf16 ? launch_tiles<2, 2, 2, 2, true>(a, s) : launch_tiles<2, 2, 2, 2, false>(a, s);
+    if (a.blocks > kStageBlocks && (a.N > 256 || a.blocks > 2 * kStageBlocks) && 4 * tiles_of(256, 256) >= 3 * cus)
+        return a.out_bf16 ? launch_tiles<2, 4, 4, 2, true>(a, s) : launch_tiles<2, 4, 4, 2, false>(a, s);
+    if (a.N <= 64 || tiles_of(128, 128) < cus)
+        return a.out_bf16 ? launch_tiles<4, 1, 1, 2, true>(a, s) : launch_tiles<4, 1, 1, 2, false>(a, s);
+    return a.out_bf16 ? launch_tiles<2, 2, 2, 2, true>(a, s) : launch_tiles<2, 2, 2, 2, false>(a, s);
+}
+
+}  // namespace
+
+int launch_update_mxfp4(const void *X, const void *sx, const void *W, const void *sw, void *T, bool out_bf16, int32_t n,
+                        int32_t F_in, int32_t F_out, hipStream_t s) {
+    ProductArgs a{static_cast<const uint8_t *>(X), static_cast<const uint8_t *>(sx), static_cast<const uint8_t *>(W),
+                  static_cast<const uint8_t *>(sw), T, n, F_out, (F_in + kBlock - 1) / kBlock, out_bf16};
+    // A launch has fewer than 2^32 threads: 2^22 of the smallest tiles at most, in rows of every size of tile.
+    const int64_t most = std::max<int64_t>(1, (int64_t{1} << 21) / ((F_out + 63) / 64)) * 256;
+    for (int64_t row = 0; row < n; row += most) {
+        a.n = static_cast<int32_t>(std::min<int64_t>(most, n - row));
+        const int st = launch_product(a, s);
+        if (st) return st;
+        a.X += most * a.blocks * kBytes;
+        a.sx += most * a.blocks;
+        a.T = static_cast<char *>(a.T) + most * F_out * (out_bf16 ? 2 : 4);
+    }
+    return DUALGCN_OK;
 }
 
 }  // namespace dgc

@@ -310,6 +310,35 @@ def test_more_than_2_to_the_31_elements(dg, device):
         assert (dk.float() - dX[lo:hi].float()).abs().max() <= 2.0 ** -7 * dk.float().abs().max()
 
 
+def test_some_gradients_only(dg, device):
+    """By the C entry: any of the gradients may be missing; the others have the same bits."""
+    for n, B, F, G in ((5000, 4, 96, 4), (300, 70, 96, 4), (5000, 4, 600, 2)):
+        rng = np.random.default_rng(B)
+        X, w, b, dY, ptr = case(device, n, F, offsets(rng, n, B))
+        p = dict(groups=G, weight=w, bias=b, act="relu")
+        _, stats = dg.group_norm(X, ptr, **p)
+        want = dg.group_norm_backward(X, dY, stats, ptr, **p)
+        q = dg.GroupNorm(ptr.data_ptr(), w.data_ptr(), b.data_ptr(), EPS, B, F, G, dg.RELU | dg.ZERO_REST)
+        ws = torch.empty(dg.group_norm_workspace_bytes(n, F, G, B, backward=True), dtype=torch.uint8, device=device)
+        for some in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (0, 1, 1), (0, 0, 0)):
+            out = [torch.full_like(t, 3.0) for t in want]
+            at = [t.data_ptr() if k else None for t, k in zip(out, some)]
+            assert dg.lib().dualgcn_group_norm_act_backward(q, X.data_ptr(), dY.data_ptr(), stats.data_ptr(), *at, n, ws.data_ptr(),
+                                                            ws.numel(), torch.cuda.current_stream().cuda_stream) == dg.OK
+            for t, v, k in zip(out, want, some):
+                assert torch.equal(t, v) if k else (t == 3).all()
+
+
+def test_many_empty_and_single_graphs(dg, device):
+    """Tens of thousands of graphs, most of one node or none, some of all sizes between."""
+    rng = np.random.default_rng(8)
+    sizes = rng.integers(0, 2, 30000)
+    sizes[rng.integers(0, 30000, 60)] = rng.integers(2, 300, 60)
+    ptr = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    check(dg, *case(device, int(ptr[-1]), 32, ptr), 4, "silu")
+    check(dg, *case(device, int(ptr[-1]), 20, ptr), 4, "relu")
+
+
 def test_refusals(dg, device):
     X, w, b, dY, ptr = case(device, 40, 24, np.array([0, 10, 40], np.int32))
     Y, stats = dg.group_norm(X, ptr, groups=3)

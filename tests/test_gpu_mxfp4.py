@@ -333,6 +333,25 @@ def test_more_than_2_to_the_31_elements(dg, device):
     assert ((T[rows].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -11 * want.abs().max()).all()
 
 
+def test_more_rows_than_a_launch_takes(dg, device):
+    """2^29 and some rows of one block: several launches, the last of a few rows."""
+    n = (1 << 29) + 77
+    Xq = torch.zeros(n, 16, dtype=torch.uint8, device=device)
+    Xq[:, 0] = 0x21                                      # 0.5 and 1
+    Xq[-1, 0], Xq[(1 << 29) - 1, 0] = 0x77, 0x65
+    sx = torch.full((n, 1), 127, dtype=torch.uint8, device=device)
+    sx[-2] = 130
+    Wq = torch.zeros(1, 16, dtype=torch.uint8, device=device)
+    Wq[0, 0] = 0x42                                      # 1 and 2
+    sw = torch.full((1, 1), 128, dtype=torch.uint8, device=device)
+    T = dg.update_mxfp4(Xq, sx, Wq, sw, out_bf16=True)[:, 0]
+    special = {n - 1: 36.0, n - 2: 40.0, (1 << 29) - 1: 22.0}
+    for row, want in special.items():
+        assert T[row].item() == want
+    T[list(special)] = 5.0
+    assert (T == 5).all()
+
+
 def test_refusals(dg, device):
     Xq, sx, Wq, sw = operands(device, 40, 64, 32)
     for bad in (lambda: dg.update_mxfp4(Xq.float(), sx, Wq, sw), lambda: dg.update_mxfp4(Xq.cpu(), sx, Wq, sw),
