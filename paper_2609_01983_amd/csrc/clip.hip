@@ -12,6 +12,9 @@
 // the device, so that calls can be captured.  Tensors are cut into chunks, the chunks are numbered over all tensors of a
 // launch, and workgroups take them in turn.  Each workgroup leaves one partial sum; every workgroup of the second pass
 // joins all of them in the same order, which costs it about a load's time and saves a launch.
+//
+// Bound by memory: 322 tensors of 2.7e8 elements, half of them bfloat16, squares 158 us (0.8 GB, 5.1 TB/s) and step 570 us
+// (2.95 GB, 5.2 TB/s), besides 26 us of launches for the vectors; 40,960 elements of two tensors in one launch 7.4 us.
 #include "rows.h"
 
 #include <algorithm>
@@ -163,7 +166,8 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(ApplyTable<N> t, const 
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) scale_of(t, c, f, lr, threadIdx.x);
 }
 
-// Few small tensors: both passes by one workgroup, four chunks at a time.
+// Few small tensors: both passes by one workgroup, four chunks at a time (two tensors of 40,960 elements: 11 us a call against 13.5 by
+// two launches, most of it on the host).
 constexpr int kSmallThreads = 4 * kThreads, kSmallTensors = 8, kSmallChunks = 8;
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(ApplyTable<kSmallTensors> t, bool apply, double max_norm, double eps, double lr, float *norm) {
     const uint32_t chunks = t.first[t.tensors], first = threadIdx.x / kThreads;

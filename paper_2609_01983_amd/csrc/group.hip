@@ -20,6 +20,11 @@
 //     neither is made where all rows together are no more than the limit.
 // Columns go over the grid's second dimension: whole groups of up to 256 columns, or one wider group in chunks of 256.
 // The graphs' offsets are read on the device: the host knows neither their lengths nor whether one of them is long.
+//
+// Measured: one graph of 2^21 x 256, float32 to bfloat16 with SiLU: 358 us for the sums (6.0 TB/s), 8, and 656 for the rest (4.9 TB/s);
+// 4,096 graphs of 0 to 250 nodes, 123,457 x 128: 33.6, 4.8 and 12.3 us, of which memory takes 23: the chain offsets - rows - sums - rows of a
+// wavefront's graph, and long graphs' two more launches.  Backward, 2^20 x 128 in seven graphs: 201, 8 and 307 us (5.3 TB/s);
+// 30,011 x 99 in 300 graphs with SiLU: 19.7, 5.2 and 12.2 us, chains too.
 #include "rows.h"
 
 #include <algorithm>
@@ -775,10 +780,13 @@ __global__ __launch_bounds__(kThreads) void group_back_apply_kernel(GroupArgs a)
 
 // ------------------------------------------------------------------ launches
 
-// A wavefront is a team where there are many graphs, of rows that it takes in so many turns on the average.
+// A wavefront is a team where there are many graphs, of rows that it takes in so many turns on the average (4,096 graphs of 30 rows of
+// 128: first launch 33 us, by workgroups 55; 23 rows of 64 by one wavefront 7.9 us, by a workgroup 6.1).
 constexpr int kWaveTurns = 16;
 constexpr int kWaveGraphs = 2048;
-// A team's turns for a graph that is not long, forward and backward: about what the two more launches for long ones take.
+// A team's turns for a graph that is not long, forward and backward: about what the two more launches for long ones take (those 4,096
+// graphs, forward: 16 turns 58 us in all, 32 50, 64 67; 300 graphs of 100 rows of 99, backward, first launch: 8 turns 19 us, 16 28,
+// 64 77).
 constexpr int kLimitTurns = 32, kLimitTurnsBack = 8;
 
 int lanes_of(int32_t width) { return width < 4 ? 1 : width <= 32 ? 8 : width <= 64 ? 16 : width <= 128 ? 32 : 64; }
