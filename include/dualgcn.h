@@ -641,7 +641,7 @@ typedef struct dualgcn_group_norm {
     uint32_t flags;
 } dualgcn_group_norm;
 
-/* Bytes of the workspace dualgcn_group_norm_act needs (host only). */
+/* Bytes of the workspace dualgcn_group_norm_act needs (host only); 0 where there are so few rows that it needs none. */
 int dualgcn_group_norm_act_workspace(const dualgcn_group_norm *norm, int32_t n, size_t *bytes);
 
 /*
@@ -657,8 +657,8 @@ int dualgcn_group_norm_act_workspace(const dualgcn_group_norm *norm, int32_t n, 
  * Sums are float64, in a fixed order; u is formed from float32 differences with m as two float32 numbers.
  * n from 1 to 2^31 - 2^22, 1 <= F <= 8192, up to 2^30 graphs (larger: DUALGCN_ERR_UNSUPPORTED); rows may start at
  * any element.
- * `workspace` (device, 256-byte aligned) holds at least dualgcn_group_norm_act_workspace bytes; calls that may run
- * at the same time need one each.  Outputs overlap nothing but as said for Y.  Asynchronous.
+ * `workspace` (device, 256-byte aligned) holds at least dualgcn_group_norm_act_workspace bytes (not looked at where
+ * that is 0); calls that may run at the same time need one each.  Outputs overlap nothing but as said for Y.  Asynchronous.
  */
 int dualgcn_group_norm_act(const dualgcn_group_norm *norm, const void *X, void *Y, double *stats, int32_t n,
                            void *workspace, size_t workspace_bytes, void *stream);

@@ -900,6 +900,8 @@ def _workspace(query, what, p, n, like, workspace, stream):
         return _dev(workspace, torch.uint8, "workspace")
     nbytes = ctypes.c_size_t()
     _check(query(p, n, ctypes.byref(nbytes)), what)
+    if nbytes.value == 0:
+        return None
     return _empty((nbytes.value,), torch.uint8, like, stream)
 
 
@@ -940,8 +942,8 @@ def group_norm(X, ptr=None, *, groups, weight=None, bias=None, act=None, eps=1e-
         _shaped(stats, torch.float64, (p.graphs, groups, 2), "stats")
     workspace = _workspace(_lib.dualgcn_group_norm_act_workspace, "dualgcn_group_norm_act_workspace", p, n, X, workspace,
                            stream)
-    _check(_lib.dualgcn_group_norm_act(p, X.data_ptr(), Y.data_ptr(), stats.data_ptr(), n, workspace.data_ptr(),
-                                       workspace.numel(), s), "dualgcn_group_norm_act")
+    _check(_lib.dualgcn_group_norm_act(p, X.data_ptr(), Y.data_ptr(), stats.data_ptr(), n, _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), s), "dualgcn_group_norm_act")
     return Y, stats
 
 

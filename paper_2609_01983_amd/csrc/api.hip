@@ -806,11 +806,11 @@ int dualgcn_group_norm_act(const dualgcn_group_norm *norm, const void *X, void *
     int st = check_group(norm, n, DUALGCN_OUT_BF16);
     if (st) return st;
     const bool xbf = norm->flags & DUALGCN_IN_BF16, ybf = norm->flags & DUALGCN_OUT_BF16;
-    if (!X || !Y || !stats || !workspace || !elem_aligned(X, xbf) || !elem_aligned(Y, ybf) ||
-        reinterpret_cast<uintptr_t>(stats) % 16 || reinterpret_cast<uintptr_t>(workspace) % 256)
+    if (!X || !Y || !stats || !elem_aligned(X, xbf) || !elem_aligned(Y, ybf) || reinterpret_cast<uintptr_t>(stats) % 16)
         return DUALGCN_ERR_INVALID_ARG;
     const size_t ws = dgc::group_norm_workspace_bytes(*norm, n), elems = static_cast<size_t>(n) * norm->F, vb = vector_bytes(norm->F);
-    if (workspace_bytes < ws) return DUALGCN_ERR_INVALID_ARG;
+    if (ws == 0) workspace = nullptr;
+    else if (!workspace || workspace_bytes < ws || reinterpret_cast<uintptr_t>(workspace) % 256) return DUALGCN_ERR_INVALID_ARG;
     const Span in[] = {{X, elems * (xbf ? 2 : 4)}, {norm->ptr, group_ptr_bytes(*norm)}, {norm->weight, vb}, {norm->bias, vb}};
     const Span out[] = {{Y, elems * (ybf ? 2 : 4), xbf == ybf ? 0 : -1}, {stats, group_stats_bytes(*norm)}, {workspace, ws}};
     if (!apart(in, out)) return DUALGCN_ERR_INVALID_ARG;

@@ -820,9 +820,9 @@ struct Shape {
 
 size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t slot_bytes(const Shape &s, int32_t n, int32_t B, int32_t G) {
-    return n <= s.limit ? 256 : up(sizeof(double2) * (static_cast<size_t>(s.tiles) + B) * G) + up(sizeof(int4) * 2 * static_cast<size_t>(s.tiles));
+    return n <= s.limit ? 0 : up(sizeof(double2) * (static_cast<size_t>(s.tiles) + B) * G) + up(sizeof(int4) * 2 * static_cast<size_t>(s.tiles));
 }
-size_t joined_bytes(const Shape &s, int32_t G) { return up(sizeof(double2) * static_cast<size_t>(s.tiles) * G); }
+size_t joined_bytes(const Shape &s, int32_t n, int32_t G) { return n <= s.limit ? 0 : up(sizeof(double2) * static_cast<size_t>(s.tiles) * G); }
 size_t column_bytes(const Shape &s, int32_t F) { return up(sizeof(double) * 2 * static_cast<size_t>(s.workgroups) * F); }
 
 template <template <int, bool, bool> class Launch>
@@ -911,7 +911,7 @@ size_t group_norm_workspace_bytes(const dualgcn_group_norm &p, int32_t n) { retu
 
 size_t group_norm_backward_workspace_bytes(const dualgcn_group_norm &p, int32_t n) {
     const Shape s = shape_of(p, n, true);
-    return slot_bytes(s, n, graphs_of(p), p.groups) + joined_bytes(s, p.groups) + column_bytes(s, p.F);
+    return slot_bytes(s, n, graphs_of(p), p.groups) + joined_bytes(s, n, p.groups) + column_bytes(s, p.F);
 }
 
 int launch_group_norm(const dualgcn_group_norm &p, const void *X, void *Y, double *stats, int32_t n, void *workspace,
@@ -932,7 +932,7 @@ int launch_group_norm_backward(const dualgcn_group_norm &p, const void *X, const
     a.stats = reinterpret_cast<double2 *>(const_cast<double *>(stats));
     char *more = static_cast<char *>(workspace) + slot_bytes(shape, n, a.B, a.G);
     a.joined = reinterpret_cast<double2 *>(more);
-    more += joined_bytes(shape, a.G);
+    more += joined_bytes(shape, n, a.G);
     a.columns = dweight || dbias ? reinterpret_cast<double *>(more) : nullptr;
     a.dweight = dweight;
     a.dbias = dbias;

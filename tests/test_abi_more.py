@@ -34,7 +34,8 @@ def test_group_norm(dg):
     X, Y, st, ws = (at(k) for k in range(1, 5))
     need = ctypes.c_size_t()
     q = L.dualgcn_group_norm_act_workspace
-    assert q(group(dg), 10, ctypes.byref(need)) == dg.OK and need.value >= 4 * 4 * 16
+    assert q(group(dg), 10, ctypes.byref(need)) == dg.OK and need.value == 0         # no graph can be long
+    assert q(group(dg), 100000, ctypes.byref(need)) == dg.OK and need.value >= 4 * 4 * 16
     assert q(group(dg), 10, None) == dg.ERR_INVALID_ARG and q(group(dg), 0, ctypes.byref(need)) == dg.ERR_INVALID_ARG
     assert q(None, 10, ctypes.byref(need)) == dg.ERR_INVALID_ARG
     assert q(group(dg, F=8192, groups=1), (1 << 31) - (1 << 22), ctypes.byref(need)) == dg.OK
@@ -44,11 +45,13 @@ def test_group_norm(dg):
 
     for k in (dict(), dict(Y=X), dict(ptr=None, graphs=0), dict(w=None, b=None), dict(flags=dg.RELU), dict(flags=dg.SILU | dg.ZERO_REST),
               dict(flags=dg.IN_BF16 | dg.OUT_BF16, X=X + 2, Y=X + 2), dict(F=8192, groups=1, size=1 << 32), dict(F=1, groups=1, n=1),
-              dict(F=3, groups=3), dict(X=X + 4, Y=Y + 4)):
+              dict(F=3, groups=3), dict(X=X + 4, Y=Y + 4), dict(ws=None, size=0), dict(n=100000, size=1 << 32)):
         assert call(**k) == dg.ERR_NO_DEVICE, k
-    for k in PARAMETERS_OUT + [dict(n=0), dict(n=-1), dict(X=None), dict(Y=None), dict(st=None), dict(ws=None), dict(size=64), dict(ws=ws + 64),
+    for k in (dict(ws=None), dict(size=64), dict(ws=ws + 64), dict(Y=ws), dict(ws=X)):
+        assert call(**{**dict(n=100000, size=1 << 32), **k}) == dg.ERR_INVALID_ARG, k
+    for k in PARAMETERS_OUT + [dict(n=0), dict(n=-1), dict(X=None), dict(Y=None), dict(st=None),
                                dict(st=st + 8), dict(Y=X + 4), dict(Y=X, flags=dg.OUT_BF16), dict(Y=st), dict(Y=at(20)), dict(Y=at(21) - 8),
-                               dict(st=X), dict(ws=X), dict(X=X + 2), dict(Y=Y + 1), dict(flags=dg.GRAD_BF16)]:
+                               dict(st=X), dict(X=X + 2), dict(Y=Y + 1), dict(flags=dg.GRAD_BF16)]:
         assert call(**k) == dg.ERR_INVALID_ARG, k
     for k in (dict(F=8193, groups=1), dict(n=(1 << 31) - (1 << 22) + 1), dict(graphs=(1 << 30) + 1)):
         assert call(**k) == dg.ERR_UNSUPPORTED, k

@@ -355,8 +355,10 @@ def test_refusals(dg, device):
                 lambda: dg.group_norm_backward(X, dY, stats, groups=3)):
         with pytest.raises(ValueError):
             bad()
-    for bad in (lambda: dg.group_norm(X, groups=3, eps=0.0), lambda: dg.group_norm(X, ptr, groups=3, Y=X[:, :].view(40, 24), out_bf16=False,
-                                                                                  workspace=torch.empty(64, dtype=torch.uint8, device=device))):
+    large = torch.zeros(5000, 24, device=device)
+    for bad in (lambda: dg.group_norm(X, groups=3, eps=0.0),
+                lambda: dg.group_norm(large, groups=3, workspace=torch.empty(64, dtype=torch.uint8, device=device)),
+                lambda: dg.group_norm_backward(X, dY, stats, ptr, groups=3, weight=w, workspace=torch.empty(64, dtype=torch.uint8, device=device))):
         with pytest.raises(dg.DualGCNError) as e:
             bad()
         assert e.value.status == dg.ERR_INVALID_ARG
