@@ -280,6 +280,7 @@ constexpr uint32_t kFar = 0xFFFFFF00u;               // a byte offset past every
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kStageBlocks = 8;
 constexpr int kStageBytes = kStageBlocks * kBytes;   // of a row
+constexpr int kWaitLds = 0xC07F;                     // s_waitcnt lgkmcnt(0), the other counters as they are
 constexpr int kScaleStages = 4;                           // stages whose scales are read together
 
 // Row i of a matrix instruction is column wide_column(i) of the 32, so that a lane's 16 results are consecutive columns.
@@ -457,16 +458,18 @@ __global__ __launch_bounds__(64 * WR * WC, R * C <= 2 ? 4 : R * C <= 4 ? 3 : 2) 
 #pragma unroll
         for (int k = 0; k < kStageTurns; ++k) {
             if (k % 2 == 0) scales_of(k);
+            // a stage's first operands are waited for here: behind the next turn's reads the compiler waits for those too
+            if (k == 0) __builtin_amdgcn_s_waitcnt(kWaitLds);
             if (k + 1 < kStageTurns) {
                 fetch(stage, k + 1);
             } else {
                 const int next = b0 + kStageBlocks;
                 if (next % kGroupBlocks == 0) keep_scales(next);
                 hand_over();                         // the next stage is there, this one has been read
-                if (next + kStageBlocks < a.blocks) request(stage, next + kStageBlocks);
-                if (next % kGroupBlocks == 0 && next + kGroupBlocks < a.blocks) request_scales(next + kGroupBlocks);
                 fetch_scales(next);
                 fetch(stage ^ 1, 0);
+                if (next + kStageBlocks < a.blocks) request(stage, next + kStageBlocks);
+                if (next % kGroupBlocks == 0 && next + kGroupBlocks < a.blocks) request_scales(next + kGroupBlocks);
             }
             __builtin_amdgcn_sched_barrier(0);
             multiply(k, nx, nw);
@@ -476,6 +479,7 @@ __global__ __launch_bounds__(64 * WR * WC, R * C <= 2 ? 4 : R * C <= 4 ? 3 : 2) 
 #pragma unroll
     for (int k = 0; k < kStageTurns; ++k) {
         if (k % 2 == 0) scales_of(k);
+        if (k == 0) __builtin_amdgcn_s_waitcnt(kWaitLds);
         if (k + 1 < kStageTurns) fetch(stage, k + 1);
         __builtin_amdgcn_sched_barrier(0);
         multiply(k, nx, nw);
