@@ -697,7 +697,8 @@ int dualgcn_grad_norm_workspace(int32_t tensors, size_t *bytes);
 
 /*
  * Training with clipped gradients (dualgcn_weight_grad's own step is applied before the other layers' gradients are
- * known).  grads_h (host; read before the call returns) lists 1 to 2^20 tensors of up to 2^40 elements.  With
+ * known).  grads_h (host; read before the call returns) lists 1 to 2^20 tensors of up to 2^40 elements, 2^42 together
+ * (larger: DUALGCN_ERR_UNSUPPORTED).  With
  *   norm = sqrt(the sum of all elements' squares)   (device, float32[1])
  *   f    = 1 if norm + eps <= max_norm, else max_norm / (norm + eps)
  * dualgcn_grad_norm     norm

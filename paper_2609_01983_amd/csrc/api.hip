@@ -338,6 +338,7 @@ int check_grads(const dualgcn_grad *g, int32_t tensors, int kind, const float *n
         bool out;
     };
     try {
+        int64_t elements = 0;
         std::vector<Range> all;
         all.reserve(3 * static_cast<size_t>(tensors) + 2);
         auto add = [&](const void *p, size_t bytes, bool out) {
@@ -348,7 +349,8 @@ int check_grads(const dualgcn_grad *g, int32_t tensors, int kind, const float *n
         add(workspace, ws, true);
         for (int32_t i = 0; i < tensors; ++i) {
             if (g[i].count < 0 || (g[i].flags & ~DUALGCN_GRAD_BF16)) return DUALGCN_ERR_INVALID_ARG;
-            if (g[i].count > (int64_t{1} << 40)) return DUALGCN_ERR_UNSUPPORTED;
+            // (a table's tensors then have fewer chunks than 32 bits count, also where one is listed many times)
+            if (g[i].count > (int64_t{1} << 40) || (elements += g[i].count) > (int64_t{1} << 42)) return DUALGCN_ERR_UNSUPPORTED;
             if ((!kind && g[i].out) || (kind != 2 && g[i].weight)) return DUALGCN_ERR_INVALID_ARG;
             if (g[i].count && (!g[i].grad || (kind && !g[i].out) || (kind == 2 && !g[i].weight))) return DUALGCN_ERR_INVALID_ARG;
             const bool bf = g[i].flags & DUALGCN_GRAD_BF16;

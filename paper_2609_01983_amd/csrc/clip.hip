@@ -189,11 +189,11 @@ void in_tables(const dualgcn_grad *g, int32_t tensors, Fill fill, Go go) {
     t.first[0] = 0;
     for (int32_t i = 0; i < tensors; ++i) {
         const int64_t chunks = (g[i].count + kChunk - 1) / kChunk;
-        if (t.tensors == N || t.first[t.tensors] + chunks > 0x40000000) {
-            if (t.first[t.tensors]) go(t);
+        if (!chunks) continue;
+        if (t.tensors == N) {
+            go(t);
             t.tensors = 0;
         }
-        if (!chunks) continue;
         t.grad[t.tensors] = g[i].grad;
         t.count[t.tensors] = g[i].flags & DUALGCN_GRAD_BF16 ? -g[i].count : g[i].count;
         fill(t, t.tensors, g[i]);

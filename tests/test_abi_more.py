@@ -139,6 +139,17 @@ def test_clipped_gradients(dg):
         assert step((g[0], w[0], w[0], 10, 0), **k) == dg.ERR_INVALID_ARG
 
 
+def test_clipped_gradients_of_too_many_elements(dg):
+    # one gradient listed often has more chunks of it than a launch's partial sums have places for
+    def call(times, count):
+        t = (dg.Grad * times)(*[dg.Grad(at(1), None, None, count, 0) for _ in range(times)])
+        return dg.lib().dualgcn_grad_norm(t, times, at(40), at(41), 1 << 20, None)
+
+    assert call(5, 1 << 38) == dg.ERR_NO_DEVICE and call(160, 1 << 34) == dg.ERR_NO_DEVICE
+    assert call(200, 1 << 36) == dg.ERR_UNSUPPORTED and call(9, 1 << 39) == dg.ERR_UNSUPPORTED
+    assert call(8, 1 << 39) == dg.ERR_NO_DEVICE
+
+
 def test_mxfp4(dg):
     L = dg.lib()
     X, Q, s, W, sw, T = (at(k) for k in range(1, 7))
