@@ -673,8 +673,8 @@ int dualgcn_group_norm_act_backward_workspace(const dualgcn_group_norm *norm, in
  * DUALGCN_GRAD_BF16) the gradient of Y; dX (in dY's type; may be dY) the gradient of X, on rows of no graph as
  * said for Y; dweight and dbias (device, float32[F]) those of the vectors, over the rows of all graphs; each NULL if it
  * is not wanted.  The sign of weight * u + bias decides what a ReLU passes, as float64 arithmetic gives
- * it.  Sums are float32 over four terms and then float64, in a fixed order.  DUALGCN_OUT_BF16 has no meaning here
- * and is ignored.  Limits, workspace and overlaps as for dualgcn_group_norm_act.  Asynchronous.
+ * it.  Sums are float32 over four terms and then float64, in a fixed order; where a graph's group has 32 elements or fewer, so that next to
+ * nothing may be left of dX's terms, they and dX are formed in float64.  DUALGCN_OUT_BF16 has no meaning here and is ignored.  Limits, workspace and overlaps as for dualgcn_group_norm_act.  Asynchronous.
  */
 int dualgcn_group_norm_act_backward(const dualgcn_group_norm *norm, const void *X, const void *dY, const double *stats,
                                     void *dX, float *dweight, float *dbias, int32_t n, void *workspace,

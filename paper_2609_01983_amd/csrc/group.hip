@@ -36,6 +36,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kSlice = 256;                          // columns of a workgroup at a time, at most
 constexpr int kAhead = 8, kAheadBack = 4;            // rows a thread has in flight, forward and backward
+constexpr int kFew = 32;                             // elements, at most, of a group whose gradient is formed in float64
 
 struct GroupArgs {
     const void *X, *dY;
@@ -538,25 +539,25 @@ struct Backward {
     static constexpr bool TINY = L == 1;
     using Cols = Columns<L, W>;
 
-    // f(place, d, u) for rows [first, first + rows) of graph `number` in chunk `chunk`, where d = dY act'(p).  Next to 0 it is the
+    // f(place, d, u, x) for rows [first, first + rows) of graph `number` in chunk `chunk`, where d = dY act'(p).  Next to 0 it is the
     // sign of p in float64 that decides what a ReLU passes.
-    // after() follows each kAheadBack of a thread's rows.
-    template <class Fn, class After>
+    // after() follows each AHEAD of a thread's rows.
+    template <int AHEAD, class Fn, class After>
     static __device__ __forceinline__ void rows_do(const GroupArgs &a, const Cols &c, const Unit &unit, row_f32x4 weight, row_f32x4 bias, int number,
                                                    int first, int rows, Fn f, After after) {
         const __amdgpu_buffer_rsrc_t wx = rows_of<X_BF>(a, a.X, first, rows), wg = rows_of<G_BF>(a, a.dY, first, rows);
-        for (int row = 0; row < rows; row += c.kRows * kAheadBack) {
-            RawRowQuad<X_BF, TINY> xs[kAheadBack];
-            RawRowQuad<G_BF, TINY> gs[kAheadBack];
-            QuadPlace at[kAheadBack];
+        for (int row = 0; row < rows; row += c.kRows * AHEAD) {
+            RawRowQuad<X_BF, TINY> xs[AHEAD];
+            RawRowQuad<G_BF, TINY> gs[AHEAD];
+            QuadPlace at[AHEAD];
 #pragma unroll
-            for (int k = 0; k < kAheadBack; ++k) {
+            for (int k = 0; k < AHEAD; ++k) {
                 at[k] = c.row(a, row + k * c.kRows, rows);
                 xs[k].load(wx, at[k].at, at[k].count);
                 gs[k].load(wg, at[k].at, at[k].count);
             }
 #pragma unroll
-            for (int k = 0; k < kAheadBack; ++k) {
+            for (int k = 0; k < AHEAD; ++k) {
                 if (row + k * c.kRows + c.slot >= rows) continue;
                 const row_f32x4 x = xs[k].get(c.at, c.odd), u = unit(x);
                 row_f32x4 g = gs[k].get(c.at, c.odd);
@@ -583,7 +584,7 @@ struct Backward {
                         }
                     }
                 }
-                f(at[k], g, u);
+                f(at[k], g, u, x);
                 __builtin_amdgcn_sched_barrier(0);       // a row after the other: four at once take twice the registers
             }
             after();
@@ -611,9 +612,56 @@ struct Backward {
                 m1[i] = static_cast<float>(v.x * one);
                 m2[i] = static_cast<float>(v.y * one);
             }
-            rows_do(a, c, unit, weight, bias, g.number, first, rows, [&](const QuadPlace &at, row_f32x4 d, row_f32x4 u) {
+            rows_do<kAheadBack>(a, c, unit, weight, bias, g.number, first, rows, [&](const QuadPlace &at, row_f32x4 d, row_f32x4 u, row_f32x4) {
                 store_row_quad<G_BF, TINY>(to, at, unit.r * (d * weight - m1 - u * m2), c.odd, a.streaming);
             }, [] {});
+        }
+    }
+    // dX of a graph whose groups have kFew elements at most, and the columns' sums.  What is left of t - mean(t) - u mean(t u) there may be
+    // next to nothing beside its terms (0 of one element, eps r^2 of two), and r up to 1 / sqrt(eps): u, the sums and the difference are
+    // float64.  Both passes go by the same code, so that they have the same d and its roundings cancel as d does.
+    static __device__ __forceinline__ void few(const GroupArgs &a, const Cols &c, const Graph &g, TeamMemory<L, W> &sh, int &turn,
+                                               double (&d1)[4], double (&d2)[4]) {
+        const __amdgpu_buffer_rsrc_t to = rows_of<G_BF>(a, a.out, g.first, g.rows);
+        const row_f32x4 weight = c.vector(a.weight, 1.f), bias = c.vector(a.bias, 0.f);
+        const double2 *stats = a.stats + static_cast<int64_t>(g.number) * a.G;
+        double2 st[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            st[i] = stats[c.group[i]];
+            v[i] = make_double2(0.0, 0.0);
+            d1[i] = d2[i] = 0.0;
+        }
+        const Unit unit = unit_of(a, c, g.number);
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+            rows_do<1>(a, c, unit, weight, bias, g.number, g.first, g.rows, [&](const QuadPlace &at, row_f32x4 d, row_f32x4, row_f32x4 x) {
+                double u[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = (static_cast<double>(x[i]) - st[i].x) * st[i].y;
+                if (pass) {
+                    row_f32x4 y;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = static_cast<float>(st[i].y * (static_cast<double>(d[i]) * weight[i] - v[i].x - u[i] * v[i].y));
+                    store_row_quad<G_BF, TINY>(to, at, y, c.odd, a.streaming);
+                    return;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    d1[i] += d[i];
+                    d2[i] = fma(d[i], u[i], d2[i]);
+                }
+            }, [] {});
+            if (pass || !a.out) break;
+            double t1[4], t2[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (c.first + i >= c.end) d1[i] = d2[i] = 0.0;           // columns behind the last
+                t1[i] = d1[i] * weight[i];
+                t2[i] = d2[i] * weight[i];
+            }
+            const double count = g.count(a);
+            group_sums(a, c, t1, t2, sh, turn, v, [&](int, double2 sums, bool) { return make_double2(sums.x / count, sums.y / count); });
         }
     }
 };
@@ -681,7 +729,7 @@ __global__ __launch_bounds__(kThreads, 3) void group_back_kernel(GroupArgs a) {
             // float32 over kAheadBack rows, then float64
             const row_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
             row_f32x4 s1 = zero, s2 = zero;
-            K::rows_do(a, c, K::unit_of(a, c, number), weight, bias, number, first, rows, [&](const QuadPlace &, row_f32x4 d, row_f32x4 u) {
+            K::template rows_do<kAheadBack>(a, c, K::unit_of(a, c, number), weight, bias, number, first, rows, [&](const QuadPlace &, row_f32x4 d, row_f32x4 u, row_f32x4) {
                 s1 += d;
                 s2 += d * u;
             }, [&] {
@@ -710,6 +758,16 @@ __global__ __launch_bounds__(kThreads, 3) void group_back_kernel(GroupArgs a) {
         for (int b = blockIdx.x * kTeams + team; b < a.B; b += a.graph_groups * kTeams) {
             const int first = offset_of(a, b), rows = offset_of(a, b + 1) - first;
             if (rows > a.limit || rows <= 0) continue;
+            if (rows <= kFew / a.D) {
+                double d1[4], d2[4];
+                K::few(a, c, Graph{b, first, rows}, sh.graph[team], turn, d1, d2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    total.d[i] += d1[i];
+                    total.du[i] += d2[i];
+                }
+                continue;
+            }
             double t1[4], t2[4];
             sum(K(), b, first, rows, t1, t2);
             if (!a.out) continue;
@@ -811,7 +869,8 @@ struct Shape {
         rows = std::min(rows, std::max<int64_t>(1, (int64_t{1} << 26) / F / turn) * turn);       // 32-bit offsets
         tile_rows = static_cast<int32_t>(rows);
         tiles = static_cast<int32_t>((n + rows - 1) / rows);
-        limit = static_cast<int32_t>(std::max(rows, at_once));
+        // (a graph of kFew elements is not long)
+        limit = static_cast<int32_t>(std::max<int64_t>({rows, at_once, back ? kFew / D : 0}));
         const int32_t teams = kWaves / team;
         graph_groups = static_cast<int32_t>(std::min<int64_t>(2 * most, (B - 1) / teams + 1));
         workgroups = graph_groups + tiles;

@@ -339,6 +339,49 @@ def test_many_empty_and_single_graphs(dg, device):
     check(dg, *case(device, int(ptr[-1]), 20, ptr), 4, "relu")
 
 
+@pytest.mark.parametrize("act", [None, "relu", "silu"])
+@pytest.mark.parametrize("F,G", [(1, 1), (8, 8), (12, 4), (64, 16), (99, 99), (300, 300), (300, 150)])
+@pytest.mark.parametrize("B", [9, 2400])
+def test_gradients_of_few_elements(dg, device, B, F, G, act):
+    """What is left of dX in a group of one or two elements is next to nothing beside its terms, r up to 1 / sqrt(eps)
+    times them: 0 for one element, eps r^2 of them for two.  dX = r (I - 1 / c - u u^T / c) t in float64, rounded once: 2^-24
+    of it, and 2^-44 of the terms for float64's own roundings (under a hundred of 2^-53, and the statistics').  t = w dY act'(p) is
+    exact but for SiLU: three units of 2^-23 in the sigmoid s, as many in 1 - s, p off by 8 2^-24 M with M up to 10 times
+    a slope of 1/2 are under 2^-18, and the matrix takes them down as it does t."""
+    rng = np.random.default_rng(B + F)
+    D = F // G
+    rows = np.array([1, 2, 1, 3, 2, 5, 32 // D, 1, 4])[np.arange(B) % 9]
+    rows = np.minimum(rows, 32 // D)
+    ptr = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    n = int(ptr[-1])
+    X, w, b, dY, p = case(device, n, F, ptr, shift=0.2)
+    X *= torch.from_numpy(np.repeat(np.array([1.0, 1e-3, 0.1, 1.0])[np.arange(B) % 4], rows).astype(np.float32)).to(device)[:, None]
+    _, stats = dg.group_norm(X, p, groups=G, weight=w, bias=b, act=act, eps=EPS)
+    got = host(dg.group_norm_backward(X, dY, stats, p, groups=G, weight=w, bias=b, act=act)[0])
+    hX, hg, hw, hb = (host(v) for v in (X, dY, w, b))
+    for c in np.unique(rows):
+        at = ptr[:-1][rows == c][:, None] + np.arange(c)
+
+        def groups(a):                               # [graphs, G, elements]
+            return a[at].reshape(len(at), c, G, D).transpose(0, 2, 1, 3).reshape(len(at), G, c * D)
+
+        x, g, wg, bg = groups(hX), groups(hg), groups(np.broadcast_to(hw, hX.shape)), groups(np.broadcast_to(hb, hX.shape))
+        d = x - x.mean(2, keepdims=True)
+        r = 1 / np.sqrt((d * d).mean(2, keepdims=True) + EPS)
+        u = d * r
+        t = wg * g * groupref.slope(u * wg + bg, act)
+        rest = np.eye(c * D) - 1 / (c * D) - u[..., :, None] * u[..., None, :] / (c * D)
+        want = r * np.matmul(rest, t[..., None])[..., 0]
+        terms = r * (np.abs(t) + np.abs(t).mean(2, keepdims=True) + np.abs(u) * np.abs(t * u).mean(2, keepdims=True))
+        bound = 2.0 ** -24 * np.abs(want) + 2.0 ** -44 * terms
+        if act == "silu":
+            bound += r * np.matmul(np.abs(rest), np.abs(wg * g)[..., None])[..., 0] * 2.0 ** -18
+        off = np.abs(groups(got) - want)
+        assert (off <= bound).all(), (c, off.max(), (off / bound).max())
+        if c * D == 1:
+            assert not groups(got).any()
+
+
 def test_refusals(dg, device):
     X, w, b, dY, ptr = case(device, 40, 24, np.array([0, 10, 40], np.int32))
     Y, stats = dg.group_norm(X, ptr, groups=3)
