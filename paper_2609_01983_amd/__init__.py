@@ -22,6 +22,7 @@ Over the graphs of a batch, and for all weights at once:
     Y, stats = group_norm(X, ptr, groups=8, act="silu")    # and group_norm_backward
     norm = clipped_sgd(weights, grads, lr, max_norm=1.0)   # W -= lr * clipped gradient
 """
+import array
 import collections
 import ctypes
 import os
@@ -987,36 +988,54 @@ def grad_norm_workspace_bytes(tensors):
     return nbytes.value
 
 
-def _flat(t, name):
-    """A float32 or bfloat16 tensor of any shape: is it bfloat16?"""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and
-            (t.dtype is torch.float32 or t.dtype is torch.bfloat16)):
-        _float_or_bf16(t, name)
-    return t.dtype is torch.bfloat16
+def _addresses(tensors, like, dtypes, name, device):
+    """Where the tensors are, each of them in its dtype and in the shape of its tensor of `like`."""
+    if len(tensors) != len(like):
+        raise ValueError(f"as many tensors as gradients: {name}")
+    at = []
+    for t, g, dtype in zip(tensors, like, dtypes):
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous() and t.get_device() == device and t.shape == g.shape):
+            _shaped(t, dtype, g.shape, name)
+            _queue(None, t)
+        at.append(t.data_ptr())
+    return at
 
 
 def _grads(grads, weights, out, norm, workspace, stream):
     """The list of a call on many gradients as the library takes it, and what the call needs beside it."""
     if not grads:
         raise ValueError("no gradients")
-    rows = (Grad * len(grads))()
-    for i, g in enumerate(grads):
-        rows[i].flags = GRAD_BF16 if _flat(g, "a gradient") else 0
-        rows[i].grad, rows[i].count = g.data_ptr(), g.numel()
-    s = _queue(stream, *grads, *(weights or ()), *(out or ()), norm, workspace)
-    if weights is not None:
-        if len(weights) != len(grads):
-            raise ValueError("as many weights as gradients")
-        for i, (w, g) in enumerate(zip(weights, grads)):
-            rows[i].weight = _shaped(w, torch.float32, g.shape, "a weight").data_ptr()
-    if out is not None:
-        if len(out) != len(grads):
-            raise ValueError("as many outputs as gradients")
-        for i, (o, g) in enumerate(zip(out, grads)):
-            rows[i].out = _shaped(o, g.dtype if weights is None else torch.float32, g.shape, "an output").data_ptr()
-    norm = _empty((1,), torch.float32, grads[0], stream) if norm is None else _shaped(norm, torch.float32, (1,), "norm")
+    device, f32, bf16 = torch.cuda.current_device(), torch.float32, torch.bfloat16
+    at, counts, dtypes = [], [], []
+    for g in grads:
+        if not (isinstance(g, torch.Tensor) and ((dtype := g.dtype) is f32 or dtype is bf16) and g.is_contiguous() and g.get_device() == device):
+            if not isinstance(g, torch.Tensor) or g.dtype not in (f32, bf16):
+                raise TypeError("a gradient must be a float32 or bfloat16 tensor")
+            _dev(g, g.dtype, "a gradient")
+            _queue(None, g)
+        at.append(g.data_ptr())
+        counts.append(g.numel())
+        dtypes.append(dtype)
+    s = _queue(stream, norm, workspace)
+    single, none = [f32] * len(at), [0] * len(at)
+    of_weights = none if weights is None else _addresses(weights, grads, single, "a weight", device)
+    if out is None:
+        of_out = none
+    elif weights is None and out is grads:
+        of_out = at
+    elif weights is not None and out is weights:
+        of_out = of_weights
+    else:
+        of_out = _addresses(out, grads, dtypes if weights is None else single, "an output", device)
+    # a Grad is five words
+    words = array.array("Q", [v for row in zip(at, of_weights, of_out, counts, none) for v in row])
+    for i, dtype in enumerate(dtypes):
+        if dtype is bf16:
+            words[5 * i + 4] = GRAD_BF16
+    rows = (Grad * len(at)).from_buffer(words)
+    norm = _empty((1,), f32, grads[0], stream) if norm is None else _shaped(norm, f32, (1,), "norm")
     if workspace is None:
-        workspace = _empty((grad_norm_workspace_bytes(len(grads)),), torch.uint8, grads[0], stream)
+        workspace = _empty((grad_norm_workspace_bytes(len(at)),), torch.uint8, grads[0], stream)
     else:
         _dev(workspace, torch.uint8, "workspace")
     return rows, norm, workspace, s

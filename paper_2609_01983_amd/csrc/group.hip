@@ -23,8 +23,8 @@
 //
 // Measured: one graph of 2^21 x 256, float32 to bfloat16 with SiLU: 358 us for the sums (6.0 TB/s), 8, and 656 for the rest (4.9 TB/s);
 // 4,096 graphs of 0 to 250 nodes, 123,457 x 128: 33.6, 4.8 and 12.3 us, of which memory takes 23: the chain offsets - rows - sums - rows of a
-// wavefront's graph, and long graphs' two more launches.  Backward, 2^20 x 128 in seven graphs: 201, 8 and 307 us (5.3 TB/s);
-// 30,011 x 99 in 300 graphs with SiLU: 19.7, 5.2 and 12.2 us, chains too.
+// wavefront's graph, and long graphs' two more launches.  Backward, 2^20 x 128 in seven graphs: 205, 8 and 312 us (5.2 TB/s);
+// 30,011 x 99 in 300 graphs with SiLU: 21.1, 5.3 and 12.3 us, chains too.
 #include "rows.h"
 
 #include <algorithm>

@@ -199,6 +199,25 @@ def test_streams_and_graphs(dg, device):
             assert torch.equal(cap, norm) and all(torch.equal(a, b) for a, b in zip(out, want))
 
 
+def test_lists_in_place(dg, device):
+    """The same list, or another with the same tensors, is in place; weights cannot go to the gradients' places."""
+    g, w = make(device, [(10,), (4, 5), (0,)]), make(device, [(10,), (4, 5), (0,)])
+    g[1] = g[1].to(torch.bfloat16)
+    want, norm = dg.clip_grads(g, 0.5, out=[torch.empty_like(t) for t in g])
+    new, _ = dg.clipped_sgd(w, g, 0.1, 0.5, out=[torch.empty_like(t) for t in w])
+    for same in (lambda v: v, list, tuple):
+        a, b, c = [t.clone() for t in g], [t.clone() for t in w], [t.clone() for t in g]
+        out, n = dg.clip_grads(a, 0.5, out=same(a))
+        assert torch.equal(n, norm) and all(torch.equal(x, y) for x, y in zip(out, want)) and out[0] is a[0]
+        out, n = dg.clipped_sgd(tuple(b), tuple(c), 0.1, 0.5, out=same(b))
+        assert torch.equal(n, norm) and all(torch.equal(x, y) for x, y in zip(out, new)) and out[0] is b[0]
+    c = [t.float() for t in g]
+    with pytest.raises(dg.DualGCNError):
+        dg.clipped_sgd(w, c, 0.1, 1.0, out=c)
+    with pytest.raises(TypeError):
+        dg.clip_grads(c, 1.0, out=[t.cpu() for t in c])
+
+
 def test_refusals(dg, device):
     g, w = make(device, [(10,), (4, 5)]), make(device, [(10,), (4, 5)])
     for bad in (lambda: dg.grad_norm([]), lambda: dg.clipped_sgd(w[:1], g, 0.1, 1.0), lambda: dg.clip_grads(g, 1.0, out=g[:1]),
