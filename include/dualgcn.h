@@ -654,7 +654,8 @@ int dualgcn_group_norm_act_workspace(const dualgcn_group_norm *norm, int32_t n, 
  * float64[graphs][groups][2], 16-byte aligned) receives m and 1 / sqrt(v + eps), which the backward pass reads (0
  * and 1 / sqrt(eps) for a graph without nodes).  Rows of no graph are left as they were in Y, or
  * with DUALGCN_ZERO_REST filled with zeros.  A group with an infinity or a NaN is NaN throughout.
- * Sums are float64, in a fixed order; u is formed from float32 differences with m as two float32 numbers.
+ * Sums are float64, in a fixed order; u is formed from float32 differences with m as two float32 numbers, halved, so that features may lie
+ * as far apart as float32 reaches.
  * n from 1 to 2^31 - 2^22, 1 <= F <= 8192, up to 2^30 graphs (larger: DUALGCN_ERR_UNSUPPORTED); rows may start at
  * any element.
  * `workspace` (device, 256-byte aligned) holds at least dualgcn_group_norm_act_workspace bytes (not looked at where

@@ -308,16 +308,25 @@ __device__ __forceinline__ double shift_of(const GroupArgs &a, int first, int gr
     return BF ? bf16_to_float(static_cast<const unsigned short *>(a.X)[at]) : static_cast<const float *>(a.X)[at];
 }
 
-// m as two float32 numbers, r, and with them u; for a thread's four columns of one graph.
+// m as two float32 numbers, r, and with them u; for a thread's four columns of one graph.  x - m may be twice float32's largest
+// number, and r, more than 2^-128, is then none of its normal ones: half of x and of m, and 2 r, are in its range (2 r but for a
+// last place).  A product with 1/2 and a difference round once together; halves lose nothing but where x - m is below 2^-125, whose last places
+// they take: there x - m is off by 2^-148 at most.
 struct Unit {
-    row_f32x4 hi, lo, r;
+    row_f32x4 hi, lo, r;                             // of m / 2, and 2 r
     __device__ __forceinline__ void set(int i, double2 st) {
-        hi[i] = static_cast<float>(st.x);
-        lo[i] = static_cast<float>(st.x - hi[i]);
+        const double m = 0.5 * st.x;
+        hi[i] = static_cast<float>(m);
+        lo[i] = static_cast<float>(m - hi[i]);
         if (!(fabsf(hi[i]) < INFINITY)) lo[i] = 0.f;
-        r[i] = static_cast<float>(st.y);
+        r[i] = static_cast<float>(2.0 * st.y);
     }
-    __device__ __forceinline__ row_f32x4 operator()(row_f32x4 x) const { return ((x - hi) - lo) * r; }
+    __device__ __forceinline__ row_f32x4 operator()(row_f32x4 x) const {
+        row_f32x4 u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = (fmaf(0.5f, x[i], -hi[i]) - lo[i]) * r[i];
+        return u;
+    }
 };
 
 // 1 / (1 + exp(-v)) to about 3 units in the last place: exp by base 2, with what the product's rounding leaves off put back.
@@ -613,7 +622,7 @@ struct Backward {
                 m2[i] = static_cast<float>(v.y * one);
             }
             rows_do<kAheadBack>(a, c, unit, weight, bias, g.number, first, rows, [&](const QuadPlace &at, row_f32x4 d, row_f32x4 u, row_f32x4) {
-                store_row_quad<G_BF, TINY>(to, at, unit.r * (d * weight - m1 - u * m2), c.odd, a.streaming);
+                store_row_quad<G_BF, TINY>(to, at, unit.r * (0.5f * (d * weight - m1 - u * m2)), c.odd, a.streaming);
             }, [] {});
         }
     }
