@@ -44,8 +44,8 @@ struct GroupArgs {
     const float *weight, *bias;
     void *out;                                       // Y, or dX
     double2 *stats;                                  // [B][G]: mean, r
-    double2 *slots;                                  // [tiles + B][G] partial sums of long graphs
     int4 *pieces;                                    // [tiles][2] the long graphs of a tile's first and last row: number, first row, rows
+    double2 *slots;                                  // [tiles][2][G] their partial sums there; where one graph has both rows, the first
     double2 *joined;                                 // backward: [tiles][G] the sums of the long graph that starts in a tile
     double *columns;                                 // backward: [workgroups][2][F] sums of d u and d
     float *dweight, *dbias;
@@ -101,8 +101,8 @@ __device__ __forceinline__ void graphs_at(const GroupArgs &a, const int (&row)[2
 }
 __device__ __forceinline__ int tile_end(const GroupArgs &a, int t0) { return t0 + min(a.tile_rows, a.n - t0); }
 
-// f(graph, its first row in the tile, its rows there) for the long graphs of tile [t0, t1), which the first launch finds and
-// writes down for the others.
+// f(graph, its place of two, its first row in the tile, its rows there) for the long graphs of tile [t0, t1), which the first launch
+// finds and writes down for the others.
 template <class Fn>
 __device__ __forceinline__ void long_pieces(const GroupArgs &a, int tile, int t0, int t1, bool find, Fn f) {
     Graph g[2];
@@ -125,7 +125,7 @@ __device__ __forceinline__ void long_pieces(const GroupArgs &a, int tile, int t0
         const Graph one = end ? g[1] : g[0];
         if (one.number < 0 || (end && one.number == g[0].number)) continue;
         const int from = max(one.first, t0);
-        f(one, from, min(one.first + one.rows, t1) - from);
+        f(one, end, from, min(one.first + one.rows, t1) - from);
     }
 }
 
@@ -479,12 +479,12 @@ __global__ __launch_bounds__(kThreads, 4) void group_kernel(GroupArgs a) {
     if (a.fill) zero_rest<L, Y_BF>(a, t0, t1);
     if (a.n <= a.limit) return;
     const Columns<L, kWaves> c(a, 0);
-    long_pieces(a, t, t0, t1, true, [&](const Graph &g, int from, int rows) {
+    long_pieces(a, t, t0, t1, true, [&](const Graph &g, int end, int from, int rows) {
         double s[4], q[4], shift[4];
         Forward<L, kWaves, X_BF, Y_BF>::sum(a, g.first, from, rows, s, q, shift);
         double2 v[4];
         group_sums(a, c, s, q, sh.tile, turn, v, [&](int j, double2 sums, bool mine) {
-            if (mine) a.slots[(static_cast<int64_t>(t) + g.number) * a.G + j] = sums;
+            if (mine) a.slots[(2 * static_cast<int64_t>(t) + end) * a.G + j] = sums;
             return sums;
         });
     });
@@ -502,11 +502,12 @@ __device__ __forceinline__ void join_tile(const GroupArgs &a, int tile, int g0, 
     if (graph.number < 0 || graph.first < tile * a.tile_rows) return;
     const int j = threadIdx.x % kJoinGroups, k = threadIdx.x / kJoinGroups, g = g0 + j;
     const int to = (graph.first + graph.rows - 1) / a.tile_rows;
+    const int last = a.pieces[2 * tile].x != graph.number;               // its place in this tile; in the others it has the first row
     double x = 0.0, y = 0.0;
     if (g < a.G)
 #pragma unroll 4
         for (int t = tile + k; t <= to; t += kLanes) {
-            const double2 v = a.slots[(static_cast<int64_t>(t) + graph.number) * a.G + g];
+            const double2 v = a.slots[(2 * static_cast<int64_t>(t) + (t == tile ? last : 0)) * a.G + g];
             x += v.x;
             y += v.y;
         }
@@ -535,7 +536,7 @@ __global__ __launch_bounds__(kThreads) void group_apply_kernel(GroupArgs a) {
     using K = Forward<L, kWaves, X_BF, Y_BF>;
     const int tile = a.tiles - 1 - static_cast<int>(blockIdx.x), t0 = tile * a.tile_rows, t1 = tile_end(a, t0);
     const typename K::Vectors vectors(a, typename K::Cols(a, 0));
-    long_pieces(a, tile, t0, t1, false, [&](const Graph &g, int from, int rows) {
+    long_pieces(a, tile, t0, t1, false, [&](const Graph &g, int, int from, int rows) {
         const double2 *stats = a.stats + static_cast<int64_t>(g.number) * a.G;
         K::apply(a, from, rows, vectors, [&](const Columns<L, kWaves> &c, int i) { return stats[c.group[i]]; });
     });
@@ -790,13 +791,13 @@ __global__ __launch_bounds__(kThreads, 3) void group_back_kernel(GroupArgs a) {
         const int t = static_cast<int>(blockIdx.x) - a.graph_groups, t0 = t * a.tile_rows, t1 = tile_end(a, t0);
         if (a.fill && a.out) zero_rest<L, G_BF>(a, t0, t1);
         if (a.n > a.limit)
-            long_pieces(a, t, t0, t1, true, [&](const Graph &g, int from, int rows) {
+            long_pieces(a, t, t0, t1, true, [&](const Graph &g, int end, int from, int rows) {
                 double s1[4], s2[4];
                 sum(K(), g.number, from, rows, s1, s2);
                 if (!a.out) return;
                 double2 v[4];
                 group_sums(a, c, s1, s2, sh.tile, turn, v, [&](int j, double2 sums, bool mine) {
-                    if (mine) a.slots[(static_cast<int64_t>(t) + g.number) * a.G + j] = sums;
+                    if (mine) a.slots[(2 * static_cast<int64_t>(t) + end) * a.G + j] = sums;
                     return sums;
                 });
             });
@@ -839,7 +840,7 @@ __global__ __launch_bounds__(kThreads) void group_back_join_kernel(GroupArgs a, 
 template <int L, bool X_BF, bool G_BF>
 __global__ __launch_bounds__(kThreads) void group_back_apply_kernel(GroupArgs a) {
     const int tile = a.tiles - 1 - static_cast<int>(blockIdx.x), t0 = tile * a.tile_rows, t1 = tile_end(a, t0);
-    long_pieces(a, tile, t0, t1, false, [&](const Graph &g, int from, int rows) {
+    long_pieces(a, tile, t0, t1, false, [&](const Graph &g, int, int from, int rows) {
         const double2 *sums = a.joined + static_cast<int64_t>(g.first / a.tile_rows) * a.G;
         Backward<L, kWaves, X_BF, G_BF>::apply(a, g, from, rows, [&](const Columns<L, kWaves> &c, int i) { return sums[c.group[i]]; });
     });
@@ -887,8 +888,8 @@ struct Shape {
 };
 
 size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
-size_t slot_bytes(const Shape &s, int32_t n, int32_t B, int32_t G) {
-    return n <= s.limit ? 0 : up(sizeof(double2) * (static_cast<size_t>(s.tiles) + B) * G) + up(sizeof(int4) * 2 * static_cast<size_t>(s.tiles));
+size_t slot_bytes(const Shape &s, int32_t n, int32_t G) {
+    return n <= s.limit ? 0 : up(sizeof(double2) * 2 * static_cast<size_t>(s.tiles) * G) + up(sizeof(int4) * 2 * static_cast<size_t>(s.tiles));
 }
 size_t joined_bytes(const Shape &s, int32_t n, int32_t G) { return n <= s.limit ? 0 : up(sizeof(double2) * static_cast<size_t>(s.tiles) * G); }
 size_t column_bytes(const Shape &s, int32_t F) { return up(sizeof(double) * 2 * static_cast<size_t>(s.workgroups) * F); }
@@ -969,17 +970,17 @@ GroupArgs common(const dualgcn_group_norm &p, const void *X, int32_t n, const Sh
     a.fill = p.flags & DUALGCN_ZERO_REST;
     a.streaming = static_cast<int64_t>(n) * p.F >= int64_t{1} << 26;
     a.slots = static_cast<double2 *>(workspace);
-    a.pieces = reinterpret_cast<int4 *>(static_cast<char *>(workspace) + up(sizeof(double2) * (static_cast<size_t>(s.tiles) + a.B) * a.G));
+    a.pieces = reinterpret_cast<int4 *>(static_cast<char *>(workspace) + up(sizeof(double2) * 2 * static_cast<size_t>(s.tiles) * a.G));
     return a;
 }
 
 }  // namespace
 
-size_t group_norm_workspace_bytes(const dualgcn_group_norm &p, int32_t n) { return slot_bytes(shape_of(p, n, false), n, graphs_of(p), p.groups); }
+size_t group_norm_workspace_bytes(const dualgcn_group_norm &p, int32_t n) { return slot_bytes(shape_of(p, n, false), n, p.groups); }
 
 size_t group_norm_backward_workspace_bytes(const dualgcn_group_norm &p, int32_t n) {
     const Shape s = shape_of(p, n, true);
-    return slot_bytes(s, n, graphs_of(p), p.groups) + joined_bytes(s, n, p.groups) + column_bytes(s, p.F);
+    return slot_bytes(s, n, p.groups) + joined_bytes(s, n, p.groups) + column_bytes(s, p.F);
 }
 
 int launch_group_norm(const dualgcn_group_norm &p, const void *X, void *Y, double *stats, int32_t n, void *workspace,
@@ -998,7 +999,7 @@ int launch_group_norm_backward(const dualgcn_group_norm &p, const void *X, const
     a.dY = dY;
     a.out = dX;
     a.stats = reinterpret_cast<double2 *>(const_cast<double *>(stats));
-    char *more = static_cast<char *>(workspace) + slot_bytes(shape, n, a.B, a.G);
+    char *more = static_cast<char *>(workspace) + slot_bytes(shape, n, a.G);
     a.joined = reinterpret_cast<double2 *>(more);
     more += joined_bytes(shape, n, a.G);
     a.columns = dweight || dbias ? reinterpret_cast<double *>(more) : nullptr;
