@@ -10,8 +10,9 @@
 //
 // A launch takes up to a few hundred tensors, whose addresses and sizes are its arguments: nothing is copied to
 // the device, so that calls can be captured.  Tensors are cut into chunks, the chunks are numbered over all tensors of a
-// launch, and workgroups take them in turn.  Each workgroup leaves one partial sum; every workgroup of the second pass
-// joins all of them in the same order, which costs it about a load's time and saves a launch.
+// launch, and workgroups take them in turn.  Each workgroup leaves one partial sum; where those are no more than one launch's,
+// every workgroup of the second pass joins all of them in the same order, which costs it about a load's time and saves a launch; where there
+// are more, one workgroup joins them first, in that order too.
 //
 // Bound by memory: 322 tensors of 2.7e8 elements, half of them bfloat16, squares 158 us (0.8 GB, 5.1 TB/s) and step 570 us
 // (2.95 GB, 5.2 TB/s), besides 26 us of launches for the vectors; 40,960 elements of two tensors in one launch 7.4 us.
@@ -108,12 +109,24 @@ __global__ __launch_bounds__(kThreads) void square_kernel(SumTable<N> t, double 
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-// sqrt of the partial sums' sum, in a fixed order.
-__device__ __forceinline__ double norm_of(const double *__restrict__ partial, int32_t partials) {
+// The partial sums' sum, in a fixed order; the norm is its root.
+__device__ __forceinline__ double sum_of(const double *partial, int32_t partials) {
     double s = 0.0;
 #pragma unroll 8
     for (int i = threadIdx.x; i < partials; i += kThreads) s += partial[i];
-    return sqrt(block_sum<kThreads>(s));
+    return block_sum<kThreads>(s);
+}
+__device__ __forceinline__ double norm_of(const double *__restrict__ partial, int32_t partials) { return sqrt(sum_of(partial, partials)); }
+
+// Partial sums that every workgroup of the second pass joins for itself, at most; that takes time by their number times the tensors', a launch
+// before it 3 to 4 us (steps in us, each for itself and by a launch: 9 tensors of 8,192 elements 36.8, 40.1; 160 of 131,072, 2,048
+// partial sums, 68.0, 69.2; 320, 4,096 sums, 155, 149; 640 336, 311; 2,000 1,181, 885; 10^5 of 100 elements 22,600, 10,100).
+constexpr int32_t kJoined = kGrid;
+
+// Leaves the partial sums' sum in the place of the first.
+__global__ __launch_bounds__(kThreads) void join_kernel(double *partial, int32_t partials) {
+    const double s = sum_of(partial, partials);
+    if (threadIdx.x == 0) *partial = s;              // (all have been read: the sum needs every thread's)
 }
 
 __global__ __launch_bounds__(kThreads) void norm_kernel(const double *__restrict__ partial, int32_t partials, float *norm) {
@@ -224,6 +237,10 @@ int launch_tables(const dualgcn_grad *g, int32_t tensors, bool apply, double max
             hipLaunchKernelGGL(square_kernel<S>, dim3(grid), dim3(kThreads), 0, s, t, partial + partials);
             partials += grid;
         });
+    if (apply && partials > kJoined) {
+        hipLaunchKernelGGL(join_kernel, dim3(1), dim3(kThreads), 0, s, partial, partials);
+        partials = 1;
+    }
     if (apply)
         in_tables<ApplyTable<A>, A>(
             g, tensors,
