@@ -295,9 +295,10 @@ __device__ __forceinline__ double reciprocal_root(double x) {
     return y;
 }
 
-// The mean and r from sums of x - shift and its square.
+// The mean and r from sums of x - shift and its square.  The quotient's rest is divided too: a mean that float64 holds is met exactly, so that
+// elements that are their group's mean (as whole numbers often are) are on no side of it.
 __device__ __forceinline__ double2 statistics(double2 sums, double shift, double count, double eps) {
-    const double one = reciprocal(count), d = sums.x * one, v = fma(sums.y, one, -d * d);
+    const double one = reciprocal(count), about = sums.x * one, d = fma(fma(-about, count, sums.x), one, about), v = fma(sums.y, one, -d * d);
     return make_double2(shift + d, reciprocal_root((v > 0.0 ? v : v != v ? v : 0.0) + eps));
 }
 
