@@ -735,8 +735,10 @@ int dualgcn_clipped_sgd(const dualgcn_grad *grads_h, int32_t tensors, double max
  * n x 16 blocks bytes) and scales (device, n x blocks bytes).  A scale is the least power of two, 2^-127 or more,
  * that brings the block's largest magnitude to 7 or below (1 for zeros); elements are divided by it and
  * rounded once, to nearest even, and what is then above 6 to 6: no element is off by more than half a
- * step.  A block with an infinity or a NaN has the scale NaN.  1 <= F < 2^20; n ceil(F / 32) < 2^32 - 256 (larger:
- * DUALGCN_ERR_UNSUPPORTED).  Q 16-byte aligned.  Asynchronous.
+ * step.  (Quantisers of this form often take 2^(floor(log2 of the largest) - 2): the scale here is twice that where
+ * the largest is over 1.75 times a power of two.  Their operands are read as well as these.)  A block with an infinity
+ * or a NaN has the scale NaN.  1 <= F < 2^20; n ceil(F / 32) < 2^32 - 256 (larger: DUALGCN_ERR_UNSUPPORTED).  Q 16-byte
+ * aligned.  Asynchronous.
  *
  * dualgcn_quantize_weight_mxfp4 -- W (device, float32 F_in x F_out row-major) as dualgcn_update_mxfp4 reads it: with
  * `transpose` not 0, Q is F_out rows of F_in elements (for X W); with 0, F_in rows of F_out elements (for G W^T,

@@ -12,7 +12,7 @@
 // variance then loses nothing where the mean is large beside it, and is 0 for equal elements).  The differences
 // x - m are formed with m as two float32 numbers, so that they are as exact as float32 can be.
 //
-// A team of one wavefront (where graphs are short) or of a workgroup's four takes
+// A team of one wavefront (where graphs are many and short) or of a workgroup's four takes
 //   graphs of up to `limit` rows whole: its second reading of the rows comes from the caches;
 // and a workgroup
 //   tiles of at most `limit` rows, of which it sums the pieces of longer graphs.  Such a graph has more rows than a tile, so that
@@ -21,10 +21,10 @@
 // Columns go over the grid's second dimension: whole groups of up to 256 columns, or one wider group in chunks of 256.
 // The graphs' offsets are read on the device: the host knows neither their lengths nor whether one of them is long.
 //
-// Measured: one graph of 2^21 x 256, float32 to bfloat16 with SiLU: 358 us for the sums (6.0 TB/s), 8, and 656 for the rest (4.9 TB/s);
-// 4,096 graphs of 0 to 250 nodes, 123,457 x 128: 33.6, 4.8 and 12.3 us, of which memory takes 23: the chain offsets - rows - sums - rows of a
-// wavefront's graph, and long graphs' two more launches.  Backward, 2^20 x 128 in seven graphs: 205, 8 and 312 us (5.2 TB/s);
-// 30,011 x 99 in 300 graphs with SiLU: 21.1, 5.3 and 12.3 us, chains too.
+// Measured: one graph of 2^21 x 256, float32 to bfloat16 with SiLU: 358 us for the sums (6.0 TB/s), 8, and 668 for the rest (4.8 TB/s);
+// 4,096 graphs of 0 to 250 nodes, 123,457 x 128: 33.9, 4.8 and 12.4 us, of which memory takes 23: the chain offsets - rows - sums - rows of a
+// wavefront's graph, and long graphs' two more launches.  Backward, 2^20 x 128 in seven graphs: 202, 9 and 311 us (5.2 TB/s);
+// 30,011 x 99 in 300 graphs with SiLU: 20.7, 5.3 and 12.6 us, chains too.
 #include "rows.h"
 
 #include <algorithm>
@@ -849,13 +849,21 @@ __global__ __launch_bounds__(kThreads) void group_back_apply_kernel(GroupArgs a)
 
 // ------------------------------------------------------------------ launches
 
-// A wavefront is a team where there are many graphs, of rows that it takes in so many turns on the average (4,096 graphs of 30 rows of
-// 128: first launch 33 us, by workgroups 55; 23 rows of 64 by one wavefront 7.9 us, by a workgroup 6.1).
+// A wavefront is a team where there are many graphs, of rows that it takes in so many turns on the average.  Calls in us, forward and
+// backward, by wavefronts and by workgroups: graphs of about 30 rows of 64 features, 1,024 of them 16.2, 34.7 and 15.5, 31.8; 2,048
+// 18.8, 54.5 and 24.2, 48.4; 4,096 24.8, 94.5 and 37.0, 69.7; 8,192 39.6, 79.9 and 62.9, 114; of 128 features, 1,024 24.5, 53.4 and 18.7, 40.8;
+// 2,048 29.1, 90.9 and 26.5, 60.4; 4,096 40.4, 79.0 and 41.5, 93.1; 8,192 72.3, 140 and 73.9, 186; 65,536 471, 835 and 599, 1,153.  (23 rows of 64
+// by one wavefront 7.9, by a workgroup 6.1.)
 constexpr int kWaveTurns = 16;
 constexpr int kWaveGraphs = 2048;
-// A team's turns for a graph that is not long, forward and backward: about what the two more launches for long ones take (those 4,096
-// graphs, forward: 16 turns 58 us in all, 32 50, 64 67; 300 graphs of 100 rows of 99, backward, first launch: 8 turns 19 us, 16 28,
-// 64 77).
+// A team's turns, at least, for a graph that is not long, forward and backward: about what the two more launches for long ones take (calls
+// with half as many, these and twice as many, graphs cut at random: 4,096 of 30 rows of 128 features forward 60.2, 48.1, 64.9 us; of 100 rows on
+// the average, 300 of 128 25.1, 34.0, 46.2 and backward 39.1, 33.8, 39.5; 1,000 of 128 40.1, 46.5, 64.5 and 89.5, 73.4, 71.2; 4,000 of 64
+// 66.8, 87.4, 74.6 and 164, 153, 141).  No graph of fewer rows than a tile is long, however: where there would be more than
+// 4 * 1,024 tiles of so many turns, a tile has a 1,024th of the rows, and a team's graph may have as many.  One that is much longer than
+// the others then ends the launch by itself: among 65,536 graphs of 32 rows of 128 on the average, where tiles have 2,048 rows, one of 1,937 makes 985 us of 471
+// forward and 1,575 of 835 backward (by workgroups 742 of 599 and 1,329 of 1,153); among 300,000 of 56 rows of 64 one of 16,057 rows 4,050 us of
+// 1,794 and 6,035 of 3,148.
 constexpr int kLimitTurns = 32, kLimitTurnsBack = 8;
 
 int lanes_of(int32_t width) { return width < 4 ? 1 : width <= 32 ? 8 : width <= 64 ? 16 : width <= 128 ? 32 : 64; }

@@ -137,7 +137,8 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(const void *__restri
 }
 
 // W (rows x cols, float32) transposed: a lane takes a block down a column, 32 loads of which each is a line
-// or two for the wavefront.
+// or two for the wavefront.  Up to 1,024 x 1,024 5.8 us a call, 4,096 x 4,096 14.2 (5.3 TB/s; as it stands, by the kernel above, 12.3),
+// 16,384 x 16,384 338 (3.6 TB/s; 229).
 __global__ __launch_bounds__(kThreads) void quantize_transposed_kernel(const float *__restrict__ W, int32_t rows,
                                                                        int32_t cols, uint8_t *__restrict__ Q,
                                                                        uint8_t *__restrict__ scales, int32_t blocks) {
